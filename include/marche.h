@@ -380,6 +380,160 @@ marche_status_t marche_diffusion_sample(const marche_head_t *head, const marche_
                                         float temperature, float *tok_out, void *workspace,
                                         size_t workspace_bytes, marche_stream_t stream);
 
+/* ---- Paged key/value cache ----
+ * A cache for sequences of different lengths that share one pool of pages,
+ * held in bf16 or in 8 bits.  Everything in it is as in the resident cache
+ * (keys and values per layer, head and token); a sequence's token t lies in
+ * page page_table[b][t / page_size], slot t % page_size.
+ *
+ * Formats.  In the 8-bit formats one exponent byte per (layer, page, head,
+ * slot) goes with the head_dim values of a key or value row, which stand for
+ *   value = q * 2^(code - 127),   q an e4m3 number (bias 7, largest 448) or an
+ *                                 integer in [-127, 127].
+ * Rows are quantised as they are written: with the largest magnitude A of the
+ * row and M = 448 or 127, e is the least integer >= -111 with A <= M * 2^e, code =
+ * e + 127, and q = x * 2^-e rounded to the format, ties to even.  Powers of two
+ * make this, and reading back, independent of the order of operations, and
+ * q * 2^e is exact in bf16.  A row with an infinity or a NaN is stored as
+ * q = NaN (E4M3) or 0 (INT8) with code 255 and reads back as NaN throughout. */
+typedef enum {
+  MARCHE_CACHE_BF16 = 0,
+  MARCHE_CACHE_E4M3 = 1,
+  MARCHE_CACHE_INT8 = 2
+} marche_cache_format_t;
+
+/* The pool (device buffers of the caller; host struct).
+ *   k, v            [n_layers][n_pages][n_heads][page_size][head_dim] of `format`
+ *   k_exp, v_exp    [n_layers][n_pages][n_heads][page_size] bytes (8-bit
+ *                   formats; not read otherwise)
+ *   bounds          [n_layers][n_pages][n_heads][2][head_dim] int8, largest then
+ *                   smallest key channels, and bounds_exp [n_layers][n_pages]
+ *                   [n_heads] bytes: see marche_paged_bounds (both NULL in a
+ *                   cache whose pages are never selected)
+ * n_heads counts key/value heads; the calls with queries take n_q_heads, a multiple
+ * of it, and query head h reads key head h / (n_q_heads / n_heads).  head_dim in
+ * {64, 80, 128}; page_size in {16, 32, 64, 128, 256}; pointers 16-byte aligned.
+ * The struct may be filled directly or by marche_paged_cache_init, which places the
+ * parts one after the other in one buffer in the order k, v, k_exp, v_exp
+ * (8-bit formats only), bounds, bounds_exp (with_bounds only), each at
+ * the next multiple of 256 bytes; marche_paged_cache_bytes gives that buffer's
+ * size (0 for a shape that is not supported).  Nothing is cleared: a token is read only after it
+ * was written, as far as lens say so. */
+typedef struct {
+  void *k, *v;
+  uint8_t *k_exp, *v_exp;
+  int8_t *bounds;
+  uint8_t *bounds_exp;
+  int32_t n_layers, n_pages, n_heads, page_size, head_dim;
+  int32_t format; /* marche_cache_format_t */
+} marche_paged_cache_t;
+
+size_t marche_paged_cache_bytes(int32_t n_layers, int32_t n_pages, int32_t n_heads,
+                                int32_t page_size, int32_t head_dim, int32_t format,
+                                int32_t with_bounds);
+marche_status_t marche_paged_cache_init(marche_paged_cache_t *cache, int32_t n_layers,
+                                        int32_t n_pages, int32_t n_heads, int32_t page_size,
+                                        int32_t head_dim, int32_t format, int32_t with_bounds,
+                                        void *buffer, size_t bytes);
+
+/* The calls below run on one layer of the cache and share these arguments:
+ *   page_table [n_seqs][max_pages] int32 (device): the pool page of each logical
+ *     page.  Only the entries of pages that hold a sequence's tokens are used; two
+ *     sequences may share pages that both only read.  An id outside
+ *     [0, n_pages) is never dereferenced: to the readers such a page
+ *     holds no tokens, and rows for it are not written.
+ *   lens [n_seqs] int32 (device): cached tokens of each sequence, among them any
+ *     written for this step.  0 is allowed; what exceeds max_pages * page_size is
+ *     ignored.
+ *   rows in CSR form as marche_step's active lists: sequence b owns rows
+ *     off[b] .. off[b+1] (device; NULL: every sequence owns total / n_seqs rows,
+ *     which must divide evenly).  Rows that belong to no sequence are
+ *     neither read nor written.
+ * dtype is the type of the rows outside the cache (queries, outputs, new keys
+ * and values): MARCHE_F32 or MARCHE_BF16.  Strides count elements between
+ * consecutive rows, are at least a row's length and a multiple of 8;
+ * row and output pointers are 16-byte aligned.
+ * Device lists are preconditions, as for marche_step; MARCHE_VALIDATE copies them to the
+ * host and checks them there before anything is launched (host sync; not under
+ * stream capture), returning INVALID_ARG with the sequence named. */
+
+/* Writes new keys and values into the cache: row r of sequence b becomes token
+ * a_idx[r] (>= 0; distinct within a sequence) of it, quantised as above (bf16
+ * caches: rounded to nearest even).  k_new, v_new: rows of [n_heads][head_dim]
+ * elements of `dtype` at distance row_stride, so slices of a fused projection's
+ * output will do.  A token at or past max_pages * page_size is not written.
+ * a_total * n_heads < 2^31. */
+marche_status_t marche_paged_write(const marche_paged_cache_t *cache, int32_t layer,
+                                   const int32_t *page_table, int32_t max_pages, int32_t n_seqs,
+                                   const int32_t *a_idx, const int32_t *a_off, int32_t a_total,
+                                   const void *k_new, const void *v_new, int64_t row_stride,
+                                   int32_t dtype, marche_stream_t stream);
+
+/* Reads cached tokens back in the resident layout of marche_attention_segments:
+ * k_out, v_out [n_seqs][n_heads][n_tokens][head_dim] of `dtype`, tokens
+ * j < min(lens[b], n_tokens) written, the others left as they are. */
+marche_status_t marche_paged_read(const marche_paged_cache_t *cache, int32_t layer,
+                                  const int32_t *page_table, int32_t max_pages,
+                                  const int32_t *lens, int32_t n_seqs, int32_t n_tokens,
+                                  void *k_out, void *v_out, int32_t dtype,
+                                  marche_stream_t stream);
+
+/* Key bounds of pages, for marche_paged_select: per page and head the largest
+ * and the smallest value of each key channel over the page's tokens below
+ * lens[b], as int8 with one exponent for both (quantised as an INT8 row of 2 *
+ * head_dim values; code 255 where a key is not finite).  Updates the pages of
+ * sequence b from the one of token first[b] on (first NULL: from page 0), at
+ * most `span` of them: after one appended token, first[b] = lens[b] - 1 and
+ * span = 1; after rows written anywhere, first NULL and span = max_pages.
+ * n_seqs * span * n_heads < 2^31.  Needs cache->bounds. */
+marche_status_t marche_paged_bounds(const marche_paged_cache_t *cache, int32_t layer,
+                                    const int32_t *page_table, int32_t max_pages,
+                                    const int32_t *lens, const int32_t *first, int32_t span,
+                                    int32_t n_seqs, marche_stream_t stream);
+
+/* For each query row and key head the n_select pages of its sequence whose
+ * bounds promise the highest logits.  The row's queries are quantised as INT8
+ * rows, and
+ *   score = max over the query heads of the key head of
+ *           2^(eq + eb) * sum_d (q_d > 0 ? q_d * hi_d : q_d * lo_d),
+ * a whole number times a power of two: exact, whatever the order (scores below
+ * the float32 range count as 0).  Equal scores go to the lower page, NaN (a
+ * query or a key that is not finite) ranks below every number.  Logical pages are written in ascending
+ * order to pages[r][head][0 .. n_select), then -1 where the sequence has fewer.
+ * q: rows of [n_q_heads][head_dim], q_stride apart.  1 <= n_select,
+ * max_pages <= 4096.  Needs cache->bounds, up to date for every page below lens. */
+marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t layer,
+                                    const int32_t *page_table, int32_t max_pages,
+                                    const int32_t *lens, int32_t n_seqs, const void *q,
+                                    int64_t q_stride, const int32_t *q_off, int32_t q_total,
+                                    int32_t n_q_heads, int32_t dtype, int32_t n_select,
+                                    int32_t *pages, marche_stream_t stream);
+
+/* Attention of query rows over their sequences' cached tokens:
+ *   o[r][h] = sum_j softmax_j(q[r][h] . K[j] / sqrt(head_dim)) V[j],  j < lens[b],
+ * or, with `pages` (layout as marche_paged_select writes it), only over the
+ * tokens of the logical pages listed for row r and h's key head; entries
+ * outside the sequence's pages are ignored and a page counts once however often
+ * it is listed.  A row without any token gets zeros.  One row per sequence (a
+ * newly written token's) and many (an image's active rows, or all of
+ * them) run the same code; long caches are split over workgroups and the
+ * parts joined, so a row's rounding may depend on the sizes of its call.
+ * q_max is the largest number of rows of a sequence and len_max the largest
+ * length (host copies, for launch geometry).  o: [q_total][n_q_heads * head_dim].
+ * pages NULL: n_select is 0.  With pages: max_pages <= 4096.  workspace:
+ * marche_paged_attention_workspace_bytes, 256-byte aligned (may be 0 bytes). */
+size_t marche_paged_attention_workspace_bytes(const marche_paged_cache_t *cache, int32_t n_seqs,
+                                              int32_t q_total, int32_t q_max, int32_t n_q_heads,
+                                              int32_t len_max, int32_t n_select);
+marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_t layer,
+                                       const int32_t *page_table, int32_t max_pages,
+                                       const int32_t *lens, int32_t len_max, int32_t n_seqs,
+                                       const void *q, int64_t q_stride, const int32_t *q_off,
+                                       int32_t q_total, int32_t q_max, int32_t n_q_heads,
+                                       int32_t dtype, void *o, const int32_t *pages,
+                                       int32_t n_select, void *workspace, size_t workspace_bytes,
+                                       marche_stream_t stream);
+
 /* Name of a status code (static string). */
 const char *marche_status_string(marche_status_t s);
 

@@ -22,6 +22,7 @@ MARCHE_F32, MARCHE_BF16 = 0, 1
 
 MARCHE_SELECT_HIGHEST, MARCHE_SELECT_LOWEST = 0, 1
 MARCHE_ATTN_TWO_SEGMENT, MARCHE_ATTN_CONCAT = 0, 1
+MARCHE_CACHE_BF16, MARCHE_CACHE_E4M3, MARCHE_CACHE_INT8 = 0, 1, 2
 
 EXPORTED = (
     "kv_cache_init", "marche_step_workspace_bytes", "marche_step", "marche_step_images",
@@ -30,6 +31,9 @@ EXPORTED = (
     "marche_decoder_input", "marche_attention_workspace_bytes", "marche_attention_segments",
     "marche_encoder_input", "marche_encoder_to_decoder_workspace_bytes",
     "marche_encoder_to_decoder", "marche_diffusion_workspace_bytes", "marche_diffusion_sample",
+    "marche_paged_cache_bytes", "marche_paged_cache_init", "marche_paged_write",
+    "marche_paged_read", "marche_paged_bounds", "marche_paged_select",
+    "marche_paged_attention_workspace_bytes", "marche_paged_attention",
     "marche_status_string", "marche_last_error",
     "marche_profile_enable", "marche_profile_collect", "marche_profile_entry",
     "marche_profile_reset",
@@ -63,6 +67,12 @@ class HeadWeights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("w_t1", "b_t1", "w_t2", "b_t2", "w_c", "b_c", "w_in",
                                           "b_in", "w_ada", "b_ada", "w_1", "b_1", "w_2", "b_2",
                                           "w_out", "b_out")]
+
+
+class PagedCache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_exp", "v_exp", "bounds", "bounds_exp")] + [
+        (n, C.c_int32) for n in ("n_layers", "n_pages", "n_heads", "page_size", "head_dim",
+                                 "format")]
 
 
 class MarcheError(RuntimeError):
@@ -110,6 +120,19 @@ def lib() -> C.CDLL:
         L.marche_diffusion_sample.argtypes = [C.POINTER(Head), C.POINTER(HeadWeights), vp, i32,
                                               i32, vp, vp, C.c_float, vp, vp, vp, i32, vp, i32,
                                               C.c_float, vp, vp, sz, vp]
+        pc, i64 = C.POINTER(PagedCache), C.c_int64
+        L.marche_paged_cache_bytes.argtypes = [i32] * 7
+        L.marche_paged_cache_bytes.restype = sz
+        L.marche_paged_cache_init.argtypes = [pc] + [i32] * 7 + [vp, sz]
+        L.marche_paged_write.argtypes = [pc, i32, vp, i32, i32, vp, vp, i32, vp, vp, i64, i32, vp]
+        L.marche_paged_read.argtypes = [pc, i32, vp, i32, vp, i32, i32, vp, vp, i32, vp]
+        L.marche_paged_bounds.argtypes = [pc, i32, vp, i32, vp, vp, i32, i32, vp]
+        L.marche_paged_select.argtypes = [pc, i32, vp, i32, vp, i32, vp, i64, vp, i32, i32, i32,
+                                          i32, vp, vp]
+        L.marche_paged_attention_workspace_bytes.argtypes = [pc] + [i32] * 6
+        L.marche_paged_attention_workspace_bytes.restype = sz
+        L.marche_paged_attention.argtypes = [pc, i32, vp, i32, vp, i32, i32, vp, i64, vp, i32, i32,
+                                             i32, i32, vp, vp, i32, vp, sz, vp]
         L.marche_status_string.argtypes = [C.c_int]
         L.marche_status_string.restype = C.c_char_p
         L.marche_last_error.argtypes = []
@@ -127,7 +150,9 @@ def lib() -> C.CDLL:
                      "select_refresh_ordered",
                      "marche_decoder_input", "marche_attention_segments",
                      "marche_encoder_input", "marche_encoder_to_decoder",
-                     "marche_diffusion_sample", "marche_profile_enable", "marche_profile_entry"):
+                     "marche_diffusion_sample", "marche_paged_cache_init", "marche_paged_write",
+                     "marche_paged_read", "marche_paged_bounds", "marche_paged_select",
+                     "marche_paged_attention", "marche_profile_enable", "marche_profile_entry"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -305,6 +330,77 @@ def diffusion_sample(head: Head, weights: HeadWeights, x_dec, n_tokens: int, n_b
                                          _ptr(pe_diff), _ptr(rows), _ptr(out_rows), n_rows,
                                          _ptr(noise), n_steps, temperature, _ptr(tok_out),
                                          _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def paged_cache(n_layers: int, n_pages: int, n_heads: int, page_size: int, head_dim: int, fmt: int,
+                k, v, k_exp=None, v_exp=None, bounds=None, bounds_exp=None) -> PagedCache:
+    """Handle of a paged cache over the caller's buffers (kept alive by it)."""
+    cache = PagedCache(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), _ptr(bounds), _ptr(bounds_exp),
+                       n_layers, n_pages, n_heads, page_size, head_dim, fmt)
+    cache._owners = (k, v, k_exp, v_exp, bounds, bounds_exp)
+    return cache
+
+
+def paged_cache_bytes(n_layers: int, n_pages: int, n_heads: int, page_size: int, head_dim: int,
+                      fmt: int, with_bounds: bool) -> int:
+    return lib().marche_paged_cache_bytes(n_layers, n_pages, n_heads, page_size, head_dim, fmt,
+                                          1 if with_bounds else 0)
+
+
+def paged_cache_init(n_layers: int, n_pages: int, n_heads: int, page_size: int, head_dim: int,
+                     fmt: int, with_bounds: bool, buffer, nbytes: int) -> PagedCache:
+    cache = PagedCache()
+    _check(lib().marche_paged_cache_init(C.byref(cache), n_layers, n_pages, n_heads, page_size,
+                                         head_dim, fmt, 1 if with_bounds else 0, _ptr(buffer),
+                                         nbytes))
+    cache._owners = (buffer,)
+    return cache
+
+
+def paged_write(cache: PagedCache, layer: int, page_table, max_pages: int, n_seqs: int, a_idx,
+                a_off, a_total: int, k_new, v_new, row_stride: int, dtype: int,
+                stream=None) -> None:
+    _check(lib().marche_paged_write(C.byref(cache), layer, _ptr(page_table), max_pages, n_seqs,
+                                    _ptr(a_idx), _ptr(a_off), a_total, _ptr(k_new), _ptr(v_new),
+                                    row_stride, dtype, _stream(stream)))
+
+
+def paged_read(cache: PagedCache, layer: int, page_table, max_pages: int, lens, n_seqs: int,
+               n_tokens: int, k_out, v_out, dtype: int, stream=None) -> None:
+    _check(lib().marche_paged_read(C.byref(cache), layer, _ptr(page_table), max_pages, _ptr(lens),
+                                   n_seqs, n_tokens, _ptr(k_out), _ptr(v_out), dtype,
+                                   _stream(stream)))
+
+
+def paged_bounds(cache: PagedCache, layer: int, page_table, max_pages: int, lens, first, span: int,
+                 n_seqs: int, stream=None) -> None:
+    _check(lib().marche_paged_bounds(C.byref(cache), layer, _ptr(page_table), max_pages, _ptr(lens),
+                                     _ptr(first), span, n_seqs, _stream(stream)))
+
+
+def paged_select(cache: PagedCache, layer: int, page_table, max_pages: int, lens, n_seqs: int, q,
+                 q_stride: int, q_off, q_total: int, n_q_heads: int, dtype: int, n_select: int,
+                 pages, stream=None) -> None:
+    _check(lib().marche_paged_select(C.byref(cache), layer, _ptr(page_table), max_pages, _ptr(lens),
+                                     n_seqs, _ptr(q), q_stride, _ptr(q_off), q_total, n_q_heads,
+                                     dtype, n_select, _ptr(pages), _stream(stream)))
+
+
+def paged_attention_workspace_bytes(cache: PagedCache, n_seqs: int, q_total: int, q_max: int,
+                                    n_q_heads: int, len_max: int, n_select: int = 0) -> int:
+    return lib().marche_paged_attention_workspace_bytes(C.byref(cache), n_seqs, q_total, q_max,
+                                                        n_q_heads, len_max, n_select)
+
+
+def paged_attention(cache: PagedCache, layer: int, page_table, max_pages: int, lens, len_max: int,
+                    n_seqs: int, q, q_stride: int, q_off, q_total: int, q_max: int, n_q_heads: int,
+                    dtype: int, o, pages=None, n_select: int = 0, workspace=None,
+                    workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().marche_paged_attention(C.byref(cache), layer, _ptr(page_table), max_pages,
+                                        _ptr(lens), len_max, n_seqs, _ptr(q), q_stride,
+                                        _ptr(q_off), q_total, q_max, n_q_heads, dtype, _ptr(o),
+                                        _ptr(pages), n_select, _ptr(workspace), workspace_bytes,
+                                        _stream(stream)))
 
 
 def profile_enable(on: bool) -> None:

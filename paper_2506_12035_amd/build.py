@@ -20,7 +20,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmarche.so")
 SOURCES = ("marche_api.cpp", "marche_noalloc.hip", "k_elementwise.hip", "k_gemm.hip",
-           "k_attn.hip", "k_select.hip", "k_mar.hip")
+           "k_attn.hip", "k_select.hip", "k_mar.hip", "k_paged.hip", "k_paged_attn_bf16.hip",
+           "k_paged_attn_e4m3.hip", "k_paged_attn_int8.hip")
 ARCH = "gfx950"
 
 # -packed-fp32-ops: keep the compiler from forming packed fp32 VALU ops.
@@ -41,7 +42,9 @@ def hipcc() -> str:
 # to and from the VGPRs for every softmax step on them, so their MFMAs take
 # and produce VGPRs.  The GEMM tiles keep the compiler's choice (256
 # accumulators per lane live in the AGPRs).
-EXTRA = {"k_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+         for src in ("k_attn.hip", "k_paged_attn_bf16.hip", "k_paged_attn_e4m3.hip",
+                     "k_paged_attn_int8.hip")}
 
 
 def _compile(src: str) -> str:

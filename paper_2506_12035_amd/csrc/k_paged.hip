@@ -1,0 +1,583 @@
+// Paged key/value cache: quantising rows as they are written, reading tokens
+// back, key bounds of pages, page selection and attention over the cache.
+//
+// A pool holds pages [n_pages][H][page][dh] for K and for V; a page belongs to
+// one head's `page` consecutive tokens of one sequence.  8-bit formats carry
+// one exponent byte per (page, head, token) and value = q * 2^(code - 127).
+// With powers of two, quantising (a product by 2^-e and one rounding to the
+// format) and reading back (q * 2^e, exact in bf16: both formats have at most
+// 8 significant bits) give the same bits whatever the order of operations, and
+// the page scores below are whole numbers times powers of two.
+//
+// Page ids and lengths come from device memory.  Every kernel checks a page id
+// against the pool before it forms an address from it and clamps lengths to
+// the page table, so that no list reaches outside the pool; a page id outside
+// the pool reads as "no tokens there" and a write to it is dropped.
+#include <algorithm>
+#include <type_traits>
+
+#include "paged_device.h"
+
+namespace marche {
+
+// ------------------------------------------------------------------ write
+
+// One (row, head) of new keys and values per GROUP lanes, 8 elements of each
+// per lane: the row's largest magnitude by a DPP reduction, its exponent, one
+// rounding, one 8-byte (16 for bf16) store.  Bound by bytes: each new row is read once and its
+// slot written once.
+template <int FMT, int DH, typename InT>
+__global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
+  constexpr int GROUP = DH == 64 ? 8 : 16, PER = 256 / GROUP;
+  __shared__ int s_b0;
+  const int tid = threadIdx.x, lane = tid & 63, c = tid % GROUP;
+  const uint32_t u0 = blockIdx.x * PER, unit = u0 + tid / GROUP;  // below 2^31
+  const int r = unit / (uint32_t)a.n_heads, h = unit - (uint32_t)r * a.n_heads;
+  const bool on = r < a.a_total && c < DH / 8;
+
+  // the row's values, in flight while its sequence is found
+  float kx[8], vx[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) kx[i] = vx[i] = 0.f;
+  if (on) {
+    const size_t at = (size_t)r * a.row_stride + (size_t)h * DH + 8 * c;
+    const InT *kp = static_cast<const InT *>(a.k_new) + at, *vp = static_cast<const InT *>(a.v_new) + at;
+    load8(kp, kx);
+    load8(vp, vx);
+  }
+  const int tok = on ? a.a_idx[r] : -1;
+  int b;
+  if (a.a_off) {
+    if (tid < 64) {
+      const int f = wave_find_seq(a.a_off, a.n_seqs, min((int)(u0 / (uint32_t)a.n_heads), a.a_total - 1), lane);
+      if (tid == 0) s_b0 = f;
+    }
+    __syncthreads();
+    b = s_b0;
+    while (b < a.n_seqs && a.a_off[b + 1] <= r) ++b;
+    if (b < a.n_seqs && r < a.a_off[b]) b = a.n_seqs;  // before the first sequence
+  } else {
+    b = r / a.rows_each;
+  }
+  float km = 0.f, vm = 0.f;
+  if constexpr (FMT != BF) {
+    // magnitudes as bits, which order like them and place NaN above infinity
+    uint32_t ku = 0, vu = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      ku = max(ku, __float_as_uint(kx[i]) & 0x7FFFFFFFu);
+      vu = max(vu, __float_as_uint(vx[i]) & 0x7FFFFFFFu);
+    }
+#pragma unroll
+    for (int o = GROUP / 2; o > 0; o >>= 1) {
+      ku = max(ku, (uint32_t)__shfl_xor((int)ku, o, 64));
+      vu = max(vu, (uint32_t)__shfl_xor((int)vu, o, 64));
+    }
+    km = __uint_as_float(ku);
+    vm = __uint_as_float(vu);
+  }
+  if (!on || b >= a.n_seqs || tok < 0 || (tok >> a.page_log2) >= a.max_pages) return;
+  const int page = a.table[(size_t)b * a.max_pages + (tok >> a.page_log2)];
+  if ((unsigned)page >= (unsigned)a.n_pages) return;
+  const size_t slot = (((size_t)page * a.n_heads + h) << a.page_log2) + (tok & ((1 << a.page_log2) - 1));
+  const size_t at = slot * DH + 8 * c;
+  if constexpr (FMT == BF) {
+    bf16x8 ko, vo;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ko[i] = (bf16)kx[i], vo[i] = (bf16)vx[i];
+    *reinterpret_cast<bf16x8 *>(static_cast<bf16 *>(a.k) + at) = ko;
+    *reinterpret_cast<bf16x8 *>(static_cast<bf16 *>(a.v) + at) = vo;
+  } else {
+    auto pack = [](const float (&x)[8], int code) {
+      u32x2 o;
+      if (code == 255) {  // the whole row reads back as NaN
+        o.x = o.y = FMT == E4 ? 0x7F7F7F7Fu : 0u;
+        return o;
+      }
+      const float inv = exp_inv(code);
+      if constexpr (FMT == E4) {
+        int w0 = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
+        w0 = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, w0, true);
+        int w1 = __builtin_amdgcn_cvt_pk_fp8_f32(x[4] * inv, x[5] * inv, 0, false);
+        w1 = __builtin_amdgcn_cvt_pk_fp8_f32(x[6] * inv, x[7] * inv, w1, true);
+        o.x = (uint32_t)w0;
+        o.y = (uint32_t)w1;
+      } else {
+        uint32_t w[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          w[i / 4] |= ((uint32_t)(int)rintf(x[i] * inv) & 0xFFu) << (8 * (i % 4));
+        o.x = w[0];
+        o.y = w[1];
+      }
+      return o;
+    };
+    const int kc = exp_code<FMT>(km), vc = exp_code<FMT>(vm);
+    *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.k) + at) = pack(kx, kc);
+    *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.v) + at) = pack(vx, vc);
+    if (c == 0) {
+      a.k_exp[slot] = (uint8_t)kc;
+      a.v_exp[slot] = (uint8_t)vc;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ read
+
+// TB tokens of one (sequence, head) of K and of V per workgroup.  Within a
+// page the tokens of a head lie one after another on both sides, so a thread
+// takes 16 consecutive elements whatever the head width.  Bound by bytes.
+template <int FMT, int DH, typename OutT>
+__global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
+  constexpr int CH = DH / 16;
+  const int blk = blockIdx.x % a.blocks, bh = blockIdx.x / a.blocks;
+  const int b = bh / a.n_heads, h = bh - b * a.n_heads;
+  const int len = min(paged_len(a.lens[b], a.max_pages, a.page_log2), a.n_tokens);
+  const int t0 = blk * PAGED_READ_TOKENS;
+  if (t0 >= len) return;
+  const int n = min(len - t0, PAGED_READ_TOKENS) * CH;
+  for (int x = threadIdx.x; x < n; x += 256) {
+    const int t = t0 + x / CH, d = (x % CH) * 16;
+    const int page = a.table[(size_t)b * a.max_pages + (t >> a.page_log2)];
+    if ((unsigned)page >= (unsigned)a.n_pages) continue;
+    const size_t slot = (((size_t)page * a.n_heads + h) << a.page_log2) + (t & ((1 << a.page_log2) - 1));
+    const size_t from = slot * DH + d, to = ((size_t)bh * a.n_tokens + t) * DH + d;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const void *src = w ? a.v : a.k;
+      OutT *o = static_cast<OutT *>(w ? a.v_out : a.k_out) + to;
+      float f[16];
+      if constexpr (FMT == BF) {
+        const bf16x8 *p = reinterpret_cast<const bf16x8 *>(static_cast<const bf16 *>(src) + from);
+        if constexpr (sizeof(OutT) == 2) {
+          reinterpret_cast<bf16x8 *>(o)[0] = p[0];
+          reinterpret_cast<bf16x8 *>(o)[1] = p[1];
+          continue;
+        }
+        const bf16x8 x0 = p[0], x1 = p[1];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (float)x0[i], f[8 + i] = (float)x1[i];
+      } else {
+        const u32x4 q = *reinterpret_cast<const u32x4 *>(static_cast<const uint8_t *>(src) + from);
+        const float s = exp_scale((w ? a.v_exp : a.k_exp)[slot]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpack4<FMT>(q[i], s, f + 4 * i);
+      }
+      if constexpr (sizeof(OutT) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          reinterpret_cast<float4 *>(o)[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+      } else {
+        bf16x8 y0, y1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y0[i] = (bf16)f[i], y1[i] = (bf16)f[8 + i];
+        reinterpret_cast<bf16x8 *>(o)[0] = y0;
+        reinterpret_cast<bf16x8 *>(o)[1] = y1;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ bounds
+
+// One wavefront per (sequence, page, head): lanes hold four channels, LPT lanes
+// a token and TPW tokens a load, each lane the largest and smallest of its
+// channels over its tokens; the TPW parts are joined by lane exchanges at the
+// end.  Bound by bytes: every key once, 2 dh + 1 bytes out per page.
+template <int FMT, int DH>
+__global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
+  constexpr int LPT = DH / 4, TPW = 64 / LPT;
+  const int lane = threadIdx.x & 63;
+  const uint32_t unit = blockIdx.x * 4 + (threadIdx.x >> 6);  // below 2^31
+  const uint32_t bp = unit / (uint32_t)a.n_heads;
+  const int h = unit - bp * a.n_heads, b = bp / (uint32_t)a.span;
+  if (b >= a.n_seqs) return;
+  const int len = paged_len(a.lens[b], a.max_pages, a.page_log2);
+  const int first = a.first ? max(a.first[b], 0) : 0;
+  const int p = (first >> a.page_log2) + (int)(bp - (uint32_t)b * a.span);
+  if (p >= a.max_pages || ((int64_t)p << a.page_log2) >= len) return;
+  const int page = a.table[(size_t)b * a.max_pages + p];
+  if ((unsigned)page >= (unsigned)a.n_pages) return;
+  const int n = min(len - (p << a.page_log2), 1 << a.page_log2);
+  const size_t slot0 = ((size_t)page * a.n_heads + h) << a.page_log2;
+  const int t_in = lane / LPT, l = lane - t_in * LPT;
+  float hi[4], lo[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) hi[i] = -INFINITY, lo[i] = INFINITY;
+  bool bad = false;
+  if (t_in < TPW) {
+    const size_t es = FMT == BF ? 2 : 1;
+    const char *src = static_cast<const char *>(a.k) + (slot0 * DH + 4 * l) * es;
+#pragma unroll 4
+    for (int t = t_in; t < n; t += TPW) {
+      float f[4];
+      if constexpr (FMT == BF) {
+        const bf16x4 q = *reinterpret_cast<const bf16x4 *>(src + (size_t)t * DH * 2);
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = (float)q[i], z = fmaf(f[i], 0.f, z);
+        bad |= z != 0.f;  // NaN: some value was not finite
+      } else {
+        const uint32_t code = a.k_exp[slot0 + t];
+        unpack4<FMT>(*reinterpret_cast<const uint32_t *>(src + (size_t)t * DH), exp_scale(code), f);
+        bad |= code == 255;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) hi[i] = fmaxf(hi[i], f[i]), lo[i] = fminf(lo[i], f[i]);
+    }
+  }
+  // join the tokens' parts into the first LPT lanes, then the largest magnitude
+  float amax = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float h0 = hi[i], l0 = lo[i];
+#pragma unroll
+    for (int k = 1; k < TPW; ++k) {
+      hi[i] = fmaxf(hi[i], __shfl(h0, min(lane + k * LPT, 63), 64));
+      lo[i] = fminf(lo[i], __shfl(l0, min(lane + k * LPT, 63), 64));
+    }
+    amax = fmaxf(amax, fmaxf(fabsf(hi[i]), fabsf(lo[i])));
+  }
+  bad = __ballot(bad) != 0;
+  amax = wave_max(lane < LPT ? amax : 0.f);
+  const int code = bad ? 255 : exp_code<I8>(amax);
+  const size_t out = (size_t)page * a.n_heads + h;
+  if (lane < LPT) {
+    uint32_t wh = 0, wl = 0;
+    if (code != 255) {
+      const float inv = exp_inv(code);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        wh |= ((uint32_t)(int)rintf(hi[i] * inv) & 0xFFu) << (8 * i);
+        wl |= ((uint32_t)(int)rintf(lo[i] * inv) & 0xFFu) << (8 * i);
+      }
+    }
+    uint32_t *o = reinterpret_cast<uint32_t *>(a.bounds + out * 2 * DH);
+    o[l] = wh;
+    o[DH / 4 + l] = wl;
+  }
+  if (lane == 0) a.bounds_exp[out] = (uint8_t)code;
+}
+
+// ------------------------------------------------------------------ select
+
+// Order-preserving image of a score: larger score, larger value; NaN with
+// -inf, below every number; -0 ties with +0; never 0.
+__device__ __forceinline__ uint32_t score_key(float f) {
+  if (f != f) f = -INFINITY;
+  if (f == 0.0f) f = 0.0f;
+  const uint32_t u = __float_as_uint(f);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// Page selection.  One workgroup per (16-column tile of packed rows, key head): the
+// columns are query heads of `rows_per` consecutive rows.  Each row's queries
+// are quantised to int8 with an exponent of their own, split by sign, and
+//   score = sum_d (q_d > 0 ? q_d hi_d : q_d lo_d) = [q+ ; q-] . [hi ; lo]
+// is an int8 product on the matrix cores (16 pages x 16 columns x 64 deep per
+// instruction) against the bounds as they lie in memory: whole numbers below
+// 2^24, so the sum is exact in any order and scaling it by the two powers of
+// two is too.  The largest over a row's heads is taken in LDS.  Then one
+// wavefront per row finds the k-th largest key by its bits, from the top, and
+// compacts the pages above it (and the first of those equal to it) in
+// ascending order.
+template <int DH, typename InT, int KPL>
+__global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
+  constexpr int ST = (2 * DH + 63) / 64;
+  extern __shared__ uint32_t s_key[];  // [rows_per][p_cap]
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
+  const int c = lane & 15, g = lane >> 4;
+  const int h = blockIdx.x % a.n_heads;
+  const int r0 = (blockIdx.x / a.n_heads) * a.rows_per;
+
+  for (int x = tid; x < a.rows_per * a.p_cap; x += blockDim.x) s_key[x] = 0u;
+  // the rows of the tile may belong to different sequences
+  __shared__ int s_len[16], s_seq[16];
+  if (wave == 0) {
+    int b = a.q_off ? wave_find_seq(a.q_off, a.n_seqs, min(r0, a.q_total - 1), lane) : 0;
+    if (lane < a.rows_per) {
+      const int r = r0 + lane;
+      if (!a.q_off) b = r / a.rows_each;
+      else while (b < a.n_seqs && a.q_off[b + 1] <= r) ++b;
+      if (r >= a.q_total || (a.q_off && b < a.n_seqs && r < a.q_off[b])) b = a.n_seqs;
+      s_seq[lane] = b;
+      s_len[lane] = b < a.n_seqs ? paged_len(a.lens[b], a.max_pages, a.page_log2) : 0;
+    }
+  }
+  __syncthreads();
+
+  // a tile whose rows share a sequence is scored at once; else row by row
+  int lo = 0;
+  while (lo < a.rows_per) {
+    int end = lo + 1;
+    while (end < a.rows_per && s_seq[end] == s_seq[lo]) ++end;
+    const int b = s_seq[lo], n_p = (s_len[lo] + (1 << a.page_log2) - 1) >> a.page_log2;
+    if (b < a.n_seqs && n_p > a.n_select) {
+      const int cols = (end - lo) * a.group;
+      for (int col0 = 0; col0 < cols; col0 += 16) {
+        const int col = col0 + c;
+        const bool on = col < cols;
+        const int i = lo + (on ? col / a.group : 0), hg = on ? col % a.group : 0;
+        const InT *qp = static_cast<const InT *>(a.q) + (size_t)(r0 + i) * a.q_stride +
+                        (size_t)(h * a.group + hg) * DH;
+        // this lane's 16-element groups of [q+ ; q-]
+        float x[ST][16];
+        uint32_t am = 0;
+#pragma unroll
+        for (int s = 0; s < ST; ++s) {
+          const int k0 = 64 * s + 16 * g;
+          const bool in = on && k0 < 2 * DH;
+          const InT *p = qp + (k0 < DH ? k0 : k0 - DH);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[s][e] = 0.f;
+          if (in) {
+            load8(p, x[s]);
+            load8(p + 8, x[s] + 8);
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) am = max(am, __float_as_uint(x[s][e]) & 0x7FFFFFFFu);
+        }
+        am = max(am, (uint32_t)__shfl_xor((int)am, 16, 64));
+        am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
+        const int qc = exp_code<I8>(__uint_as_float(am));
+        const float inv = qc == 255 ? 0.f : exp_inv(qc), qs = exp_scale(qc);
+        i32x4 qf[ST];
+#pragma unroll
+        for (int s = 0; s < ST; ++s) {
+          const bool neg = 64 * s + 16 * g >= DH;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t v = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int q = qc == 255 ? 0 : (int)rintf(x[s][4 * w + e] * inv);
+              v |= ((uint32_t)(neg ? min(q, 0) : max(q, 0)) & 0xFFu) << (8 * e);
+            }
+            qf[s][w] = (int)v;
+          }
+        }
+        for (int p0 = 16 * wave; p0 < n_p; p0 += 16 * waves) {
+          const int pc = min(p0 + c, n_p - 1);
+          const int page = a.table[(size_t)b * a.max_pages + pc];
+          const bool ok = (unsigned)page < (unsigned)a.n_pages;
+          const size_t at = ((size_t)(ok ? page : 0) * a.n_heads + h);
+          const float be = exp_scale(a.bounds_exp[at]);
+          i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+          for (int s = 0; s < ST; ++s) {
+            i32x4 bf = {0, 0, 0, 0};
+            if (64 * s + 16 * g < 2 * DH)
+              bf = *reinterpret_cast<const i32x4 *>(a.bounds + at * 2 * DH + 64 * s + 16 * g);
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf, qf[s], acc, 0, 0, 0);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            // lane's page 4 g + j: its exponent sits in lane 4 g + j
+            const float bs = __shfl(be, 4 * g + j, 64);
+            const bool there = __shfl((int)ok, 4 * g + j, 64) != 0;
+            const int p = p0 + 4 * g + j;
+            if (on && p < n_p) {
+              // (exponent code 255: a bound that is not finite, whatever its bytes)
+              const uint32_t key = there ? score_key(bs < INFINITY ? (float)acc[j] * bs * qs : NAN) : 1u;
+              if (a.group == 1) s_key[i * a.p_cap + p] = key;
+              else atomicMax(&s_key[i * a.p_cap + p], key);
+            }
+          }
+        }
+      }
+    }
+    lo = end;
+  }
+  __syncthreads();
+
+  for (int i = wave; i < a.rows_per; i += waves) {
+    const int r = r0 + i;
+    if (r >= a.q_total || s_seq[i] >= a.n_seqs) continue;
+    int32_t *out = a.pages + ((size_t)r * a.n_heads + h) * a.n_select;
+    const int n_p = (s_len[i] + (1 << a.page_log2) - 1) >> a.page_log2;
+    if (n_p <= a.n_select) {  // every page, without a score
+      for (int j = lane; j < a.n_select; j += 64) out[j] = j < n_p ? j : -1;
+      continue;
+    }
+    uint32_t kr[KPL];
+#pragma unroll
+    for (int j = 0; j < KPL; ++j) kr[j] = 64 * j + lane < n_p ? s_key[i * a.p_cap + 64 * j + lane] : 0u;
+    auto count_ge = [&](uint32_t v) {
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < KPL; ++j) n += __popcll(__ballot(kr[j] >= v));
+      return n;
+    };
+    uint32_t t = 0;  // the n_select-th largest key
+    for (int bit = 31; bit >= 0; --bit)
+      if (count_ge(t | (1u << bit)) >= a.n_select) t |= 1u << bit;
+    const int ties = a.n_select - (t == 0xFFFFFFFFu ? 0 : count_ge(t + 1u));
+    int base = 0, tie_base = 0;
+    const unsigned long long below = (1ull << lane) - 1ull;
+#pragma unroll
+    for (int j = 0; j < KPL; ++j) {
+      const unsigned long long tie = __ballot(kr[j] != 0u && kr[j] == t);
+      const bool take = kr[j] != 0u && (kr[j] > t || (kr[j] == t && tie_base + __popcll(tie & below) < ties));
+      const unsigned long long sel = __ballot(take);
+      if (take) out[base + __popcll(sel & below)] = 64 * j + lane;
+      base += __popcll(sel);
+      tie_base += __popcll(tie);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ join
+
+// Joins the key ranges' parts: part s of a row counts exp2(m_s - m) of it.
+// One thread per (row, head, 4 channels).
+template <int DH, typename RowT>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
+  constexpr int C4 = DH / 4;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t n = (int64_t)a.q_total * a.n_heads * a.group;
+  const int64_t row = x / C4;
+  if (row >= n) return;
+  const int d = (int)(x - row * C4) * 4;
+  // rows behind the last sequence (or before the first) belong to nobody
+  const int r = (int)(row / (a.n_heads * a.group));
+  if (a.q_off && (r < a.q_off[0] || r >= a.q_off[a.n_seqs])) return;
+  float m = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * n + row)]);
+  float l = 0.f;
+  bool any = false;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.splits; ++s) {
+    const float ms = a.part_ml[2 * (s * n + row)], ls = a.part_ml[2 * (s * n + row) + 1];
+    if (ls == -1.f) continue;
+    any = true;
+    const float w = ms == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(ms - m);
+    l += ls * w;
+    sum += *reinterpret_cast<const f32x4 *>(a.part_o + (s * n + row) * DH + d) * w;
+  }
+  const float inv = any ? 1.f / l : 0.f;
+  RowT *out = static_cast<RowT *>(a.o) + row * DH + d;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[e] = (RowT)(any ? sum[e] * inv : 0.f);
+}
+
+// ------------------------------------------------------------------ launches
+
+// f(std::integral_constant<int, FMT>, std::integral_constant<int, DH>)
+template <typename F>
+static hipError_t by_shape(int32_t format, int32_t head_dim, F f) {
+  auto dh = [&](auto fmt) {
+    switch (head_dim) {
+      case 64: f(fmt, std::integral_constant<int, 64>()); break;
+      case 80: f(fmt, std::integral_constant<int, 80>()); break;
+      case 128: f(fmt, std::integral_constant<int, 128>()); break;
+      default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+  };
+  switch (format) {
+    case BF: return dh(std::integral_constant<int, BF>());
+    case E4: return dh(std::integral_constant<int, E4>());
+    case I8: return dh(std::integral_constant<int, I8>());
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_paged_write(DType dt, int32_t format, int32_t head_dim, const PagedWriteArgs &a,
+                              hipStream_t s) {
+  if (a.a_total == 0) return hipSuccess;
+  const int per = 256 / (head_dim == 64 ? 8 : 16);
+  const unsigned grid = (unsigned)(((int64_t)a.a_total * a.n_heads + per - 1) / per);
+  return by_shape(format, head_dim, [&](auto fmt, auto dh) {
+    if (dt == DType::BF16) launch_kernel(paged_write_kernel<fmt.value, dh.value, bf16>, grid, 256, 0, s, a);
+    else launch_kernel(paged_write_kernel<fmt.value, dh.value, float>, grid, 256, 0, s, a);
+  });
+}
+
+hipError_t launch_paged_read(DType dt, int32_t format, int32_t head_dim, PagedReadArgs a,
+                             hipStream_t s) {
+  if (a.n_seqs == 0 || a.n_tokens == 0) return hipSuccess;
+  a.blocks = (a.n_tokens + PAGED_READ_TOKENS - 1) / PAGED_READ_TOKENS;
+  const unsigned grid = (unsigned)((int64_t)a.n_seqs * a.n_heads * a.blocks);
+  return by_shape(format, head_dim, [&](auto fmt, auto dh) {
+    if (dt == DType::BF16) launch_kernel(paged_read_kernel<fmt.value, dh.value, bf16>, grid, 256, 0, s, a);
+    else launch_kernel(paged_read_kernel<fmt.value, dh.value, float>, grid, 256, 0, s, a);
+  });
+}
+
+hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, const PagedBoundsArgs &a,
+                               hipStream_t s) {
+  if (a.n_seqs == 0 || a.span == 0) return hipSuccess;
+  const unsigned grid = (unsigned)(((int64_t)a.n_seqs * a.n_heads * a.span + 3) / 4);
+  return by_shape(format, head_dim, [&](auto fmt, auto dh) {
+    launch_kernel(paged_bounds_kernel<fmt.value, dh.value>, grid, 256, 0, s, a);
+  });
+}
+
+hipError_t launch_paged_select(DType dt, int32_t head_dim, PagedSelectArgs a, hipStream_t s) {
+  if (a.q_total == 0) return hipSuccess;
+  a.p_cap = (a.max_pages + 63) / 64 * 64;
+  // rows that fill the 16 columns, as far as their keys fit 32 KB of LDS
+  a.rows_per = std::max(1, std::min({16 / a.group, 8192 / a.p_cap, a.q_total}));
+  const unsigned grid = (unsigned)(((int64_t)a.q_total + a.rows_per - 1) / a.rows_per * a.n_heads);
+  // a wavefront per 16 pages, or per row where that is more
+  const int waves = std::min(16, std::max((a.max_pages + 15) / 16, a.rows_per));
+  const uint32_t lds = (uint32_t)a.rows_per * a.p_cap * 4;
+  return by_shape(BF, head_dim, [&](auto, auto dh) {
+    auto go = [&](auto kpl) {
+      constexpr int K = kpl.value;
+      if (dt == DType::BF16) launch_kernel(paged_select_kernel<dh.value, bf16, K>, grid, 64 * waves, lds, s, a);
+      else launch_kernel(paged_select_kernel<dh.value, float, K>, grid, 64 * waves, lds, s, a);
+    };
+    // keys per lane of a row's wavefront: the fewest that hold max_pages
+    const int kpl = a.p_cap / 64;
+    if (kpl <= 1) go(std::integral_constant<int, 1>());
+    else if (kpl <= 4) go(std::integral_constant<int, 4>());
+    else if (kpl <= 16) go(std::integral_constant<int, 16>());
+    else go(std::integral_constant<int, 64>());
+  });
+}
+
+void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
+  const int rows = a.q_max * a.group;  // packed rows of a sequence and key head
+  a.row_tiles = rows <= 16 ? 1 : rows <= 32 || dt == DType::F32 ? 2 : 4;
+  a.row_blocks = (rows + 16 * a.row_tiles - 1) / (16 * a.row_tiles);
+  const int block_rows = std::min(a.q_max, (16 * a.row_tiles + a.group - 2) / a.group + 1);
+  a.bit_rows = block_rows;
+  int64_t keys = a.len_max;
+  if (a.n_select > 0)
+    keys = std::min<int64_t>((int64_t)((a.len_max + (1 << a.page_log2) - 1) >> a.page_log2),
+                             (int64_t)a.n_select * block_rows)
+           << a.page_log2;
+  const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32);
+  const int64_t units = std::max<int64_t>(1, (int64_t)a.n_seqs * a.n_heads * a.row_blocks);
+  // wavefronts per unit: enough of them for the chip, two tiles each at least
+  const int64_t want = std::min<int64_t>((4096 + units - 1) / units, (tiles + 1) / 2);
+  const int most = a.row_tiles == 1 ? 8 : 4;
+  a.waves = 1;
+  while (a.waves < most && a.waves < want) a.waves *= 2;
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(64, want / a.waves));
+  a.chunk = (int32_t)((tiles + splits - 1) / splits);
+  a.chunk = (a.chunk + a.waves - 1) / a.waves * a.waves;
+  a.splits = (int32_t)((tiles + a.chunk - 1) / a.chunk);
+}
+
+hipError_t launch_paged_attention(DType dt, int32_t format, int32_t head_dim, const PagedAttnArgs &a,
+                                  hipStream_t s) {
+  switch (format) {
+    case BF: return launch_paged_attention_bf16(dt, head_dim, a, s);
+    case E4: return launch_paged_attention_e4m3(dt, head_dim, a, s);
+    case I8: return launch_paged_attention_int8(dt, head_dim, a, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_paged_join(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s) {
+  const int64_t n = (int64_t)a.q_total * a.n_heads * a.group * (head_dim / 4);
+  const unsigned grid = (unsigned)((n + 255) / 256);
+  return by_shape(BF, head_dim, [&](auto, auto dh) {
+    if (dt == DType::BF16) launch_kernel(paged_join_kernel<dh.value, bf16>, grid, 256, 0, s, a);
+    else launch_kernel(paged_join_kernel<dh.value, float>, grid, 256, 0, s, a);
+  });
+}
+
+}  // namespace marche

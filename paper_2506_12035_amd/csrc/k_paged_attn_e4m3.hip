@@ -1,0 +1,10 @@
+// Attention over a paged cache of e4m3 (kernel in paged_attn.h).
+#include "paged_attn.h"
+
+namespace marche {
+
+hipError_t launch_paged_attention_e4m3(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s) {
+  return launch_paged_fmt<E4>(dt, head_dim, a, s);
+}
+
+}  // namespace marche

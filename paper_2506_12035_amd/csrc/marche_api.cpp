@@ -112,7 +112,8 @@ enum KClass {
   K_ROW_MAP, K_GATHER_LN, K_ATTN_W1, K_ATTN_W2, K_ATTN_W4, K_ATTN_SCORES, K_SELECT, K_DECODER_INPUT,
   K_FILL, K_ATTN2_W1, K_ATTN2_W2, K_ATTN2_W4, K_CONCAT, K_ATTN_RES, K_ENC_INPUT, K_MASK_FILL,
   K_LN_ROWS, K_TIME_SINUS, K_HEAD_SILU_COND, K_HEAD_MOD, K_HEAD_STEP, K_TRANSPOSE, K_ATTN_RES_SC,
-  K_ATTN_W8, K_ATTN_SC,
+  K_ATTN_W8, K_ATTN_SC, K_PAGED_WRITE, K_PAGED_READ, K_PAGED_BOUNDS, K_PAGED_SELECT, K_PAGED_ATTN,
+  K_PAGED_JOIN,
   K_GEMM_FIRST  // then, per projection, one class per tile and the few-row kernel
 };
 const char *const kClassNames[K_GEMM_FIRST] = {
@@ -120,7 +121,9 @@ const char *const kClassNames[K_GEMM_FIRST] = {
     "attn_scores",    "select_topk",    "decoder_input",  "fill_zero",           "attention2_q32",
     "attention2_q64", "attention2_q128", "concat_kv",     "attention_res",       "encoder_input",
     "mask_fill",      "ln_rows",        "time_sinus",     "head_silu_cond",      "head_mod",
-    "head_step",      "transpose",      "attention_res_scores", "attention_q256", "attention_scores"};
+    "head_step",      "transpose",      "attention_res_scores", "attention_q256", "attention_scores",
+    "paged_write",    "paged_read",     "paged_bounds",   "paged_select",        "paged_attention",
+    "paged_join"};
 static_assert(sizeof(kClassNames) / sizeof(kClassNames[0]) == K_GEMM_FIRST, "one name per class");
 
 enum GemmProj { P_QKV, P_O, P_FC1, P_FC2, P_EMBED, P_HEAD, P_HEAD_SILU, P_COUNT };
@@ -1009,6 +1012,510 @@ marche_status_t marche_diffusion_sample(const marche_head_t *hd, const marche_he
            launch_head_step(dt, hr, W, stream));
     hr.x_cur = xs;
   }
+  return MARCHE_OK;
+}
+
+// ------------------------------------------------------------------ paged cache
+
+namespace {
+
+bool paged_shape(int32_t n_layers, int32_t n_pages, int32_t n_heads, int32_t page_size,
+                 int32_t head_dim, int32_t format, marche_status_t *st) {
+  auto bad = [&](marche_status_t s, const char *what, int32_t v) {
+    *st = fail(s, "cache.%s=%d is not supported", what, v);
+    return false;
+  };
+  if (n_layers < 1) return bad(MARCHE_ERR_INVALID_ARG, "n_layers", n_layers);
+  if (n_pages < 1) return bad(MARCHE_ERR_INVALID_ARG, "n_pages", n_pages);
+  if (n_heads < 1 || n_heads > 65535) return bad(MARCHE_ERR_INVALID_ARG, "n_heads", n_heads);
+  if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1)))
+    return bad(MARCHE_ERR_UNSUPPORTED, "page_size", page_size);
+  if (head_dim != 64 && head_dim != 80 && head_dim != 128)
+    return bad(MARCHE_ERR_UNSUPPORTED, "head_dim", head_dim);
+  if (format != MARCHE_CACHE_BF16 && format != MARCHE_CACHE_E4M3 && format != MARCHE_CACHE_INT8)
+    return bad(MARCHE_ERR_UNSUPPORTED, "format", format);
+  return true;
+}
+
+// A layer of the cache and what the calls derive from it.
+struct PagedLayer {
+  char *k, *v;
+  uint8_t *k_exp, *v_exp;
+  int8_t *bounds;
+  uint8_t *bounds_exp;
+  int32_t page_log2;
+  size_t row_bytes;  // cached bytes of one token's K (or V), all heads
+};
+
+// Bytes of the cache's parts, each rounded up to 256: K or V, exponents of
+// one, bounds, their exponents.
+struct PagedBytes {
+  size_t kv, exp, bounds, bounds_exp;
+};
+PagedBytes paged_bytes(int32_t n_layers, int32_t n_pages, int32_t n_heads, int32_t page_size,
+                       int32_t head_dim, int32_t format) {
+  const size_t per = (size_t)n_layers * n_pages * n_heads;
+  const size_t es = format == MARCHE_CACHE_BF16 ? 2 : 1;
+  return {align256(per * page_size * head_dim * es), es == 1 ? align256(per * page_size) : 0,
+          align256(per * 2 * head_dim), align256(per)};
+}
+
+// Checks the arguments that every call on the cache shares.
+marche_status_t check_paged(const marche_paged_cache_t *cache, int32_t layer, int32_t max_pages,
+                            int32_t n_seqs, PagedLayer *out) {
+  if (!cache) return fail(MARCHE_ERR_INVALID_ARG, "cache is NULL");
+  const int32_t format = raw_enum(cache->format);
+  marche_status_t st = MARCHE_OK;
+  if (!paged_shape(cache->n_layers, cache->n_pages, cache->n_heads, cache->page_size,
+                   cache->head_dim, format, &st))
+    return st;
+  if (layer < 0 || layer >= cache->n_layers)
+    return fail(MARCHE_ERR_INVALID_ARG, "layer=%d outside [0, n_layers=%d)", layer, cache->n_layers);
+  if (max_pages < 1) return fail(MARCHE_ERR_INVALID_ARG, "max_pages=%d < 1", max_pages);
+  if (n_seqs < 0) return fail(MARCHE_ERR_INVALID_ARG, "n_seqs=%d < 0", n_seqs);
+  if (!cache->k || !cache->v) return fail(MARCHE_ERR_INVALID_ARG, "cache.k / cache.v is NULL");
+  const bool bytes8 = format != MARCHE_CACHE_BF16;
+  if (bytes8 && (!cache->k_exp || !cache->v_exp))
+    return fail(MARCHE_ERR_INVALID_ARG, "cache.k_exp / cache.v_exp is NULL in an 8-bit cache");
+  if ((cache->bounds == nullptr) != (cache->bounds_exp == nullptr))
+    return fail(MARCHE_ERR_INVALID_ARG, "cache.bounds and cache.bounds_exp must both be given or both be NULL");
+  for (const void *p : {(const void *)cache->k, (const void *)cache->v,
+                        (const void *)(bytes8 ? cache->k_exp : nullptr),
+                        (const void *)(bytes8 ? cache->v_exp : nullptr), (const void *)cache->bounds})
+    if (reinterpret_cast<uintptr_t>(p) & 15)
+      return fail(MARCHE_ERR_INVALID_ARG, "the cache's buffers must be 16-byte aligned");
+  const size_t es = bytes8 ? 1 : 2;
+  const size_t per = (size_t)cache->n_pages * cache->n_heads, at = per * layer;
+  const size_t tok = at * cache->page_size;
+  out->k = static_cast<char *>(cache->k) + tok * cache->head_dim * es;
+  out->v = static_cast<char *>(cache->v) + tok * cache->head_dim * es;
+  out->k_exp = bytes8 ? cache->k_exp + tok : nullptr;
+  out->v_exp = bytes8 ? cache->v_exp + tok : nullptr;
+  out->bounds = cache->bounds ? cache->bounds + at * 2 * cache->head_dim : nullptr;
+  out->bounds_exp = cache->bounds ? cache->bounds_exp + at : nullptr;
+  out->page_log2 = __builtin_ctz((unsigned)cache->page_size);
+  out->row_bytes = (size_t)cache->n_heads * (cache->head_dim * es + (bytes8 ? 1 : 0));
+  return MARCHE_OK;
+}
+
+marche_status_t check_row_dtype(int32_t dtype) {
+  if (dtype != MARCHE_F32 && dtype != MARCHE_BF16)
+    return fail(MARCHE_ERR_UNSUPPORTED, "dtype=%d is not F32 or BF16", dtype);
+  return MARCHE_OK;
+}
+
+marche_status_t check_rows(const char *what, int32_t total, const int32_t *off, int32_t n_seqs,
+                           int64_t stride, int64_t width) {
+  if (total < 0 || (n_seqs == 0 && total > 0))
+    return fail(MARCHE_ERR_INVALID_ARG, "%s_total=%d with n_seqs=%d", what, total, n_seqs);
+  if (!off && n_seqs > 0 && total % n_seqs)
+    return fail(MARCHE_ERR_INVALID_ARG, "%s_off is NULL but %s_total=%d is no multiple of n_seqs=%d", what,
+                what, total, n_seqs);
+  if (stride < width || stride % 8)
+    return fail(MARCHE_ERR_INVALID_ARG, "row stride %lld: must be a multiple of 8, >= %lld",
+                (long long)stride, (long long)width);
+  return MARCHE_OK;
+}
+
+bool misaligned(const void *p) { return reinterpret_cast<uintptr_t>(p) & 15; }
+
+// MARCHE_VALIDATE: the device lists of a call, copied to the host.
+struct PagedLists {
+  const int32_t *page_table = nullptr, *lens = nullptr, *off = nullptr, *idx = nullptr,
+                *first = nullptr, *pages = nullptr;
+  int32_t n_seqs = 0, max_pages = 0, total = 0, row_max = 0, len_max = INT32_MAX, n_select = 0;
+};
+
+// A message naming the problem, or "" (host arrays).
+std::string check_lists(const PagedLists &l, const marche_paged_cache_t *c) {
+  auto say = [](const char *what, int b) { return std::string(what) + " (sequence " + std::to_string(b) + ")"; };
+  const int64_t cap = (int64_t)l.max_pages * c->page_size;
+  auto page_ok = [&](int b, int64_t tok) {
+    const int32_t p = l.page_table[(size_t)b * l.max_pages + tok / c->page_size];
+    return p >= 0 && p < c->n_pages;
+  };
+  if (l.off && (l.off[0] != 0 || l.off[l.n_seqs] != l.total)) return say("row offsets inconsistent with the total", 0);
+  for (int b = 0; b < l.n_seqs; ++b) {
+    const int32_t each = l.total / l.n_seqs;
+    const int32_t r0 = l.off ? l.off[b] : b * each, r1 = l.off ? l.off[b + 1] : r0 + each;
+    if (r0 < 0 || r1 < r0 || r1 > l.total || r1 - r0 > l.row_max) return say("row offsets inconsistent", b);
+    if (l.lens) {
+      if (l.lens[b] < 0 || l.lens[b] > cap || l.lens[b] > l.len_max) return say("length out of range", b);
+      for (int64_t t = 0; t < l.lens[b]; t += c->page_size)
+        if (!page_ok(b, t)) return say("page outside the pool", b);
+    }
+    if (l.first && (l.first[b] < 0 || l.first[b] > l.lens[b])) return say("first token out of range", b);
+    if (l.idx) {
+      std::vector<int32_t> seen(l.idx + r0, l.idx + r1);
+      std::sort(seen.begin(), seen.end());
+      for (size_t i = 0; i < seen.size(); ++i) {
+        if (seen[i] < 0 || seen[i] >= cap) return say("token out of range", b);
+        if (i && seen[i] == seen[i - 1]) return say("token listed twice", b);
+        if (!page_ok(b, seen[i])) return say("page outside the pool", b);
+      }
+    }
+    if (l.pages) {
+      const int64_t n = ((int64_t)l.lens[b] + c->page_size - 1) / c->page_size;
+      for (size_t x = (size_t)r0 * c->n_heads * l.n_select; x < (size_t)r1 * c->n_heads * l.n_select; ++x)
+        if (l.pages[x] < -1 || l.pages[x] >= n) return say("selected page out of range", b);
+    }
+  }
+  return "";
+}
+
+marche_status_t validate_paged(PagedLists l, const marche_paged_cache_t *c, hipStream_t stream) {
+  if (!validate_requested() || l.n_seqs == 0) return MARCHE_OK;
+  std::vector<std::vector<int32_t>> kept;
+  hipError_t e = hipSuccess;
+  auto fetch = [&](const int32_t *&p, size_t n) {
+    if (!p || e != hipSuccess) return;
+    kept.emplace_back(std::max<size_t>(n, 1));
+    if (n) e = hipMemcpyAsync(kept.back().data(), p, n * 4, hipMemcpyDeviceToHost, stream);
+    p = kept.back().data();
+  };
+  kept.reserve(6);
+  fetch(l.page_table, (size_t)l.n_seqs * l.max_pages);
+  fetch(l.lens, l.n_seqs);
+  fetch(l.off, (size_t)l.n_seqs + 1);
+  fetch(l.idx, l.total);
+  fetch(l.first, l.n_seqs);
+  fetch(l.pages, (size_t)l.total * c->n_heads * l.n_select);
+  if (e == hipSuccess) e = hipStreamSynchronize(stream);
+  if (e != hipSuccess) return fail_hip(e, "paged-list validation");
+  const std::string what = check_lists(l, c);
+  return what.empty() ? MARCHE_OK : fail(MARCHE_ERR_INVALID_ARG, "paged lists: %s", what.c_str());
+}
+
+// The kernel arguments that the workspace query and the call share.
+void paged_attn_sizes(PagedAttnArgs &p, const marche_paged_cache_t *c, int32_t n_seqs, int32_t q_total,
+                      int32_t q_max, int32_t n_q_heads, int32_t len_max, int32_t n_select, DType dt) {
+  p.n_pages = c->n_pages;
+  p.n_heads = c->n_heads;
+  p.page_log2 = __builtin_ctz((unsigned)c->page_size);
+  p.n_seqs = n_seqs;
+  p.q_total = q_total;
+  p.q_max = q_max;
+  p.group = n_q_heads / c->n_heads;
+  p.len_max = len_max;
+  p.n_select = n_select;
+  paged_plan(dt, c->head_dim, p);
+}
+
+size_t paged_part_rows(const PagedAttnArgs &p) {
+  return p.splits > 1 ? (size_t)p.splits * p.q_total * p.n_heads * p.group : 0;
+}
+
+}  // namespace
+
+size_t marche_paged_cache_bytes(int32_t n_layers, int32_t n_pages, int32_t n_heads,
+                                int32_t page_size, int32_t head_dim, int32_t format,
+                                int32_t with_bounds) {
+  marche_status_t st;
+  if (!paged_shape(n_layers, n_pages, n_heads, page_size, head_dim, format, &st)) return 0;
+  const PagedBytes p = paged_bytes(n_layers, n_pages, n_heads, page_size, head_dim, format);
+  return 2 * p.kv + 2 * p.exp + (with_bounds ? p.bounds + p.bounds_exp : 0);
+}
+
+marche_status_t marche_paged_cache_init(marche_paged_cache_t *cache, int32_t n_layers,
+                                        int32_t n_pages, int32_t n_heads, int32_t page_size,
+                                        int32_t head_dim, int32_t format, int32_t with_bounds,
+                                        void *buffer, size_t bytes) {
+  if (!cache) return fail(MARCHE_ERR_INVALID_ARG, "cache is NULL");
+  marche_status_t st;
+  if (!paged_shape(n_layers, n_pages, n_heads, page_size, head_dim, format, &st)) return st;
+  const size_t need =
+      marche_paged_cache_bytes(n_layers, n_pages, n_heads, page_size, head_dim, format, with_bounds);
+  if (!buffer || bytes < need)
+    return fail(MARCHE_ERR_INVALID_ARG, "buffer %s: %zu bytes < %zu needed",
+                buffer ? "too small" : "is NULL", bytes, need);
+  if (misaligned(buffer)) return fail(MARCHE_ERR_INVALID_ARG, "buffer must be 16-byte aligned");
+  const PagedBytes p = paged_bytes(n_layers, n_pages, n_heads, page_size, head_dim, format);
+  char *at = static_cast<char *>(buffer);
+  auto take = [&](size_t n) { char *q = at; at += n; return n ? q : nullptr; };
+  cache->k = take(p.kv);
+  cache->v = take(p.kv);
+  cache->k_exp = reinterpret_cast<uint8_t *>(take(p.exp));
+  cache->v_exp = reinterpret_cast<uint8_t *>(take(p.exp));
+  cache->bounds = reinterpret_cast<int8_t *>(take(with_bounds ? p.bounds : 0));
+  cache->bounds_exp = reinterpret_cast<uint8_t *>(take(with_bounds ? p.bounds_exp : 0));
+  cache->n_layers = n_layers;
+  cache->n_pages = n_pages;
+  cache->n_heads = n_heads;
+  cache->page_size = page_size;
+  cache->head_dim = head_dim;
+  cache->format = format;
+  return MARCHE_OK;
+}
+
+marche_status_t marche_paged_write(const marche_paged_cache_t *cache, int32_t layer,
+                                   const int32_t *page_table, int32_t max_pages, int32_t n_seqs,
+                                   const int32_t *a_idx, const int32_t *a_off, int32_t a_total,
+                                   const void *k_new, const void *v_new, int64_t row_stride,
+                                   int32_t dtype, marche_stream_t stream_) {
+  PagedLayer l;
+  marche_status_t st = check_paged(cache, layer, max_pages, n_seqs, &l);
+  if (st != MARCHE_OK || (st = check_row_dtype(dtype)) != MARCHE_OK) return st;
+  const int32_t H = cache->n_heads, dh = cache->head_dim;
+  if ((st = check_rows("a", a_total, a_off, n_seqs, row_stride, (int64_t)H * dh)) != MARCHE_OK) return st;
+  if ((int64_t)a_total * H >= (1LL << 31))
+    return fail(MARCHE_ERR_UNSUPPORTED, "a_total*n_heads reaches 2^31");
+  if (a_total == 0) return MARCHE_OK;
+  if (!page_table || !a_idx || !k_new || !v_new)
+    return fail(MARCHE_ERR_INVALID_ARG, "NULL input to marche_paged_write");
+  if (misaligned(k_new) || misaligned(v_new))
+    return fail(MARCHE_ERR_INVALID_ARG, "k_new and v_new must be 16-byte aligned");
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  PagedLists lists;
+  lists.page_table = page_table;
+  lists.off = a_off;
+  lists.idx = a_idx;
+  lists.n_seqs = n_seqs;
+  lists.max_pages = max_pages;
+  lists.total = lists.row_max = a_total;
+  if ((st = validate_paged(lists, cache, stream)) != MARCHE_OK) return st;
+  const PagedWriteArgs a{l.k, l.v, l.k_exp, l.v_exp, page_table, a_idx, a_off, k_new, v_new, row_stride,
+                         cache->n_pages, H, l.page_log2, max_pages, n_seqs, a_total, a_total / n_seqs};
+  // Algorithmic traffic: every new row read once, its slot written once.
+  LAUNCH(K_PAGED_WRITE, 0, 2.0 * a_total * ((double)H * dh * elem_size(dtype) + l.row_bytes) + 8.0 * a_total,
+         launch_paged_write(dtype == MARCHE_BF16 ? DType::BF16 : DType::F32, raw_enum(cache->format), dh, a,
+                            stream));
+  return MARCHE_OK;
+}
+
+marche_status_t marche_paged_read(const marche_paged_cache_t *cache, int32_t layer,
+                                  const int32_t *page_table, int32_t max_pages,
+                                  const int32_t *lens, int32_t n_seqs, int32_t n_tokens,
+                                  void *k_out, void *v_out, int32_t dtype,
+                                  marche_stream_t stream_) {
+  PagedLayer l;
+  marche_status_t st = check_paged(cache, layer, max_pages, n_seqs, &l);
+  if (st != MARCHE_OK || (st = check_row_dtype(dtype)) != MARCHE_OK) return st;
+  const int32_t H = cache->n_heads, dh = cache->head_dim;
+  if (n_tokens < 0) return fail(MARCHE_ERR_INVALID_ARG, "n_tokens=%d < 0", n_tokens);
+  if ((int64_t)n_seqs * H * ((n_tokens + PAGED_READ_TOKENS - 1LL) / PAGED_READ_TOKENS) >= (1LL << 31))
+    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs*n_heads*n_tokens too large");
+  if (n_seqs == 0 || n_tokens == 0) return MARCHE_OK;
+  if (!page_table || !lens || !k_out || !v_out)
+    return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_read");
+  if (misaligned(k_out) || misaligned(v_out))
+    return fail(MARCHE_ERR_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  PagedLists lists;
+  lists.page_table = page_table;
+  lists.lens = lens;
+  lists.n_seqs = n_seqs;
+  lists.max_pages = max_pages;
+  if ((st = validate_paged(lists, cache, stream)) != MARCHE_OK) return st;
+  PagedReadArgs a{l.k, l.v, l.k_exp, l.v_exp, page_table, lens, k_out, v_out, cache->n_pages, H,
+                  l.page_log2, max_pages, n_seqs, n_tokens, 0};
+  // Algorithmic traffic as if every sequence had n_tokens tokens (lens are on
+  // the device).
+  LAUNCH(K_PAGED_READ, 0, 2.0 * n_seqs * n_tokens * ((double)H * dh * elem_size(dtype) + l.row_bytes),
+         launch_paged_read(dtype == MARCHE_BF16 ? DType::BF16 : DType::F32, raw_enum(cache->format), dh, a,
+                           stream));
+  return MARCHE_OK;
+}
+
+marche_status_t marche_paged_bounds(const marche_paged_cache_t *cache, int32_t layer,
+                                    const int32_t *page_table, int32_t max_pages,
+                                    const int32_t *lens, const int32_t *first, int32_t span,
+                                    int32_t n_seqs, marche_stream_t stream_) {
+  PagedLayer l;
+  marche_status_t st = check_paged(cache, layer, max_pages, n_seqs, &l);
+  if (st != MARCHE_OK) return st;
+  if (!l.bounds) return fail(MARCHE_ERR_INVALID_ARG, "the cache has no bounds");
+  if (span < 0) return fail(MARCHE_ERR_INVALID_ARG, "span=%d < 0", span);
+  span = std::min(span, max_pages);
+  if ((int64_t)n_seqs * span * cache->n_heads >= (1LL << 31))
+    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs*span*n_heads reaches 2^31");
+  if (n_seqs == 0 || span == 0) return MARCHE_OK;
+  if (!page_table || !lens) return fail(MARCHE_ERR_INVALID_ARG, "NULL input to marche_paged_bounds");
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  PagedLists lists;
+  lists.page_table = page_table;
+  lists.lens = lens;
+  lists.first = first;
+  lists.n_seqs = n_seqs;
+  lists.max_pages = max_pages;
+  if ((st = validate_paged(lists, cache, stream)) != MARCHE_OK) return st;
+  const PagedBoundsArgs a{l.k, l.k_exp, l.bounds, l.bounds_exp, page_table, lens, first, cache->n_pages,
+                          cache->n_heads, l.page_log2, max_pages, n_seqs, span};
+  LAUNCH(K_PAGED_BOUNDS, 0,
+         (double)n_seqs * span * (cache->page_size * (double)l.row_bytes +
+                                  cache->n_heads * (2.0 * cache->head_dim + 1)),
+         launch_paged_bounds(raw_enum(cache->format), cache->head_dim, a, stream));
+  return MARCHE_OK;
+}
+
+namespace {
+
+// Arguments that the selection and the attention share.
+marche_status_t check_queries(const marche_paged_cache_t *cache, int32_t n_q_heads, int32_t dtype,
+                              int64_t q_stride, const int32_t *q_off, int32_t q_total, int32_t n_seqs) {
+  marche_status_t st = check_row_dtype(dtype);
+  if (st != MARCHE_OK) return st;
+  if (n_q_heads < 1 || n_q_heads % cache->n_heads)
+    return fail(MARCHE_ERR_INVALID_ARG, "n_q_heads=%d is no multiple of the cache's n_heads=%d", n_q_heads,
+                cache->n_heads);
+  return check_rows("q", q_total, q_off, n_seqs, q_stride, (int64_t)n_q_heads * cache->head_dim);
+}
+
+}  // namespace
+
+marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t layer,
+                                    const int32_t *page_table, int32_t max_pages,
+                                    const int32_t *lens, int32_t n_seqs, const void *q,
+                                    int64_t q_stride, const int32_t *q_off, int32_t q_total,
+                                    int32_t n_q_heads, int32_t dtype, int32_t n_select,
+                                    int32_t *pages, marche_stream_t stream_) {
+  PagedLayer l;
+  marche_status_t st = check_paged(cache, layer, max_pages, n_seqs, &l);
+  if (st != MARCHE_OK) return st;
+  if ((st = check_queries(cache, n_q_heads, dtype, q_stride, q_off, q_total, n_seqs)) != MARCHE_OK) return st;
+  if (!l.bounds) return fail(MARCHE_ERR_INVALID_ARG, "the cache has no bounds");
+  if (max_pages > PAGED_MAX_PAGES)
+    return fail(MARCHE_ERR_UNSUPPORTED, "max_pages=%d > %d", max_pages, PAGED_MAX_PAGES);
+  if (n_select < 1 || n_select > PAGED_MAX_PAGES)
+    return fail(MARCHE_ERR_INVALID_ARG, "n_select=%d outside [1, %d]", n_select, PAGED_MAX_PAGES);
+  if ((int64_t)q_total * n_q_heads >= (1LL << 31))
+    return fail(MARCHE_ERR_UNSUPPORTED, "q_total*n_q_heads reaches 2^31");
+  if (q_total == 0) return MARCHE_OK;
+  if (!page_table || !lens || !q || !pages)
+    return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_select");
+  if (misaligned(q)) return fail(MARCHE_ERR_INVALID_ARG, "q must be 16-byte aligned");
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  PagedLists lists;
+  lists.page_table = page_table;
+  lists.lens = lens;
+  lists.off = q_off;
+  lists.n_seqs = n_seqs;
+  lists.max_pages = max_pages;
+  lists.total = lists.row_max = q_total;
+  if ((st = validate_paged(lists, cache, stream)) != MARCHE_OK) return st;
+  const int32_t H = cache->n_heads, dh = cache->head_dim;
+  PagedSelectArgs a{};
+  a.bounds = l.bounds;
+  a.bounds_exp = l.bounds_exp;
+  a.table = page_table;
+  a.lens = lens;
+  a.q_off = q_off;
+  a.q = q;
+  a.pages = pages;
+  a.q_stride = q_stride;
+  a.n_pages = cache->n_pages;
+  a.n_heads = H;
+  a.page_log2 = l.page_log2;
+  a.max_pages = max_pages;
+  a.n_seqs = n_seqs;
+  a.q_total = q_total;
+  a.rows_each = q_total / n_seqs;
+  a.group = n_q_heads / H;
+  a.n_select = n_select;
+  // Algorithmic work and traffic as if every sequence had max_pages pages.
+  LAUNCH(K_PAGED_SELECT, 4.0 * q_total * (double)n_q_heads * dh * max_pages,
+         (double)n_seqs * max_pages * (H * (2.0 * dh + 1) + 4) +
+             (double)q_total * ((double)n_q_heads * dh * elem_size(dtype) + 4.0 * H * n_select),
+         launch_paged_select(dtype == MARCHE_BF16 ? DType::BF16 : DType::F32, dh, a, stream));
+  return MARCHE_OK;
+}
+
+size_t marche_paged_attention_workspace_bytes(const marche_paged_cache_t *cache, int32_t n_seqs,
+                                              int32_t q_total, int32_t q_max, int32_t n_q_heads,
+                                              int32_t len_max, int32_t n_select) {
+  PagedLayer l;
+  if (check_paged(cache, 0, 1, n_seqs, &l) != MARCHE_OK || q_total < 1 || q_max < 1 || len_max < 0 ||
+      n_select < 0 || n_q_heads < 1 || n_q_heads % cache->n_heads)
+    return 0;
+  size_t need = 0;
+  for (DType dt : {DType::BF16, DType::F32}) {  // either type of rows
+    PagedAttnArgs p{};
+    paged_attn_sizes(p, cache, n_seqs, q_total, q_max, n_q_heads, len_max, n_select, dt);
+    const size_t rows = paged_part_rows(p);
+    need = std::max(need, align256(rows * cache->head_dim * 4) + align256(rows * 8));
+  }
+  return need;
+}
+
+marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_t layer,
+                                       const int32_t *page_table, int32_t max_pages,
+                                       const int32_t *lens, int32_t len_max, int32_t n_seqs,
+                                       const void *q, int64_t q_stride, const int32_t *q_off,
+                                       int32_t q_total, int32_t q_max, int32_t n_q_heads,
+                                       int32_t dtype, void *o, const int32_t *pages,
+                                       int32_t n_select, void *workspace, size_t workspace_bytes,
+                                       marche_stream_t stream_) {
+  PagedLayer l;
+  marche_status_t st = check_paged(cache, layer, max_pages, n_seqs, &l);
+  if (st != MARCHE_OK) return st;
+  if ((st = check_queries(cache, n_q_heads, dtype, q_stride, q_off, q_total, n_seqs)) != MARCHE_OK) return st;
+  if (len_max < 0 || len_max > (int64_t)max_pages * cache->page_size)
+    return fail(MARCHE_ERR_INVALID_ARG, "len_max=%d outside [0, max_pages*page_size=%lld]", len_max,
+                (long long)max_pages * cache->page_size);
+  if (len_max > INT32_MAX - 4096) return fail(MARCHE_ERR_UNSUPPORTED, "len_max=%d", len_max);
+  if (q_max < 0 || q_max > q_total || (q_total > 0 && q_max == 0) ||
+      (!q_off && n_seqs > 0 && q_max != q_total / n_seqs))
+    return fail(MARCHE_ERR_INVALID_ARG, "q_max=%d inconsistent with q_total=%d", q_max, q_total);
+  if (!pages && n_select != 0) return fail(MARCHE_ERR_INVALID_ARG, "n_select=%d without pages", n_select);
+  if (pages && (n_select < 1 || n_select > PAGED_MAX_PAGES))
+    return fail(MARCHE_ERR_INVALID_ARG, "n_select=%d outside [1, %d]", n_select, PAGED_MAX_PAGES);
+  if (pages && max_pages > PAGED_MAX_PAGES)
+    return fail(MARCHE_ERR_UNSUPPORTED, "max_pages=%d > %d with selected pages", max_pages, PAGED_MAX_PAGES);
+  const int32_t H = cache->n_heads, dh = cache->head_dim;
+  if ((int64_t)q_total * n_q_heads * dh >= (1LL << 37) || (int64_t)q_max * (n_q_heads / H) >= (1LL << 30))
+    return fail(MARCHE_ERR_UNSUPPORTED, "too many query rows");
+  if (q_total == 0) return MARCHE_OK;
+  const DType dt = dtype == MARCHE_BF16 ? DType::BF16 : DType::F32;
+  PagedAttnArgs a{};
+  a.max_pages = max_pages;
+  paged_attn_sizes(a, cache, n_seqs, q_total, q_max, n_q_heads, len_max, n_select, dt);
+  if ((int64_t)n_seqs * H * a.row_blocks * a.splits >= (1LL << 31))
+    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs*n_heads*rows too large");
+  if (!page_table || !lens || !q || !o)
+    return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_attention");
+  if (misaligned(q) || misaligned(o)) return fail(MARCHE_ERR_INVALID_ARG, "q and o must be 16-byte aligned");
+  const size_t rows = paged_part_rows(a);
+  const size_t need = align256(rows * dh * 4) + align256(rows * 8);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(MARCHE_ERR_WORKSPACE, "workspace %s: %zu bytes < %zu needed",
+                workspace ? "too small" : "is NULL", workspace_bytes, need);
+  if (reinterpret_cast<uintptr_t>(workspace) & 255)
+    return fail(MARCHE_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  PagedLists lists;
+  lists.page_table = page_table;
+  lists.lens = lens;
+  lists.off = q_off;
+  lists.pages = pages;
+  lists.n_seqs = n_seqs;
+  lists.max_pages = max_pages;
+  lists.total = q_total;
+  lists.row_max = q_max;
+  lists.len_max = len_max;
+  lists.n_select = n_select;
+  if ((st = validate_paged(lists, cache, stream)) != MARCHE_OK) return st;
+  a.k = l.k;
+  a.v = l.v;
+  a.k_exp = l.k_exp;
+  a.v_exp = l.v_exp;
+  a.table = page_table;
+  a.lens = lens;
+  a.q_off = q_off;
+  a.q = q;
+  a.o = o;
+  a.pages = pages;
+  a.part_o = static_cast<float *>(workspace);
+  a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + align256(rows * dh * 4));
+  a.q_stride = q_stride;
+  a.rows_each = q_total / n_seqs;
+  a.sl2 = (float)(1.4426950408889634 / std::sqrt((double)dh));
+  // Algorithmic work and traffic as if every sequence had len_max tokens.
+  const double keys = pages ? std::min<double>(len_max, (double)n_select * cache->page_size) : len_max;
+  LAUNCH(K_PAGED_ATTN, 4.0 * q_total * (double)n_q_heads * dh * keys,
+         2.0 * n_seqs * keys * (double)l.row_bytes + 2.0 * q_total * (double)n_q_heads * dh * elem_size(dtype),
+         launch_paged_attention(dt, raw_enum(cache->format), dh, a, stream));
+  if (a.splits > 1)
+    LAUNCH(K_PAGED_JOIN, 0, (double)rows * (dh + 2) * 4 + (double)q_total * n_q_heads * dh * elem_size(dtype),
+           launch_paged_join(dt, dh, a, stream));
   return MARCHE_OK;
 }
 

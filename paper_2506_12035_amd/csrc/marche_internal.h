@@ -247,4 +247,74 @@ hipError_t launch_select_topk(const float *scores, int32_t n_parts, const int32_
                               int32_t *out_idx, const int32_t *out_off, bool lowest,
                               hipStream_t s);
 
+// ---- paged cache (k_paged.hip, k_paged_attn_*.hip) ----
+// Pointers are one layer's; formats are marche_cache_format_t; a page holds
+// 1 << page_log2 tokens.  *_off NULL: every sequence has rows_each rows.
+struct PagedWriteArgs {
+  void *k, *v;
+  uint8_t *k_exp, *v_exp;
+  const int32_t *table, *a_idx, *a_off;
+  const void *k_new, *v_new;
+  int64_t row_stride;
+  int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, a_total, rows_each;
+};
+hipError_t launch_paged_write(DType dt, int32_t format, int32_t head_dim, const PagedWriteArgs &a,
+                              hipStream_t s);
+constexpr int PAGED_READ_TOKENS = 128;  // tokens per workgroup of the read kernel
+struct PagedReadArgs {
+  const void *k, *v;
+  const uint8_t *k_exp, *v_exp;
+  const int32_t *table, *lens;
+  void *k_out, *v_out;
+  int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, n_tokens, blocks;
+};
+hipError_t launch_paged_read(DType dt, int32_t format, int32_t head_dim, PagedReadArgs a,
+                             hipStream_t s);
+struct PagedBoundsArgs {
+  const void *k;
+  const uint8_t *k_exp;
+  int8_t *bounds;
+  uint8_t *bounds_exp;
+  const int32_t *table, *lens, *first;
+  int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, span;
+};
+hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, const PagedBoundsArgs &a,
+                               hipStream_t s);
+constexpr int PAGED_MAX_PAGES = 4096;  // pages of a sequence, where pages are selected
+struct PagedSelectArgs {
+  const int8_t *bounds;
+  const uint8_t *bounds_exp;
+  const int32_t *table, *lens, *q_off;
+  const void *q;
+  int32_t *pages;
+  int64_t q_stride;
+  int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, q_total, rows_each, group, n_select;
+  int32_t rows_per, p_cap;  // set by the launch: rows per workgroup, keys per row in LDS
+};
+hipError_t launch_paged_select(DType dt, int32_t head_dim, PagedSelectArgs a, hipStream_t s);
+struct PagedAttnArgs {
+  const void *k, *v;
+  const uint8_t *k_exp, *v_exp;
+  const int32_t *table, *lens, *q_off;
+  const void *q;
+  void *o;
+  const int32_t *pages;  // [q_total][n_heads][n_select], or NULL: every token
+  float *part_o, *part_ml;
+  int64_t q_stride;
+  int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, q_total, q_max, rows_each, group, len_max,
+      n_select;
+  float sl2;  // log2(e) / sqrt(head_dim)
+  // the plan (paged_plan): 16-row tiles and wavefronts per workgroup, row
+  // blocks per sequence, key ranges, 32-key tiles per range, rows of a block
+  int32_t row_tiles, waves, row_blocks, splits, chunk, bit_rows;
+};
+// Fills the plan from the sizes.
+void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a);
+hipError_t launch_paged_attention(DType dt, int32_t format, int32_t head_dim, const PagedAttnArgs &a,
+                                  hipStream_t s);
+hipError_t launch_paged_join(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
+hipError_t launch_paged_attention_bf16(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
+hipError_t launch_paged_attention_e4m3(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
+hipError_t launch_paged_attention_int8(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
+
 }  // namespace marche
