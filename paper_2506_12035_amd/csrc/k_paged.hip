@@ -270,29 +270,40 @@ __device__ __forceinline__ uint32_t score_key(float f) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// Page selection.  One workgroup per (16-column tile of packed rows, key head): the
-// columns are query heads of `rows_per` consecutive rows.  Each row's queries
-// are quantised to int8 with an exponent of their own, split by sign, and
+// Four int8 numbers from floats whose low bytes hold them.
+__device__ __forceinline__ int pack_low(float a, float b, float c, float d) {
+  const uint32_t x = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x0C0C0400u);
+  const uint32_t y = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x04000C0Cu);
+  return (int)(x | y);
+}
+
+// Page selection.  One workgroup per (rows_per consecutive rows, key head): the
+// query heads of those rows that share the key head are the columns of 16-wide
+// products.  Each row's queries are quantised to int8 with an exponent of their
+// own, split by sign, and
 //   score = sum_d (q_d > 0 ? q_d hi_d : q_d lo_d) = [q+ ; q-] . [hi ; lo]
 // is an int8 product on the matrix cores (16 pages x 16 columns x 64 deep per
 // instruction) against the bounds as they lie in memory: whole numbers below
 // 2^24, so the sum is exact in any order and scaling it by the two powers of
 // two is too.  The largest over a row's heads is taken in LDS.  Then one
-// wavefront per row finds the k-th largest key by its bits, from the top, and
-// compacts the pages above it (and the first of those equal to it) in
+// wavefront per row finds the n_select-th largest key by its bits, from the
+// top, and compacts the pages above it (and the first of those equal to it) in
 // ascending order.
 template <int DH, typename InT, int KPL>
 __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
   constexpr int ST = (2 * DH + 63) / 64;
+  constexpr int NT = 2;  // 16-page tiles in flight
   extern __shared__ uint32_t s_key[];  // [rows_per][p_cap]
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
+  __shared__ int s_len[16], s_seq[16];
+  const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g = lane >> 4;
   const int h = blockIdx.x % a.n_heads;
   const int r0 = (blockIdx.x / a.n_heads) * a.rows_per;
 
-  for (int x = tid; x < a.rows_per * a.p_cap; x += blockDim.x) s_key[x] = 0u;
-  // the rows of the tile may belong to different sequences
-  __shared__ int s_len[16], s_seq[16];
+  if (a.group > 1)
+    for (int x = tid; x < a.rows_per * a.p_cap; x += blockDim.x) s_key[x] = 0u;
+  // the rows may belong to different sequences
   if (wave == 0) {
     int b = a.q_off ? wave_find_seq(a.q_off, a.n_seqs, min(r0, a.q_total - 1), lane) : 0;
     if (lane < a.rows_per) {
@@ -306,87 +317,98 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
   }
   __syncthreads();
 
-  // a tile whose rows share a sequence is scored at once; else row by row
-  int lo = 0;
-  while (lo < a.rows_per) {
-    int end = lo + 1;
-    while (end < a.rows_per && s_seq[end] == s_seq[lo]) ++end;
-    const int b = s_seq[lo], n_p = (s_len[lo] + (1 << a.page_log2) - 1) >> a.page_log2;
-    if (b < a.n_seqs && n_p > a.n_select) {
-      const int cols = (end - lo) * a.group;
-      for (int col0 = 0; col0 < cols; col0 += 16) {
-        const int col = col0 + c;
-        const bool on = col < cols;
-        const int i = lo + (on ? col / a.group : 0), hg = on ? col % a.group : 0;
-        const InT *qp = static_cast<const InT *>(a.q) + (size_t)(r0 + i) * a.q_stride +
-                        (size_t)(h * a.group + hg) * DH;
-        // this lane's 16-element groups of [q+ ; q-]
-        float x[ST][16];
-        uint32_t am = 0;
+  // runs of rows of one sequence are scored at once
+  for (int lo = 0, end; lo < a.rows_per; lo = end) {
+    const int b = __builtin_amdgcn_readfirstlane(s_seq[lo]);
+    const int n_p = __builtin_amdgcn_readfirstlane((s_len[lo] + (1 << a.page_log2) - 1) >> a.page_log2);
+    end = lo + 1;
+    while (end < a.rows_per && s_seq[end] == b) ++end;
+    if (b >= a.n_seqs || n_p <= a.n_select || 16 * wave >= n_p) continue;
+    const int cols = (end - lo) * a.group;
+    for (int col0 = 0; col0 < cols; col0 += 16) {
+      const int col = col0 + c;
+      const bool on = col < cols;
+      const int i = lo + (on ? col / a.group : 0), hg = on ? col % a.group : 0;
+      const InT *qp = static_cast<const InT *>(a.q) + (size_t)(r0 + i) * a.q_stride +
+                      (size_t)(h * a.group + hg) * DH;
+      // this lane's 16-element groups of [q+ ; q-]
+      float x[ST][16];
+      uint32_t am = 0;
 #pragma unroll
-        for (int s = 0; s < ST; ++s) {
-          const int k0 = 64 * s + 16 * g;
-          const bool in = on && k0 < 2 * DH;
-          const InT *p = qp + (k0 < DH ? k0 : k0 - DH);
+      for (int s = 0; s < ST; ++s) {
+        const int k0 = 64 * s + 16 * g;
+        const InT *p = qp + (k0 < DH ? k0 : k0 - DH);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[s][e] = 0.f;
-          if (in) {
-            load8(p, x[s]);
-            load8(p + 8, x[s] + 8);
-          }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) am = max(am, __float_as_uint(x[s][e]) & 0x7FFFFFFFu);
+        for (int e = 0; e < 16; ++e) x[s][e] = 0.f;
+        if (on && k0 < 2 * DH) {
+          load8(p, x[s]);
+          load8(p + 8, x[s] + 8);
         }
-        am = max(am, (uint32_t)__shfl_xor((int)am, 16, 64));
-        am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
-        const int qc = exp_code<I8>(__uint_as_float(am));
-        const float inv = qc == 255 ? 0.f : exp_inv(qc), qs = exp_scale(qc);
-        i32x4 qf[ST];
 #pragma unroll
-        for (int s = 0; s < ST; ++s) {
-          const bool neg = 64 * s + 16 * g >= DH;
+        for (int e = 0; e < 16; ++e) am = max(am, __float_as_uint(x[s][e]) & 0x7FFFFFFFu);
+      }
+      am = max(am, (uint32_t)__shfl_xor((int)am, 16, 64));
+      am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
+      const int qc = exp_code<I8>(__uint_as_float(am));
+      // a query that is not finite: NaN for every score
+      const float inv = exp_inv(min(qc, 253)), qs = qc == 255 ? NAN : exp_scale(qc);
+      i32x4 qf[ST];
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            uint32_t v = 0;
+      for (int s = 0; s < ST; ++s) {
+        const bool neg = 64 * s + 16 * g >= DH;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int q = qc == 255 ? 0 : (int)rintf(x[s][4 * w + e] * inv);
-              v |= ((uint32_t)(neg ? min(q, 0) : max(q, 0)) & 0xFFu) << (8 * e);
-            }
-            qf[s][w] = (int)v;
+        for (int w = 0; w < 4; ++w) {
+          float y[4];
+          // x inv is exact; adding 1.5 2^23 rounds it to a whole number (ties to
+          // even), whose two's complement is the sum's low byte
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = x[s][4 * w + e];
+            y[e] = fmaf(neg ? fminf(v, 0.f) : fmaxf(v, 0.f), inv, 12582912.f);
           }
+          qf[s][w] = pack_low(y[0], y[1], y[2], y[3]);
         }
-        for (int p0 = 16 * wave; p0 < n_p; p0 += 16 * waves) {
-          const int pc = min(p0 + c, n_p - 1);
-          const int page = a.table[(size_t)b * a.max_pages + pc];
+      }
+      const int32_t *tab = a.table + (size_t)b * a.max_pages;
+      for (int p0 = 16 * wave; p0 < n_p; p0 += 16 * NT * waves) {
+        float be[NT];
+        i32x4 bf[NT][ST];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const int page = tab[min(p0 + 16 * t * waves + c, n_p - 1)];
           const bool ok = (unsigned)page < (unsigned)a.n_pages;
-          const size_t at = ((size_t)(ok ? page : 0) * a.n_heads + h);
-          const float be = exp_scale(a.bounds_exp[at]);
-          i32x4 acc = {0, 0, 0, 0};
+          const size_t at = (size_t)(ok ? page : 0) * a.n_heads + h;
+          const uint32_t code = a.bounds_exp[at];
 #pragma unroll
           for (int s = 0; s < ST; ++s) {
-            i32x4 bf = {0, 0, 0, 0};
-            if (64 * s + 16 * g < 2 * DH)
-              bf = *reinterpret_cast<const i32x4 *>(a.bounds + at * 2 * DH + 64 * s + 16 * g);
-            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf, qf[s], acc, 0, 0, 0);
+            bf[t][s] = i32x4{0, 0, 0, 0};
+            if (64 * s + 48 < 2 * DH || 64 * s + 16 * g < 2 * DH)
+              bf[t][s] = *reinterpret_cast<const i32x4 *>(a.bounds + at * 2 * DH + 64 * s + 16 * g);
           }
+          // bounds that are not finite, and pages outside the pool: NaN
+          be[t] = ok && code != 255 ? exp_scale(code) : NAN;
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const int pt = p0 + 16 * t * waves;
+          i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+          for (int s = 0; s < ST; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf[t][s], qf[s], acc, 0, 0, 0);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             // lane's page 4 g + j: its exponent sits in lane 4 g + j
-            const float bs = __shfl(be, 4 * g + j, 64);
-            const bool there = __shfl((int)ok, 4 * g + j, 64) != 0;
-            const int p = p0 + 4 * g + j;
+            const float bs = __shfl(be[t], 4 * g + j, 64);
+            const uint32_t key = score_key((float)acc[j] * bs * qs);
+            const int p = pt + 4 * g + j;
             if (on && p < n_p) {
-              // (exponent code 255: a bound that is not finite, whatever its bytes)
-              const uint32_t key = there ? score_key(bs < INFINITY ? (float)acc[j] * bs * qs : NAN) : 1u;
-              if (a.group == 1) s_key[i * a.p_cap + p] = key;
-              else atomicMax(&s_key[i * a.p_cap + p], key);
+              uint32_t *to = &s_key[i * a.p_cap + p];
+              if (a.group == 1) *to = key;
+              else atomicMax(to, key);
             }
           }
         }
       }
     }
-    lo = end;
   }
   __syncthreads();
 
@@ -408,16 +430,24 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
       for (int j = 0; j < KPL; ++j) n += __popcll(__ballot(kr[j] >= v));
       return n;
     };
-    uint32_t t = 0;  // the n_select-th largest key
-    for (int bit = 31; bit >= 0; --bit)
-      if (count_ge(t | (1u << bit)) >= a.n_select) t |= 1u << bit;
-    const int ties = a.n_select - (t == 0xFFFFFFFFu ? 0 : count_ge(t + 1u));
+    // the largest t with n_select keys or more at or above it; where there are
+    // just as many, they are the selection
+    uint32_t t = 0;
+    int at_least = n_p;
+    for (int bit = 31; bit >= 0 && at_least != a.n_select; --bit) {
+      const int n = count_ge(t | (1u << bit));
+      if (n >= a.n_select) t |= 1u << bit, at_least = n;
+    }
+    // of the keys equal to t the first `ties` are taken (at_least == n_select: all)
+    const int above = at_least == a.n_select || t == 0xFFFFFFFFu ? 0 : count_ge(t + 1u);
+    const int ties = a.n_select - above;
+    const bool all = at_least == a.n_select;
     int base = 0, tie_base = 0;
     const unsigned long long below = (1ull << lane) - 1ull;
 #pragma unroll
     for (int j = 0; j < KPL; ++j) {
       const unsigned long long tie = __ballot(kr[j] != 0u && kr[j] == t);
-      const bool take = kr[j] != 0u && (kr[j] > t || (kr[j] == t && tie_base + __popcll(tie & below) < ties));
+      const bool take = kr[j] != 0u && (kr[j] > t || (kr[j] == t && (all || tie_base + __popcll(tie & below) < ties)));
       const unsigned long long sel = __ballot(take);
       if (take) out[base + __popcll(sel & below)] = 64 * j + lane;
       base += __popcll(sel);
@@ -428,36 +458,66 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
 
 // ------------------------------------------------------------------ join
 
-// Joins the key ranges' parts: part s of a row counts exp2(m_s - m) of it.
-// One thread per (row, head, 4 channels).
+// Joins the key ranges' parts: part s of a row counts exp2(m_s - m) of it, m the
+// largest m_s.  One workgroup per (row, head); each of its four wavefronts
+// holds every part's maximum and sum (lane s part s: there are at most 64) and
+// sums every fourth part, four of them in flight.
 template <int DH, typename RowT>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
-  constexpr int C4 = DH / 4;
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  constexpr int C = DH == 64 ? 1 : 2;  // channels per lane, C lane + e
+  __shared__ float s_sum[4][2 * 64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t n = (int64_t)a.q_total * a.n_heads * a.group;
-  const int64_t row = x / C4;
-  if (row >= n) return;
-  const int d = (int)(x - row * C4) * 4;
+  const int64_t row = blockIdx.x;
+  // everything that needs no other load first: the parts' statistics (of as
+  // many ranges as there can be) and the sequences' lengths
+  float ms = 0.f, ls = 0.f;
+  if (lane < a.splits) {
+    ms = a.part_ml[2 * (lane * n + row)];
+    ls = a.part_ml[2 * (lane * n + row) + 1];
+  }
   // rows behind the last sequence (or before the first) belong to nobody
   const int r = (int)(row / (a.n_heads * a.group));
   if (a.q_off && (r < a.q_off[0] || r >= a.q_off[a.n_seqs])) return;
-  float m = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * n + row)]);
-  float l = 0.f;
-  bool any = false;
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.splits; ++s) {
-    const float ms = a.part_ml[2 * (s * n + row)], ls = a.part_ml[2 * (s * n + row) + 1];
-    if (ls == -1.f) continue;
-    any = true;
-    const float w = ms == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(ms - m);
-    l += ls * w;
-    sum += *reinterpret_cast<const f32x4 *>(a.part_o + (s * n + row) * DH + d) * w;
+  int splits = a.splits;
+  if (a.budget > 0) {  // the ranges of the row's sequence
+    const int b = a.q_off ? min(wave_find_seq(a.q_off, a.n_seqs, r, lane), a.n_seqs - 1) : r / a.rows_each;
+    const Shares sh(a, lane);
+    splits = sh.ranges((min(paged_len(a.lens[b], a.max_pages, a.page_log2), a.len_max) + 31) >> 5);
   }
-  const float inv = any ? 1.f / l : 0.f;
-  RowT *out = static_cast<RowT *>(a.o) + row * DH + d;
+  const bool has = lane < splits && ls != -1.f;  // a part that saw keys
+  if (!has) ms = -INFINITY;
+  const unsigned long long seen = __ballot(has);
+  const float m = wave_max(ms);
+  const float w = !has ? 0.f : ms == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(ms - m);
+  const float l = wave_sum(has ? ls * w : 0.f);
+  const bool on = C * lane < DH;
+  float sum[C] = {};
+  for (int s0 = wave; s0 < splits; s0 += 16) {
+    float x[4][C];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) out[e] = (RowT)(any ? sum[e] * inv : 0.f);
+    for (int u = 0; u < 4; ++u) {
+      const float *o = a.part_o + (min(s0 + 4 * u, splits - 1) * n + row) * DH + (on ? C * lane : 0);
+#pragma unroll
+      for (int e = 0; e < C; ++e) x[u][e] = o[e];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int s = s0 + 4 * u;
+      const float ws = __shfl(w, min(s, 63), 64);
+      const bool add = s < splits && ((seen >> s) & 1);  // (a part without keys was not written)
+#pragma unroll
+      for (int e = 0; e < C; ++e) sum[e] = add ? fmaf(x[u][e], ws, sum[e]) : sum[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < C; ++e) s_sum[wave][C * lane + e] = sum[e];
+  __syncthreads();
+  const int d = threadIdx.x;
+  if (d >= DH) return;
+  const float total = (s_sum[0][d] + s_sum[1][d]) + (s_sum[2][d] + s_sum[3][d]);
+  static_cast<RowT *>(a.o)[row * DH + d] = (RowT)(seen ? total / l : 0.f);
 }
 
 // ------------------------------------------------------------------ launches
@@ -516,11 +576,13 @@ hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, const PagedBoun
 hipError_t launch_paged_select(DType dt, int32_t head_dim, PagedSelectArgs a, hipStream_t s) {
   if (a.q_total == 0) return hipSuccess;
   a.p_cap = (a.max_pages + 63) / 64 * 64;
-  // rows that fill the 16 columns, as far as their keys fit 32 KB of LDS
-  a.rows_per = std::max(1, std::min({16 / a.group, 8192 / a.p_cap, a.q_total}));
+  // consecutive rows that a sequence is likely to own, as far as they fit the
+  // 16 columns and their keys 32 KB of LDS
+  const int mean = (a.q_total + a.n_seqs - 1) / a.n_seqs;
+  a.rows_per = std::max(1, std::min({16 / a.group, 8192 / a.p_cap, mean}));
   const unsigned grid = (unsigned)(((int64_t)a.q_total + a.rows_per - 1) / a.rows_per * a.n_heads);
-  // a wavefront per 16 pages, or per row where that is more
-  const int waves = std::min(16, std::max((a.max_pages + 15) / 16, a.rows_per));
+  // a wavefront per two tiles of 16 pages, or per four rows where that is more
+  const int waves = std::min(16, std::max((a.max_pages + 31) / 32, (a.rows_per + 3) / 4));
   const uint32_t lds = (uint32_t)a.rows_per * a.p_cap * 4;
   return by_shape(BF, head_dim, [&](auto, auto dh) {
     auto go = [&](auto kpl) {
@@ -537,9 +599,14 @@ hipError_t launch_paged_select(DType dt, int32_t head_dim, PagedSelectArgs a, hi
   });
 }
 
+int64_t paged_grid(const PagedAttnArgs &a) {
+  const int64_t pairs = (int64_t)(a.budget > 0 ? a.budget : a.n_seqs) * a.n_heads;  // dealt to 8 XCDs
+  return (pairs + 7) / 8 * 8 * a.row_blocks * (a.budget > 0 ? 1 : a.splits);
+}
+
 void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
   const int rows = a.q_max * a.group;  // packed rows of a sequence and key head
-  a.row_tiles = rows <= 16 ? 1 : rows <= 32 || dt == DType::F32 ? 2 : 4;
+  a.row_tiles = rows <= 16 || dt == DType::F32 ? 1 : 2;
   a.row_blocks = (rows + 16 * a.row_tiles - 1) / (16 * a.row_tiles);
   const int block_rows = std::min(a.q_max, (16 * a.row_tiles + a.group - 2) / a.group + 1);
   a.bit_rows = block_rows;
@@ -550,7 +617,8 @@ void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
            << a.page_log2;
   const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32);
   const int64_t units = std::max<int64_t>(1, (int64_t)a.n_seqs * a.n_heads * a.row_blocks);
-  // wavefronts per unit: enough of them for the chip, two tiles each at least
+  // Wavefronts per unit: enough of them to fill the chip, two tiles each at
+  // least; beyond a workgroup's, the keys are split over workgroups.
   const int64_t want = std::min<int64_t>((4096 + units - 1) / units, (tiles + 1) / 2);
   const int most = a.row_tiles == 1 ? 8 : 4;
   a.waves = 1;
@@ -559,6 +627,22 @@ void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
   a.chunk = (int32_t)((tiles + splits - 1) / splits);
   a.chunk = (a.chunk + a.waves - 1) / a.waves * a.waves;
   a.splits = (int32_t)((tiles + a.chunk - 1) / a.chunk);
+  a.budget = 0;
+  // Split caches may differ in length, so that the longest would be waited for:
+  // equal ranges, shared out on the device, over 512 workgroups (two of 4
+  // wavefronts per compute unit; measured against 256 to 1024 of 2 to 8).
+  const int64_t per = (int64_t)a.n_heads * a.row_blocks;
+  if (a.n_select == 0 && a.n_seqs <= PAGED_MAX_SHARED && tiles * a.n_seqs < (1LL << 31) &&
+      a.splits > 1) {
+    a.waves = std::min(a.waves, 4);
+    a.budget = (int32_t)std::max<int64_t>(2 * a.n_seqs, (512 + per - 1) / per);
+    a.chunk = 2 * a.waves;  // at least
+    a.splits = (int32_t)std::min<int64_t>({64, a.budget, (tiles + a.chunk - 1) / a.chunk});
+  }
+  a.d_splits = FastDiv::of(a.budget > 0 ? 1 : a.splits);
+  a.d_blocks = FastDiv::of(a.row_blocks);
+  a.d_heads = FastDiv::of(a.n_heads);
+  a.d_group = FastDiv::of(a.group);
 }
 
 hipError_t launch_paged_attention(DType dt, int32_t format, int32_t head_dim, const PagedAttnArgs &a,
@@ -572,8 +656,7 @@ hipError_t launch_paged_attention(DType dt, int32_t format, int32_t head_dim, co
 }
 
 hipError_t launch_paged_join(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s) {
-  const int64_t n = (int64_t)a.q_total * a.n_heads * a.group * (head_dim / 4);
-  const unsigned grid = (unsigned)((n + 255) / 256);
+  const unsigned grid = (unsigned)((int64_t)a.q_total * a.n_heads * a.group);
   return by_shape(BF, head_dim, [&](auto, auto dh) {
     if (dt == DType::BF16) launch_kernel(paged_join_kernel<dh.value, bf16>, grid, 256, 0, s, a);
     else launch_kernel(paged_join_kernel<dh.value, float>, grid, 256, 0, s, a);

@@ -1126,9 +1126,12 @@ struct PagedLists {
   int32_t n_seqs = 0, max_pages = 0, total = 0, row_max = 0, len_max = INT32_MAX, n_select = 0;
 };
 
-// A message naming the problem, or "" (host arrays).
-std::string check_lists(const PagedLists &l, const marche_paged_cache_t *c) {
-  auto say = [](const char *what, int b) { return std::string(what) + " (sequence " + std::to_string(b) + ")"; };
+// What is wrong with the lists (host arrays), or NULL; `seq`: where.
+const char *check_lists(const PagedLists &l, const marche_paged_cache_t *c, int32_t *seq) {
+  auto say = [&](const char *what, int b) {
+    *seq = b;
+    return what;
+  };
   const int64_t cap = (int64_t)l.max_pages * c->page_size;
   auto page_ok = [&](int b, int64_t tok) {
     const int32_t p = l.page_table[(size_t)b * l.max_pages + tok / c->page_size];
@@ -1160,7 +1163,7 @@ std::string check_lists(const PagedLists &l, const marche_paged_cache_t *c) {
         if (l.pages[x] < -1 || l.pages[x] >= n) return say("selected page out of range", b);
     }
   }
-  return "";
+  return nullptr;
 }
 
 marche_status_t validate_paged(PagedLists l, const marche_paged_cache_t *c, hipStream_t stream) {
@@ -1182,8 +1185,9 @@ marche_status_t validate_paged(PagedLists l, const marche_paged_cache_t *c, hipS
   fetch(l.pages, (size_t)l.total * c->n_heads * l.n_select);
   if (e == hipSuccess) e = hipStreamSynchronize(stream);
   if (e != hipSuccess) return fail_hip(e, "paged-list validation");
-  const std::string what = check_lists(l, c);
-  return what.empty() ? MARCHE_OK : fail(MARCHE_ERR_INVALID_ARG, "paged lists: %s", what.c_str());
+  int32_t seq = 0;
+  const char *what = check_lists(l, c, &seq);
+  return what ? fail(MARCHE_ERR_INVALID_ARG, "paged lists: %s (sequence %d)", what, seq) : MARCHE_OK;
 }
 
 // The kernel arguments that the workspace query and the call share.
@@ -1451,7 +1455,7 @@ marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_
   if (len_max < 0 || len_max > (int64_t)max_pages * cache->page_size)
     return fail(MARCHE_ERR_INVALID_ARG, "len_max=%d outside [0, max_pages*page_size=%lld]", len_max,
                 (long long)max_pages * cache->page_size);
-  if (len_max > INT32_MAX - 4096) return fail(MARCHE_ERR_UNSUPPORTED, "len_max=%d", len_max);
+  if (len_max > 1 << 30) return fail(MARCHE_ERR_UNSUPPORTED, "len_max=%d > 2^30", len_max);
   if (q_max < 0 || q_max > q_total || (q_total > 0 && q_max == 0) ||
       (!q_off && n_seqs > 0 && q_max != q_total / n_seqs))
     return fail(MARCHE_ERR_INVALID_ARG, "q_max=%d inconsistent with q_total=%d", q_max, q_total);
@@ -1461,14 +1465,14 @@ marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_
   if (pages && max_pages > PAGED_MAX_PAGES)
     return fail(MARCHE_ERR_UNSUPPORTED, "max_pages=%d > %d with selected pages", max_pages, PAGED_MAX_PAGES);
   const int32_t H = cache->n_heads, dh = cache->head_dim;
-  if ((int64_t)q_total * n_q_heads * dh >= (1LL << 37) || (int64_t)q_max * (n_q_heads / H) >= (1LL << 30))
-    return fail(MARCHE_ERR_UNSUPPORTED, "too many query rows");
+  if ((int64_t)q_total * n_q_heads >= (1LL << 31))
+    return fail(MARCHE_ERR_UNSUPPORTED, "q_total*n_q_heads reaches 2^31");
   if (q_total == 0) return MARCHE_OK;
   const DType dt = dtype == MARCHE_BF16 ? DType::BF16 : DType::F32;
   PagedAttnArgs a{};
   a.max_pages = max_pages;
   paged_attn_sizes(a, cache, n_seqs, q_total, q_max, n_q_heads, len_max, n_select, dt);
-  if ((int64_t)n_seqs * H * a.row_blocks * a.splits >= (1LL << 31))
+  if (paged_grid(a) >= (1LL << 31))
     return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs*n_heads*rows too large");
   if (!page_table || !lens || !q || !o)
     return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_attention");

@@ -292,6 +292,21 @@ struct PagedSelectArgs {
   int32_t rows_per, p_cap;  // set by the launch: rows per workgroup, keys per row in LDS
 };
 hipError_t launch_paged_select(DType dt, int32_t head_dim, PagedSelectArgs a, hipStream_t s);
+// Division of numbers below 2^31 by a constant known at launch: with s the
+// bits of d - 1 and m = ceil(2^(32 + s) / d) - 2^32 < 2^32,
+// n / d = (n m / 2^32 + n) / 2^s.
+struct FastDiv {
+  uint32_t m, s;
+  static FastDiv of(uint32_t d) {
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    return {(uint32_t)(((1ull << (32 + s)) + d - 1) / d - (1ull << 32)), s};
+  }
+  __host__ __device__ uint32_t div(uint32_t n) const {
+    return (uint32_t)(((((uint64_t)n * m) >> 32) + n) >> s);
+  }
+};
+constexpr int PAGED_MAX_SHARED = 256;  // sequences of a call whose ranges are shared out on the device
 struct PagedAttnArgs {
   const void *k, *v;
   const uint8_t *k_exp, *v_exp;
@@ -306,8 +321,14 @@ struct PagedAttnArgs {
   float sl2;  // log2(e) / sqrt(head_dim)
   // the plan (paged_plan): 16-row tiles and wavefronts per workgroup, row
   // blocks per sequence, key ranges, 32-key tiles per range, rows of a block
-  int32_t row_tiles, waves, row_blocks, splits, chunk, bit_rows;
+  // (with selected pages).  budget > 0: sequences are cut into equal ranges on
+  // the device (Shares), at most `splits` each and `budget` in all, of `chunk`
+  // tiles at least.
+  int32_t row_tiles, waves, row_blocks, splits, chunk, bit_rows, budget;
+  FastDiv d_splits, d_blocks, d_heads, d_group;
 };
+// Workgroups of the attention launch.
+int64_t paged_grid(const PagedAttnArgs &a);
 // Fills the plan from the sizes.
 void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a);
 hipError_t launch_paged_attention(DType dt, int32_t format, int32_t head_dim, const PagedAttnArgs &a,

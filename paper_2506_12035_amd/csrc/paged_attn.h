@@ -75,17 +75,20 @@ struct KvRaw {
                                        const uint8_t *vx, size_t slot, int c, int g) {
     const char *kp = static_cast<const char *>(kb) + slot * (DH * ES);
     const char *vp = static_cast<const char *>(vb) + slot * (DH * ES);
-    const uint32_t ko = c * DH * ES;
+    // (unsigned 32-bit lane offsets: the loads take them beside a scalar base)
+    const uint32_t ko = (uint32_t)(c * DH * ES + 16 * g);
 #pragma unroll
-    for (int m = 0; m < KQ; ++m) k[u][m] = *reinterpret_cast<const u32x4 *>(kp + ko + 64 * m + 16 * g);
+    for (int m = 0; m < KQ; ++m) k[u][m] = *reinterpret_cast<const u32x4 *>(kp + (ko + 64 * m));
     if constexpr (T) {
-      if constexpr (W) kt[u] = *reinterpret_cast<const u32x2 *>(kp + ko + 64 * ES + 8 * g);
-      else kt[u].x = *reinterpret_cast<const uint32_t *>(kp + ko + 64 * ES + 4 * g);
+      const uint32_t to = (uint32_t)(c * DH * ES + 64 * ES + 4 * ES * g);
+      if constexpr (W) kt[u] = *reinterpret_cast<const u32x2 *>(kp + to);
+      else kt[u].x = *reinterpret_cast<const uint32_t *>(kp + to);
     }
-    const uint32_t vo = 4 * g * DH * ES + c * VC * ES;
+    const uint32_t vo = (uint32_t)(4 * g * DH * ES + c * VC * ES);
+    const uint32_t vto = (uint32_t)(4 * g * DH * ES + 64 * ES + c * ES);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const char *p = vp + vo + r * DH * ES;
+      const char *p = vp + (vo + r * DH * ES);
       uint32_t(&x)[VW] = v[4 * u + r];
       if constexpr (VW == 1) {
         x[0] = *reinterpret_cast<const uint32_t *>(p);
@@ -97,15 +100,15 @@ struct KvRaw {
         x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;
       }
       if constexpr (T) {
-        const char *t = vp + 4 * g * DH * ES + r * DH * ES + 64 * ES + c * ES;
+        const char *t = vp + (vto + r * DH * ES);
         if constexpr (W) vt[4 * u + r] = *reinterpret_cast<const uint16_t *>(t);
         else vt[4 * u + r] = *reinterpret_cast<const uint8_t *>(t);
       }
     }
     if constexpr (!W) {
-      if constexpr (FMT == E4) ke[u] = kx[slot + c];
-      else ke[u] = *reinterpret_cast<const uint32_t *>(kx + slot + 4 * g);
-      ve[u] = *reinterpret_cast<const uint32_t *>(vx + slot + 4 * g);
+      if constexpr (FMT == E4) ke[u] = (kx + slot)[(uint32_t)c];
+      else ke[u] = *reinterpret_cast<const uint32_t *>(kx + slot + (uint32_t)(4 * g));
+      ve[u] = *reinterpret_cast<const uint32_t *>(vx + slot + (uint32_t)(4 * g));
     }
   }
   // V of keys n .. 15 of half u becomes zero (they hold nothing, or another
@@ -149,38 +152,37 @@ struct KvRaw {
       return hi16(__float_as_uint(a), __float_as_uint(b));  // at most 8 significant bits: exact
     }
   }
-  // V^T of the eight keys as operands, tile m: channel vchan(m, c).
-  __device__ __forceinline__ void values(bf16x8 (&f)[M]) const {
-    uint32_t o[M][4];
+  // V^T of the eight keys as operands, tiles m and m + 1 (the last one of an
+  // odd count alone): channels vchan(m, c), vchan(m + 1, c).
+  __device__ __forceinline__ void values(int m, bf16x8 &f0, bf16x8 &f1) const {
+    uint32_t o[2][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {  // keys 2 i and 2 i + 1
       const int a = 2 * i, b = a + 1, u = a / 4;
-      if constexpr (FMT == I8) {
+      const float sa = FMT == E4 ? exp_scale((ve[u] >> (8 * (a % 4))) & 0xFFu) : 1.f;
+      const float sb = FMT == E4 ? exp_scale((ve[u] >> (8 * (b % 4))) & 0xFFu) : 1.f;
+      if (T && m == M - 1) {
+        if constexpr (FMT == I8)
+          o[0][i] = hi16(__float_as_uint((float)(int8_t)vt[a]), __float_as_uint((float)(int8_t)vt[b]));
+        else if constexpr (FMT == E4)
+          o[0][i] = lo16(pair(vt[a], sa, 0), pair(vt[b], sb, 0));
+        else
+          o[0][i] = lo16(vt[a], vt[b]);
+      } else if constexpr (FMT == I8) {
 #pragma unroll
-        for (int m = 0; m < VC; ++m)
-          o[m][i] = hi16(__float_as_uint((float)(int8_t)(v[a][m / 4] >> (8 * (m % 4)))),
-                         __float_as_uint((float)(int8_t)(v[b][m / 4] >> (8 * (m % 4)))));
-        if constexpr (T)
-          o[4][i] = hi16(__float_as_uint((float)(int8_t)vt[a]), __float_as_uint((float)(int8_t)vt[b]));
+        for (int e = 0; e < 2; ++e)
+          o[e][i] = hi16(__float_as_uint((float)(int8_t)(v[a][m / 4] >> (8 * (m % 4 + e)))),
+                         __float_as_uint((float)(int8_t)(v[b][m / 4] >> (8 * (m % 4 + e)))));
       } else {
-        const float sa = FMT == E4 ? exp_scale((ve[u] >> (8 * (a % 4))) & 0xFFu) : 1.f;
-        const float sb = FMT == E4 ? exp_scale((ve[u] >> (8 * (b % 4))) & 0xFFu) : 1.f;
-#pragma unroll
-        for (int p = 0; p < VC / 2; ++p) {
-          uint32_t x, y;
-          if constexpr (FMT == E4) x = pair(v[a][p / 2], sa, p % 2), y = pair(v[b][p / 2], sb, p % 2);
-          else x = v[a][p], y = v[b][p];
-          o[2 * p][i] = lo16(x, y);
-          o[2 * p + 1][i] = hi16(x, y);
-        }
-        if constexpr (T) {
-          if constexpr (FMT == E4) o[4][i] = lo16(pair(vt[a], sa, 0), pair(vt[b], sb, 0));
-          else o[4][i] = lo16(vt[a], vt[b]);
-        }
+        uint32_t x, y;
+        if constexpr (FMT == E4) x = pair(v[a][m / 4], sa, m / 2 % 2), y = pair(v[b][m / 4], sb, m / 2 % 2);
+        else x = v[a][m / 2], y = v[b][m / 2];
+        o[0][i] = lo16(x, y);
+        o[1][i] = hi16(x, y);
       }
     }
-#pragma unroll
-    for (int m = 0; m < M; ++m) f[m] = __builtin_bit_cast(bf16x8, u32x4{o[m][0], o[m][1], o[m][2], o[m][3]});
+    f0 = __builtin_bit_cast(bf16x8, u32x4{o[0][0], o[0][1], o[0][2], o[0][3]});
+    if (!(T && m == M - 1)) f1 = __builtin_bit_cast(bf16x8, u32x4{o[1][0], o[1][1], o[1][2], o[1][3]});
   }
   // first channel of product n's eight in lane group g
   static __device__ __forceinline__ int chan(int n, int g) {
@@ -203,51 +205,133 @@ __device__ __forceinline__ void split(float x, bf16 (&o)[T]) {
   }
 }
 
+// Attention of a block's packed rows [p0, p1) over the pages that each of them
+// looks at, a wavefront per row, 16 keys at a time (lanes 0 .. 15 a key each):
+// the plain loop, for blocks that hold values that are not finite.
+template <int FMT, int DH, typename RowT>
+__device__ __forceinline__ void one_by_one(const PagedAttnArgs &a, const int32_t *tab, const uint32_t *s_bits,
+                                           const uint16_t *s_list, int words, int p0, int p1, int i0, int row0, int h,
+                                           int split_i, int len, int end, int wave, int waves, int lane) {
+  const int page = 1 << a.page_log2;
+  auto at = [&](const void *x, const uint8_t *ex, size_t slot, int d) {
+    if constexpr (FMT == BF) return (float)static_cast<const bf16 *>(x)[slot * DH + d];
+    const uint32_t q = static_cast<const uint8_t *>(x)[slot * DH + d];
+    const float s = exp_scale(ex[slot]);
+    return FMT == E4 ? __builtin_amdgcn_cvt_f32_fp8((int)q, 0) * s : (float)(int8_t)q * s;
+  };
+  for (int pr = p0 + wave; pr < p1; pr += waves) {
+    const int i = (int)a.d_group.div(pr), hg = pr - i * a.group;
+    const RowT *q = static_cast<const RowT *>(a.q) + (size_t)(row0 + i) * a.q_stride + (size_t)(h * a.group + hg) * DH;
+    float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};
+    bool seen = false;
+#pragma unroll 1
+    for (int pos = 32 * split_i * a.chunk; pos < end; pos += 16) {
+      const int lp = s_list[pos >> a.page_log2];
+      if (!((s_bits[(i - i0) * words + (lp >> 5)] >> (lp & 31)) & 1u)) continue;
+      const int phys = tab[lp];
+      const int n = min(len - (lp << a.page_log2) - (pos & (page - 1)), 16);
+      if ((unsigned)phys >= (unsigned)a.n_pages || n <= 0) continue;
+      const size_t slot = (((size_t)phys * a.n_heads + h) << a.page_log2) + (pos & (page - 1));
+      seen = true;
+      float s = 0.f;
+      if (lane < n) {
+#pragma unroll 1
+        for (int d = 0; d < DH; ++d) s = fmaf(to_f32(q[d]), at(a.k, a.k_exp, slot + lane, d), s);
+        s *= a.sl2;
+      }
+      const float m_new = fmaxf(m, wave_max(lane < n ? s : -INFINITY));
+      const float al = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      const float p = lane < n ? __builtin_amdgcn_exp2f(s - (m_new == -INFINITY ? 0.f : m_new)) : 0.f;
+      m = m_new;
+      l = l * al + wave_sum(p);
+      acc[0] *= al;
+      acc[1] *= al;
+#pragma unroll 1
+      for (int r = 0; r < n; ++r) {
+        const float w = __shfl(p, r, 64);
+        acc[0] = fmaf(w, at(a.v, a.v_exp, slot + r, lane), acc[0]);
+        if (lane + 64 < DH) acc[1] = fmaf(w, at(a.v, a.v_exp, slot + r, lane + 64), acc[1]);
+      }
+    }
+    const size_t row = (size_t)(row0 + i) * (a.n_heads * a.group) + h * a.group + hg;
+    const size_t part = (size_t)split_i * a.q_total * (a.n_heads * a.group) + row;
+    const float inv = a.splits > 1 ? 1.f : seen ? 1.f / l : 0.f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int d = lane + 64 * j;
+      if (d >= DH) break;
+      if (a.splits > 1) a.part_o[part * DH + d] = acc[j];
+      else static_cast<RowT *>(a.o)[row * DH + d] = (RowT)(acc[j] * inv);
+    }
+    if (a.splits > 1 && lane == 0) {
+      a.part_ml[2 * part] = m;
+      a.part_ml[2 * part + 1] = seen ? l : -1.f;
+    }
+  }
+}
+
 template <int FMT, int DH, int RT, typename RowT, bool SEL>
 __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAttnArgs a,
                                                                          const int32_t *__restrict__ table) {
   using Raw = KvRaw<FMT, DH>;
   constexpr int TERMS = sizeof(RowT) == 4 ? 3 : 1;
   constexpr int NC = Raw::NC, M = Raw::M;
-  constexpr int OS = DH + 4;  // row stride of the joined parts
+  constexpr int OS = DH + 4;              // row stride of the joined parts
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g = lane >> 4;
 
-  // (sequence, key head, row block, key range), ranges and blocks of one
-  // sequence and head side by side on one XCD
-  int at = xcd_remap(blockIdx.x, gridDim.x);
-  const int split_i = at % a.splits;
-  at /= a.splits;
-  const int rb = at % a.row_blocks;
-  at /= a.row_blocks;
-  const int h = at % a.n_heads, b = at / a.n_heads;
-
-  int row0, n_rows;  // the sequence's rows
-  if (a.q_off) {
-    row0 = min(max(a.q_off[b], 0), a.q_total);
-    n_rows = min(max(a.q_off[b + 1], row0), a.q_total) - row0;
-  } else {
-    row0 = b * a.rows_each;
-    n_rows = a.rows_each;
+  // (sequence, key head, row block, key range): consecutive workgroup ids go
+  // round the 8 XCDs, so (sequence, head) pairs are dealt to them one by one
+  // and the blocks and ranges of a pair follow each other on its XCD, whose L2
+  // they share.  (Contiguous sequences per XCD leave most XCDs idle at the end
+  // where sequences differ.)
+  const int at0 = blockIdx.x >> 3;
+  const int at1 = a.d_splits.div(at0);
+  const int at2 = a.d_blocks.div(at1), rb = at1 - at2 * a.row_blocks;
+  const int pair = 8 * at2 + (blockIdx.x & 7);
+  int split_i = at0 - at1 * a.splits, chunk = a.chunk;
+  int b = a.d_heads.div(pair);
+  const int h = pair - b * a.n_heads;
+  if (!SEL && a.budget > 0) {
+    if (b >= a.budget) return;
+    const Shares sh(a, lane);
+    chunk = sh.chunk;
+    b = __builtin_amdgcn_readfirstlane(sh.find(b, lane, split_i));
+    if (b < 0) return;
+  } else if (b >= a.n_seqs) {
+    return;
   }
-  const int packed = min(n_rows, a.q_max) * a.group;
-  const int p0 = rb * 16 * RT;
-  if (p0 >= packed) return;
-  const int n_rt = min(RT, (packed - p0 + 15) >> 4);
-  const int len = min(paged_len(a.lens[b], a.max_pages, a.page_log2), a.len_max);
+
+  // The lists' entries that a workgroup starts from are loaded together: the
+  // length, the rows and the page of its first tile (where that lies if the
+  // sequence is long enough).
   const int page = 1 << a.page_log2;
   const int32_t *tab = table + (size_t)b * a.max_pages;
+  const int first = split_i * chunk + wave;
+  const int ahead = SEL ? 0 : tab[min((32 * first) >> a.page_log2, a.max_pages - 1)];
+  const int len = min(paged_len(a.lens[b], a.max_pages, a.page_log2), a.len_max);
+  int row0 = b * a.rows_each, row1 = row0 + a.rows_each;  // the sequence's rows
+  if (a.q_off) {
+    row0 = min(max(a.q_off[b], 0), a.q_total);
+    row1 = min(max(a.q_off[b + 1], row0), a.q_total);
+  }
+  const int packed = min(row1 - row0, a.q_max) * a.group;
+  const int p0 = rb * 16 * RT;
+  if (p0 >= packed) return;
 
-  // LDS: joined O parts, maxima and sums of every wavefront, then the page
-  // bits of the block's rows and the list of pages that any of them looks at
-  float *s_o = reinterpret_cast<float *>(smem);             // [waves][16][OS]
-  float *s_m = s_o + waves * 16 * OS;                       // [waves][RT*16]
-  float *s_l = s_m + waves * RT * 16;                       // [waves][RT*16]
-  uint32_t *s_bits = reinterpret_cast<uint32_t *>(s_l + waves * RT * 16);
+  // LDS: joined O parts, maxima and sums of every wavefront and the rows'
+  // places in the output (several wavefronts only), then the page bits of the
+  // block's rows and the list of pages that any of them looks at
+  float *s_o = reinterpret_cast<float *>(smem);             // [waves][RT*16][OS]
+  float *s_m = s_o + (waves > 1 ? waves * RT * 16 * OS : 0);  // [waves][RT*16]
+  float *s_l = s_m + (waves > 1 ? waves * RT * 16 : 0);       // [waves][RT*16]
+  int *s_row = reinterpret_cast<int *>(s_l + (waves > 1 ? waves * RT * 16 : 0));  // [RT*16]
+  uint32_t *s_bits = reinterpret_cast<uint32_t *>(s_row + (waves > 1 ? RT * 16 : 0));
   const int words = (a.max_pages + 31) >> 5;
-  const int i0 = p0 / a.group, i1 = (min(p0 + 16 * RT, packed) - 1) / a.group;  // the block's rows
+  auto row_of = [&](int p) { return (int)a.d_group.div(p); };  // a packed row's row
+  const int i0 = row_of(p0), i1 = row_of(min(p0 + 16 * RT, packed) - 1);  // the block's rows
   uint32_t *s_any = s_bits + (SEL ? a.bit_rows * words : 0);
   uint16_t *s_list = reinterpret_cast<uint16_t *>(s_any + words);
   int n_list = 0;
@@ -288,27 +372,31 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   }
   n_list = __builtin_amdgcn_readfirstlane(n_list);
   const int n_keys = SEL ? n_list << a.page_log2 : len;  // positions the block walks through
-  const int t0 = min(split_i * a.chunk, (n_keys + 31) >> 5), t1 = min(t0 + a.chunk, (n_keys + 31) >> 5);
+  const int t1 = min((split_i + 1) * chunk, (n_keys + 31) >> 5);  // the range's last tile
 
-  // queries: lane (c, g) holds row c of each tile
+  // queries: lane (c, g) holds row c of each tile (columns behind the last row
+  // repeat the block's first: computed and never stored)
   bf16x8 qf[RT][TERMS][NC];
-  int bit_at[RT];  // the row's page bits
+  int loc[RT];  // the row within the block
+  int out[RT];  // and its (row, query head) in the output, or -1
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int pr = p0 + rt * 16 + c;
     const bool on = pr < packed;
-    const int i = on ? pr / a.group : i0, hg = on ? pr - i * a.group : 0;
+    const int i = on ? row_of(pr) : i0, hg = on ? pr - i * a.group : 0;
+    loc[rt] = i - i0;
+    out[rt] = on ? (row0 + i) * (a.n_heads * a.group) + h * a.group + hg : -1;
     const RowT *q = static_cast<const RowT *>(a.q) + (size_t)(row0 + i) * a.q_stride +
                     (size_t)(h * a.group + hg) * DH;
-    bit_at[rt] = (i - i0) * words;
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
       float x[8];
+      if (Raw::T && n == NC - 1) {
+        load4(q + Raw::chan(n, g), x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = 0.f;
-      if (on) {
-        if (Raw::T && n == NC - 1) load4(q + Raw::chan(n, g), x);
-        else load8(q + Raw::chan(n, g), x);
+        for (int e = 4; e < 8; ++e) x[e] = 0.f;
+      } else {
+        load8(q + Raw::chan(n, g), x);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -320,28 +408,35 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
     }
   }
 
-  // Where a tile's halves lie: first slot in the pool, how many of the 16
-  // tokens exist, and (selected pages) the logical page.
-  struct Half {
-    size_t slot;
-    int n, lp;
+  // Where the halves of a 32-key tile lie: first slots in the pool, how many of
+  // the 16 tokens exist, and (selected pages) the logical pages.  All uniform.
+  struct Tile {
+    size_t slot[2];
+    int n[2], lp[2];
   };
-  auto half = [&](int pos, int only) {
-    Half x;
-    int lp = pos >> a.page_log2, key = pos;
-    bool ok = pos < n_keys;
-    if constexpr (SEL) {
-      lp = __builtin_amdgcn_readfirstlane((int)s_list[ok ? lp : 0]);
-      if (!ok) lp = 0;
-      key = (lp << a.page_log2) + (pos & (page - 1));
-      if (only >= 0) ok = ok && ((s_bits[only * words + (lp >> 5)] >> (lp & 31)) & 1u);
+  auto place = [&](int t, bool start) {
+    Tile x;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int pos = 32 * t + 16 * u;
+      if (u == 1 && a.page_log2 > 4) {  // the same page
+        x.lp[1] = x.lp[0];
+        x.slot[1] = x.slot[0] + 16;
+        x.n[1] = x.n[0] < 16 ? 0 : min(max(len - (SEL ? (x.lp[0] << a.page_log2) + (pos & (page - 1)) : pos), 0), 16);
+        break;
+      }
+      bool ok = pos < n_keys;
+      int lp = ok ? pos >> a.page_log2 : 0, key = pos;
+      if constexpr (SEL) {
+        lp = __builtin_amdgcn_readfirstlane((int)s_list[lp]);
+        key = (lp << a.page_log2) + (pos & (page - 1));
+      }
+      const int phys = !ok ? 0 : !SEL && start && u == 0 ? ahead : tab[lp];
+      ok = ok && (unsigned)phys < (unsigned)a.n_pages;
+      x.n[u] = ok ? min(max(len - key, 0), 16) : 0;
+      x.slot[u] = (((size_t)(ok ? phys : 0) * a.n_heads + h) << a.page_log2) + (pos & (page - 1));
+      x.lp[u] = lp;
     }
-    const int phys = ok ? tab[lp] : 0;
-    ok = ok && (unsigned)phys < (unsigned)a.n_pages;
-    x.n = __builtin_amdgcn_readfirstlane(ok ? min(max(len - key, 0), 16) : 0);
-    const int ph = __builtin_amdgcn_readfirstlane(ok ? phys : 0);
-    x.slot = (((size_t)ph * a.n_heads + h) << a.page_log2) + (pos & (page - 1));
-    x.lp = lp;
     return x;
   };
 
@@ -349,9 +444,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   float m_run[RT], l_run[RT];
   bool seen[RT];
 
-  // every row at once (only < 0), or, where that met values that are not
-  // finite, row `only` over its own pages
-  auto pass = [&](int only) {
+  auto pass = [&]() {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       m_run[rt] = -INFINITY;
@@ -360,190 +453,229 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
 #pragma unroll
       for (int m = 0; m < M; ++m) acc[rt][m] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    int t = t0 + wave;
+    int t = first;
     if (t >= t1) return;
     Raw raw;
-    Half x0 = half(32 * t, only), x1 = half(32 * t + 16, only);
-    raw.load(0, a.k, a.v, a.k_exp, a.v_exp, x0.slot, c, g);
-    raw.load(1, a.k, a.v, a.k_exp, a.v_exp, x1.slot, c, g);
-    Half y0 = x0, y1 = x1;
-    if (t + waves < t1) y0 = half(32 * (t + waves), only), y1 = half(32 * (t + waves) + 16, only);
+    Tile x = place(t, true);
+    raw.load(0, a.k, a.v, a.k_exp, a.v_exp, x.slot[0], c, g);
+    raw.load(1, a.k, a.v, a.k_exp, a.v_exp, x.slot[1], c, g);
+    Tile y = t + waves < t1 ? place(t + waves, false) : x;
     while (true) {
       // the next tile's loads, and the page ids of the one after it
       const bool more = t + waves < t1;
       Raw next;
-      Half z0 = y0, z1 = y1;
+      Tile z = y;
       if (more) {
-        next.load(0, a.k, a.v, a.k_exp, a.v_exp, y0.slot, c, g);
-        next.load(1, a.k, a.v, a.k_exp, a.v_exp, y1.slot, c, g);
-        if (t + 2 * waves < t1)
-          z0 = half(32 * (t + 2 * waves), only), z1 = half(32 * (t + 2 * waves) + 16, only);
+        next.load(0, a.k, a.v, a.k_exp, a.v_exp, y.slot[0], c, g);
+        next.load(1, a.k, a.v, a.k_exp, a.v_exp, y.slot[1], c, g);
+        if (t + 2 * waves < t1) z = place(t + 2 * waves, false);
       }
-      const int nv[2] = {x0.n, x1.n}, lp[2] = {x0.lp, x1.lp};
-      const bool part = nv[0] + nv[1] < 32;
+      const bool part = x.n[0] + x.n[1] < 32;
       if (part) {
-        raw.clear(0, nv[0], g);
-        raw.clear(1, nv[1], g);
+        raw.clear(0, x.n[0], g);
+        raw.clear(1, x.n[1], g);
       }
-      if (nv[0] + nv[1] > 0) {
-        bf16x8 kf[2][NC], vf[M];
-        raw.keys(0, kf[0]);
-        raw.keys(1, kf[1]);
-        raw.values(vf);
-        float ks[2][4], vs[2][4];
-        if constexpr (FMT == I8) {
+      // Every step runs over all row tiles before the next begins: their chains
+      // of dependent instructions overlap (a lone chain leaves most issue
+      // slots empty).
+      f32x4 s[RT][2];
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u) {
+        bf16x8 kf[NC];
+        raw.keys(u, kf);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              ks[u][r] = exp_scale((raw.ke[u] >> (8 * r)) & 0xFFu) * a.sl2;
-              vs[u][r] = exp_scale((raw.ve[u] >> (8 * r)) & 0xFFu);
+        for (int rt = 0; rt < RT; ++rt) s[rt][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = TERMS - 1; e >= 0; --e)
+#pragma unroll
+          for (int n = 0; n < NC; ++n)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+              s[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[n], qf[rt][e][n], s[rt][u], 0, 0, 0);
+      }
+      if constexpr (FMT == I8) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float sc = exp_scale((raw.ke[u] >> (8 * r)) & 0xFFu);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) s[rt][u][r] *= sc;
+          }
+      }
+      if (part) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (4 * g + r >= x.n[u]) {
+#pragma unroll
+              for (int rt = 0; rt < RT; ++rt) s[rt][u][r] = -INFINITY;
             }
+      }
+      float mx[RT];
+      bool raise = false;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        mx[rt] = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          bool look = true;
+          if constexpr (SEL) look = (s_bits[loc[rt] * words + (x.lp[u] >> 5)] >> (x.lp[u] & 31)) & 1u;
+          seen[rt] |= look && x.n[u] > 0;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if (SEL && !look) s[rt][u][r] = -INFINITY;
+            mx[rt] = fmaxf(mx[rt], s[rt][u][r]);
+          }
         }
+        raise |= mx[rt] * a.sl2 > m_run[rt] + 8.f;
+      }
+      if (__any(raise)) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          if (rt >= n_rt) break;
-          float s[2][4];
-          float mx = -INFINITY;
+          const float m_new = fmaxf(m_run[rt], quad_max(mx[rt]) * a.sl2);
+          const float al = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[rt] - m_new);
+          m_run[rt] = m_new;
+          l_run[rt] *= al;
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            f32x4 d = {0.f, 0.f, 0.f, 0.f};
+          for (int m = 0; m < M; ++m) acc[rt][m] *= al;
+        }
+      }
+      bf16x8 pb[RT][TERMS];
 #pragma unroll
-            for (int e = TERMS - 1; e >= 0; --e)
+      for (int rt = 0; rt < RT; ++rt) {
+        const float mm = m_run[rt] == -INFINITY ? 0.f : -m_run[rt];
+        float sum[2];
 #pragma unroll
-              for (int n = 0; n < NC; ++n)
-                d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[u][n], qf[rt][e][n], d, 0, 0, 0);
-            bool look = true;
-            if constexpr (SEL) {
-              look = (s_bits[bit_at[rt] + (lp[u] >> 5)] >> (lp[u] & 31)) & 1u;
-              seen[rt] |= look && nv[u] > 0;
-            } else {
-              seen[rt] = true;
-            }
+        for (int u = 0; u < 2; ++u) {
+          float p[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              s[u][r] = d[r] * (FMT == I8 ? ks[u][r] : a.sl2);
-              if (SEL ? !look : false) s[u][r] = -INFINITY;
-              if (part && 4 * g + r >= nv[u]) s[u][r] = -INFINITY;
-              mx = fmaxf(mx, s[u][r]);
-            }
+          for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[rt][u][r], a.sl2, mm));
+          sum[u] = (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if constexpr (FMT == I8) p[r] *= exp_scale((raw.ve[u] >> (8 * r)) & 0xFFu);
+            bf16 q[TERMS];
+            split<TERMS>(p[r], q);
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e) pb[rt][e][4 * u + r] = q[e];
           }
-          if (__any(mx > m_run[rt] + 8.f)) {
-            const float m_new = fmaxf(m_run[rt], quad_max(mx));
-            const float al = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[rt] - m_new);
-            m_run[rt] = m_new;
-            l_run[rt] *= al;
+        }
+        l_run[rt] += sum[0] + sum[1];
+      }
 #pragma unroll
-            for (int m = 0; m < M; ++m) acc[rt][m] *= al;
-          }
-          const float mm = m_run[rt] == -INFINITY ? 0.f : m_run[rt];
-          bf16x8 pb[TERMS];
+      for (int m = 0; m < M; m += 2) {
+        bf16x8 vf[2];
+        raw.values(m, vf[0], vf[1]);
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              float p = __builtin_amdgcn_exp2f(s[u][r] - mm);
-              l_run[rt] += p;
-              if constexpr (FMT == I8) p *= vs[u][r];
-              bf16 y[TERMS];
-              split<TERMS>(p, y);
-#pragma unroll
-              for (int e = 0; e < TERMS; ++e) pb[e][4 * u + r] = y[e];
-            }
+        for (int j = 0; j < 2; ++j) {
+          if (m + j == M) break;
 #pragma unroll
           for (int e = TERMS - 1; e >= 0; --e)
 #pragma unroll
-            for (int m = 0; m < M; ++m)
-              acc[rt][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[m], pb[e], acc[rt][m], 0, 0, 0);
+            for (int rt = 0; rt < RT; ++rt)
+              acc[rt][m + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j], pb[rt][e], acc[rt][m + j], 0, 0, 0);
         }
       }
       if (!more) break;
       t += waves;
       raw = next;
-      x0 = y0, x1 = y1;
-      y0 = z0, y1 = z1;
+      x = y;
+      y = z;
     }
   };
 
-  // Joins the wavefronts' parts and writes them; `only`: that row alone.
-  // l = -1 stands for "no key at all" (the row gets zeros; a sum of 0 over
-  // keys that all have logit -inf gives 0 / 0).
-  auto join = [&](int only) {
+  // Four channels from d on of tile rt's row c, for every such group of the lane.
+  auto groups = [&](int rt, auto f) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int m = 0; m < Raw::VC; m += 4)
+        f(Raw::VC * (4 * g + r) + m, f32x4{acc[rt][m][r], acc[rt][m + 1][r], acc[rt][m + 2][r], acc[rt][m + 3][r]});
+    if constexpr (Raw::T) f(64 + 4 * g, acc[rt][M - 1]);
+  };
+  auto store = [&](int row, int d, f32x4 v) {
+    if (a.splits > 1) {
+      const size_t part = (size_t)split_i * a.q_total * (a.n_heads * a.group) + row;
+      *reinterpret_cast<f32x4 *>(a.part_o + part * DH + d) = v;
+    } else if constexpr (sizeof(RowT) == 4) {
+      *reinterpret_cast<f32x4 *>(static_cast<float *>(a.o) + (size_t)row * DH + d) = v;
+    } else {
+      *reinterpret_cast<bf16x4 *>(static_cast<bf16 *>(a.o) + (size_t)row * DH + d) =
+          bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+    }
+  };
+
+  // Joins the wavefronts' parts and writes them.  l = -1 stands for "no key at
+  // all" (the row gets zeros; a sum of 0 over keys that all have logit -inf
+  // gives 0 / 0).
+  auto join = [&]() {
+    float scale[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      float l = l_run[rt];
-      l += __shfl_xor(l, 16, 64);
-      l += __shfl_xor(l, 32, 64);
-      if (g == 0) {
+      l_run[rt] += __shfl_xor(l_run[rt], 16, 64);
+      l_run[rt] += __shfl_xor(l_run[rt], 32, 64);
+      if (waves > 1 && g == 0) {
         s_m[wave * RT * 16 + rt * 16 + c] = m_run[rt];
-        s_l[wave * RT * 16 + rt * 16 + c] = seen[rt] ? l : -1.f;
+        s_l[wave * RT * 16 + rt * 16 + c] = seen[rt] ? l_run[rt] : -1.f;
+        if (wave == 0) s_row[rt * 16 + c] = out[rt];
       }
     }
-    __syncthreads();
+    if (waves > 1) __syncthreads();
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      if (rt >= n_rt) break;
-      const int col = rt * 16 + c;
-      float m = -INFINITY;
-      for (int w = 0; w < waves; ++w) m = fmaxf(m, s_m[w * RT * 16 + col]);
-      const float al = m_run[rt] == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(m_run[rt] - m);
-      float *o = s_o + (wave * 16 + c) * OS;
-#pragma unroll
-      for (int m4 = 0; m4 < M; ++m4)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) o[Raw::vchan(m4, 4 * g + r)] = acc[rt][m4][r] * al;
-      __syncthreads();
-      for (int x = tid; x < 16 * (DH / 4); x += blockDim.x) {
-        const int cc = x / (DH / 4), d = (x - cc * (DH / 4)) * 4, cl = rt * 16 + cc;
-        const int pr = p0 + cl;
-        if (pr >= packed) continue;
-        const int i = pr / a.group, hg = pr - i * a.group;
-        if (only >= 0 && i != only) continue;
-        float mt = -INFINITY;
-        for (int w = 0; w < waves; ++w) mt = fmaxf(mt, s_m[w * RT * 16 + cl]);
-        float l = 0.f;
-        bool any = false;
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+      float m = m_run[rt], l = l_run[rt];
+      bool any = seen[rt];
+      scale[rt] = 1.f;
+      if (waves > 1) {
+        m = -INFINITY;
+        for (int w = 0; w < waves; ++w) m = fmaxf(m, s_m[w * RT * 16 + rt * 16 + c]);
+        l = 0.f;
+        any = false;
         for (int w = 0; w < waves; ++w) {
-          const float lw = s_l[w * RT * 16 + cl], mw = s_m[w * RT * 16 + cl];
+          const float lw = s_l[w * RT * 16 + rt * 16 + c], mw = s_m[w * RT * 16 + rt * 16 + c];
           if (lw == -1.f) continue;
           any = true;
-          l += lw * (mw == -INFINITY ? (mt == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(mw - mt));
-          sum += *reinterpret_cast<const f32x4 *>(s_o + (w * 16 + cc) * OS + d);
+          l += lw * (mw == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(mw - m));
         }
-        const size_t row = (size_t)(row0 + i) * (a.n_heads * a.group) + h * a.group + hg;
-        if (a.splits > 1) {
-          const size_t part = (size_t)split_i * a.q_total * (a.n_heads * a.group) + row;
-          *reinterpret_cast<f32x4 *>(a.part_o + part * DH + d) = sum;
-          if (d == 0) {
-            a.part_ml[2 * part] = mt;
-            a.part_ml[2 * part + 1] = any ? l : -1.f;
-          }
-        } else {
-          const float inv = any ? 1.f / l : 0.f;
-          RowT *out = static_cast<RowT *>(a.o) + row * DH + d;
-          if constexpr (sizeof(RowT) == 4) {
-            f32x4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = any ? sum[e] * inv : 0.f;
-            *reinterpret_cast<f32x4 *>(out) = y;
-          } else {
-            bf16x4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = (bf16)(any ? sum[e] * inv : 0.f);
-            *reinterpret_cast<bf16x4 *>(out) = y;
-          }
-        }
+        scale[rt] = m_run[rt] == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(m_run[rt] - m);
       }
-      __syncthreads();
+      if (a.splits == 1) {
+        scale[rt] *= any ? 1.f / l : 0.f;
+      } else if (wave == 0 && g == 0 && out[rt] >= 0) {
+        const size_t part = (size_t)split_i * a.q_total * (a.n_heads * a.group) + out[rt];
+        a.part_ml[2 * part] = m;
+        a.part_ml[2 * part + 1] = any ? l : -1.f;
+      }
+    }
+    if (waves == 1) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+        if (out[rt] >= 0) groups(rt, [&](int d, f32x4 v) { store(out[rt], d, v * scale[rt]); });
+      return;
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float *o = s_o + ((wave * RT + rt) * 16 + c) * OS;
+      groups(rt, [&](int d, f32x4 v) { *reinterpret_cast<f32x4 *>(o + d) = v * scale[rt]; });
+    }
+    __syncthreads();
+    for (int x = tid; x < RT * 16 * (DH / 4); x += blockDim.x) {
+      const int col = x / (DH / 4), d = (x - col * (DH / 4)) * 4;
+      const int row = s_row[col];
+      if (row < 0) continue;
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < waves; ++w) sum += *reinterpret_cast<const f32x4 *>(s_o + (w * RT * 16 + col) * OS + d);
+      store(row, d, sum);
     }
   };
 
-  pass(-1);
+  pass();
   if constexpr (SEL) {
     // A weight of zero times an infinite or NaN value of a page that only
-    // another row looks at would be NaN: rows of a block in which anything is
-    // not finite are computed again, each over its own pages alone.
+    // another row looks at is NaN: a block in which anything is not finite is
+    // computed again, row by row over each row's own pages.
     bool bad = false;
     if (i1 > i0) {
 #pragma unroll
@@ -554,21 +686,19 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
           for (int r = 0; r < 4; ++r) bad |= !(fabsf(acc[rt][m][r]) < INFINITY);
     }
     if (__syncthreads_or(bad)) {
-      for (int i = i0; i <= i1; ++i) {
-        pass(i - i0);
-        join(i);
-      }
+      one_by_one<FMT, DH, RowT>(a, tab, s_bits, s_list, words, p0, min(p0 + 16 * RT, packed), i0, row0, h, split_i,
+                                len, min(32 * t1, n_keys), wave, waves, lane);
       return;
     }
   }
-  join(-1);
+  join();
 }
 
 template <int FMT, int DH, int RT, typename RowT, bool SEL>
 hipError_t launch_paged_attn(const PagedAttnArgs &a, hipStream_t s) {
   constexpr int OS = DH + 4;
   const int words = (a.max_pages + 31) / 32;
-  size_t lds = (size_t)a.waves * (16 * OS + 2 * RT * 16) * 4;
+  size_t lds = a.waves > 1 ? ((size_t)a.waves * (RT * 16 * OS + 2 * RT * 16) + RT * 16) * 4 : 0;
   if (SEL) lds += ((size_t)(a.bit_rows + 1) * words) * 4 + (size_t)words * 64;
   auto kernel = paged_attn_kernel<FMT, DH, RT, RowT, SEL>;
   if (lds > 65536) {
@@ -576,19 +706,16 @@ hipError_t launch_paged_attn(const PagedAttnArgs &a, hipStream_t s) {
                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  const int64_t grid = (int64_t)a.n_seqs * a.n_heads * a.row_blocks * a.splits;
+  const int64_t grid = paged_grid(a);
   launch_kernel(kernel, dim3((unsigned)grid), dim3(64 * a.waves), (uint32_t)lds, s, a, a.table);
   return hipGetLastError();
 }
 
 template <int FMT, int DH, typename RowT, bool SEL>
 hipError_t launch_paged_rt(const PagedAttnArgs &a, hipStream_t s) {
-  switch (a.row_tiles) {
-    case 1: return launch_paged_attn<FMT, DH, 1, RowT, SEL>(a, s);
-    case 2: return launch_paged_attn<FMT, DH, 2, RowT, SEL>(a, s);
-    case 4:
-      if constexpr (sizeof(RowT) == 2) return launch_paged_attn<FMT, DH, 4, RowT, SEL>(a, s);
-  }
+  if (a.row_tiles == 1) return launch_paged_attn<FMT, DH, 1, RowT, SEL>(a, s);
+  if constexpr (sizeof(RowT) == 2)
+    if (a.row_tiles == 2) return launch_paged_attn<FMT, DH, 2, RowT, SEL>(a, s);
   return hipErrorInvalidValue;
 }
 

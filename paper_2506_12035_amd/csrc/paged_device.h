@@ -98,4 +98,59 @@ __device__ __forceinline__ int wave_find_seq(const int32_t *off, int n_seqs, int
   return lo;
 }
 
+// ------------------------------------------------------------------ shares of long caches
+
+// Sequences of different lengths are cut into ranges of one length, `chunk`
+// 32-key tiles, so that `budget` ranges or fewer cover all of them: with total
+// the sum of the sequences' tiles, ceil(total / (budget - n_seqs)) is enough, as each
+// sequence adds less than one range to total / chunk.  At most 64 ranges a
+// sequence.  One wavefront per call; n_seqs <= PAGED_MAX_SHARED.
+struct Shares {
+  int chunk;
+  int tiles[PAGED_MAX_SHARED / 64];  // of sequence 64 k + lane
+  __device__ __forceinline__ Shares(const PagedAttnArgs &a, int lane) {
+    int sum = 0, most = 0;
+#pragma unroll
+    for (int k = 0; k < PAGED_MAX_SHARED / 64; ++k) {
+      const int b = 64 * k + lane;
+      const int len = b < a.n_seqs ? min(paged_len(a.lens[b], a.max_pages, a.page_log2), a.len_max) : 0;
+      tiles[k] = (len + 31) >> 5;
+      sum += tiles[k];
+      most = max(most, tiles[k]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      sum += __shfl_xor(sum, o, 64);
+      most = max(most, __shfl_xor(most, o, 64));
+    }
+    const int room = a.budget - a.n_seqs;
+    chunk = max(max((sum + room - 1) / room, (most + 63) >> 6), a.chunk);
+    chunk = __builtin_amdgcn_readfirstlane(chunk);
+  }
+  __device__ __forceinline__ int ranges(int n) const { return (int)((uint32_t)(n + chunk - 1) / (uint32_t)chunk); }
+  // Range x of all: its sequence (-1: there are fewer) and place in it.
+  __device__ __forceinline__ int find(int x, int lane, int &part) const {
+    int before = 0;
+#pragma unroll
+    for (int k = 0; k < PAGED_MAX_SHARED / 64; ++k) {
+      const int n = ranges(tiles[k]);
+      int end = n;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(end, o, 64);
+        if (lane >= o) end += y;
+      }
+      end += before;
+      const unsigned long long past = __ballot(end > x);
+      if (past) {
+        const int l = __ffsll((long long)past) - 1;
+        part = __builtin_amdgcn_readfirstlane(x - __shfl(end - n, l, 64));
+        return 64 * k + l;
+      }
+      before = __shfl(end, 63, 64);
+    }
+    return -1;
+  }
+};
+
 }  // namespace marche
