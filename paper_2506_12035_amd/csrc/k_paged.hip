@@ -270,6 +270,23 @@ __device__ __forceinline__ uint32_t score_key(float f) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
+// Largest over the wavefront, uniform (lane exchanges inside 16 lanes as DPP
+// modifiers, then row swaps: no LDS crossbar).
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = dpp_max<0xB1>(v);   // quad_perm [1,0,3,2]
+  v = dpp_max<0x4E>(v);   // quad_perm [2,3,0,1]
+  v = dpp_max<0x141>(v);  // row_half_mirror
+  v = dpp_max<0x140>(v);  // row_mirror
+  auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(p[0], p[1]);
+  auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __builtin_amdgcn_readfirstlane(max(q[0], q[1]));
+}
+
 // Four int8 numbers from floats whose low bytes hold them.
 __device__ __forceinline__ int pack_low(float a, float b, float c, float d) {
   const uint32_t x = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x0C0C0400u);
@@ -294,68 +311,71 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
   constexpr int ST = (2 * DH + 63) / 64;
   constexpr int NT = 2;  // 16-page tiles in flight
   extern __shared__ uint32_t s_key[];  // [rows_per][p_cap]
+  // of [q+ ; q-], whose groups of 64 hold the same channels twice where DH is a
+  // multiple of 64
+  constexpr int XN = DH % 64 == 0 ? ST / 2 : ST;
   __shared__ int s_len[16], s_seq[16];
+  __shared__ i32x4 s_q[ST][64];
+  __shared__ float s_qs[16];
   const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g = lane >> 4;
   const int h = blockIdx.x % a.n_heads;
   const int r0 = (blockIdx.x / a.n_heads) * a.rows_per;
+  const int rows = min(a.rows_per, a.q_total - r0), cols = rows * a.group;
 
-  if (a.group > 1)
-    for (int x = tid; x < a.rows_per * a.p_cap; x += blockDim.x) s_key[x] = 0u;
-  // the rows may belong to different sequences
+  for (int x = 4 * tid; x < a.rows_per * a.p_cap; x += 4 * blockDim.x)
+    *reinterpret_cast<u32x4 *>(s_key + x) = u32x4{0, 0, 0, 0};
+  // the rows' sequences, by the first wavefront (the last one sees to the queries)
   if (wave == 0) {
-    int b = a.q_off ? wave_find_seq(a.q_off, a.n_seqs, min(r0, a.q_total - 1), lane) : 0;
-    if (lane < a.rows_per) {
-      const int r = r0 + lane;
-      if (!a.q_off) b = r / a.rows_each;
-      else while (b < a.n_seqs && a.q_off[b + 1] <= r) ++b;
-      if (r >= a.q_total || (a.q_off && b < a.n_seqs && r < a.q_off[b])) b = a.n_seqs;
+    int b = a.n_seqs;
+    if (a.q_off) {
+      const int first = a.q_off[0];
+      b = wave_find_seq(a.q_off, a.n_seqs, r0, lane);
+      if (lane > 0 && lane < rows)
+        while (b < a.n_seqs && a.q_off[b + 1] <= r0 + lane) ++b;
+      if (r0 + lane < first) b = a.n_seqs;  // of no sequence
+    } else if (lane < rows) {
+      b = (r0 + lane) / a.rows_each;
+    }
+    if (lane < rows) {
       s_seq[lane] = b;
       s_len[lane] = b < a.n_seqs ? paged_len(a.lens[b], a.max_pages, a.page_log2) : 0;
     }
   }
-  __syncthreads();
 
-  // runs of rows of one sequence are scored at once
-  for (int lo = 0, end; lo < a.rows_per; lo = end) {
-    const int b = __builtin_amdgcn_readfirstlane(s_seq[lo]);
-    const int n_p = __builtin_amdgcn_readfirstlane((s_len[lo] + (1 << a.page_log2) - 1) >> a.page_log2);
-    end = lo + 1;
-    while (end < a.rows_per && s_seq[end] == b) ++end;
-    if (b >= a.n_seqs || n_p <= a.n_select || 16 * wave >= n_p) continue;
-    const int cols = (end - lo) * a.group;
-    for (int col0 = 0; col0 < cols; col0 += 16) {
-      const int col = col0 + c;
-      const bool on = col < cols;
-      const int i = lo + (on ? col / a.group : 0), hg = on ? col % a.group : 0;
+  for (int col0 = 0; col0 < cols; col0 += 16) {
+    const int col = col0 + c;
+    const bool on = col < cols;
+    const int i = on ? col / a.group : 0, hg = on ? col - i * a.group : 0;
+    if (col0 > 0) __syncthreads();  // the products with the last 16 columns are done
+    if (wave == waves - 1) {
+      // The columns' queries as the products' operand, for all wavefronts: a lane holds
+      // its 16-element groups of [q+ ; q-] (columns past the last repeat the first).
       const InT *qp = static_cast<const InT *>(a.q) + (size_t)(r0 + i) * a.q_stride +
                       (size_t)(h * a.group + hg) * DH;
-      // this lane's 16-element groups of [q+ ; q-]
-      float x[ST][16];
+      float x[XN][16];
       uint32_t am = 0;
 #pragma unroll
-      for (int s = 0; s < ST; ++s) {
+      for (int s = 0; s < XN; ++s) {
         const int k0 = 64 * s + 16 * g;
-        const InT *p = qp + (k0 < DH ? k0 : k0 - DH);
+        const InT *p = qp + (k0 < DH ? k0 : k0 < 2 * DH ? k0 - DH : 0);
+        load8(p, x[s]);
+        load8(p + 8, x[s] + 8);
+      }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[s][e] = 0.f;
-        if (on && k0 < 2 * DH) {
-          load8(p, x[s]);
-          load8(p + 8, x[s] + 8);
-        }
+      for (int s = 0; s < XN; ++s)
 #pragma unroll
         for (int e = 0; e < 16; ++e) am = max(am, __float_as_uint(x[s][e]) & 0x7FFFFFFFu);
-      }
       am = max(am, (uint32_t)__shfl_xor((int)am, 16, 64));
       am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
       const int qc = exp_code<I8>(__uint_as_float(am));
-      // a query that is not finite: NaN for every score
-      const float inv = exp_inv(min(qc, 253)), qs = qc == 255 ? NAN : exp_scale(qc);
-      i32x4 qf[ST];
+      const float inv = exp_inv(min(qc, 253));
 #pragma unroll
       for (int s = 0; s < ST; ++s) {
-        const bool neg = 64 * s + 16 * g >= DH;
+        const int k0 = 64 * s + 16 * g;
+        const bool neg = k0 >= DH;
+        i32x4 q;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           float y[4];
@@ -363,12 +383,30 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
           // even), whose two's complement is the sum's low byte
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float v = x[s][4 * w + e];
+            const float v = x[s % XN][4 * w + e];
             y[e] = fmaf(neg ? fminf(v, 0.f) : fmaxf(v, 0.f), inv, 12582912.f);
           }
-          qf[s][w] = pack_low(y[0], y[1], y[2], y[3]);
+          q[w] = k0 < 2 * DH ? pack_low(y[0], y[1], y[2], y[3]) : 0;
         }
+        s_q[s][lane] = q;
       }
+      // a query that is not finite: NaN for every score
+      if (g == 0) s_qs[c] = qc == 255 ? NAN : exp_scale(qc);
+    }
+    __syncthreads();
+    i32x4 qf[ST];
+#pragma unroll
+    for (int s = 0; s < ST; ++s) qf[s] = s_q[s][lane];
+    const float qs = s_qs[c];
+
+    // runs of rows of one sequence are scored at once
+    const int seq = lane < rows ? s_seq[lane] : -1;
+    const int row_p = lane < rows ? (s_len[lane] + (1 << a.page_log2) - 1) >> a.page_log2 : 0;
+    for (int lo = 0, end; lo < rows; lo = end) {
+      const int b = __builtin_amdgcn_readlane(seq, lo), n_p = __builtin_amdgcn_readlane(row_p, lo);
+      end = lo + __builtin_ctzll(__ballot(seq != b) >> lo);  // (lanes behind the rows differ)
+      if (b >= a.n_seqs || n_p <= a.n_select) continue;
+      const bool mine = on && i >= lo && i < end;
       const int32_t *tab = a.table + (size_t)b * a.max_pages;
       for (int p0 = 16 * wave; p0 < n_p; p0 += 16 * NT * waves) {
         float be[NT];
@@ -400,7 +438,7 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
             const float bs = __shfl(be[t], 4 * g + j, 64);
             const uint32_t key = score_key((float)acc[j] * bs * qs);
             const int p = pt + 4 * g + j;
-            if (on && p < n_p) {
+            if (mine && p < n_p) {
               uint32_t *to = &s_key[i * a.p_cap + p];
               if (a.group == 1) *to = key;
               else atomicMax(to, key);
@@ -412,38 +450,67 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
   }
   __syncthreads();
 
-  for (int i = wave; i < a.rows_per; i += waves) {
-    const int r = r0 + i;
-    if (r >= a.q_total || s_seq[i] >= a.n_seqs) continue;
-    int32_t *out = a.pages + ((size_t)r * a.n_heads + h) * a.n_select;
-    const int n_p = (s_len[i] + (1 << a.page_log2) - 1) >> a.page_log2;
+  for (int i = wave; i < rows; i += waves) {
+    if (s_seq[i] >= a.n_seqs) continue;
+    int32_t *out = a.pages + ((size_t)(r0 + i) * a.n_heads + h) * a.n_select;
+    const int n_p = __builtin_amdgcn_readfirstlane((s_len[i] + (1 << a.page_log2) - 1) >> a.page_log2);
     if (n_p <= a.n_select) {  // every page, without a score
       for (int j = lane; j < a.n_select; j += 64) out[j] = j < n_p ? j : -1;
       continue;
     }
-    uint32_t kr[KPL];
+    uint32_t kr[KPL];  // pages 64 j + lane; 0 behind the last
 #pragma unroll
     for (int j = 0; j < KPL; ++j) kr[j] = 64 * j + lane < n_p ? s_key[i * a.p_cap + 64 * j + lane] : 0u;
+    const unsigned long long below = (1ull << lane) - 1ull;
+    if constexpr (KPL == 1) {
+      // One page per lane: a page's rank is the number of larger keys.  Ranks below
+      // n_select are the selection, unless the last of them is shared: of those
+      // pages the first are taken.
+      int rank = 0;
+      for (int j = 0; j < n_p; j += 4) {
+        const u32x4 k = *reinterpret_cast<const u32x4 *>(s_key + i * a.p_cap + j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) rank += k[e] > kr[0] ? 1 : 0;
+      }
+      bool take = rank < a.n_select && kr[0] != 0u;
+      unsigned long long sel = __ballot(take);
+      if (__popcll(sel) > a.n_select) {
+        const uint32_t last = wave_max_u32(take ? (uint32_t)rank : 0u);
+        const unsigned long long tied = __ballot(take && rank == (int)last);
+        take = take && (rank < (int)last || __popcll(tied & below) < a.n_select - (int)last);
+        sel = __ballot(take);
+      }
+      if (take) out[__popcll(sel & below)] = lane;
+      continue;
+    }
+    uint32_t lo = 0xFFFFFFFFu, hi = 0u;
+#pragma unroll
+    for (int j = 0; j < KPL; ++j) {
+      lo = min(lo, kr[j] ? kr[j] : 0xFFFFFFFFu);
+      hi = max(hi, kr[j]);
+    }
     auto count_ge = [&](uint32_t v) {
       int n = 0;
 #pragma unroll
       for (int j = 0; j < KPL; ++j) n += __popcll(__ballot(kr[j] >= v));
       return n;
     };
-    // the largest t with n_select keys or more at or above it; where there are
-    // just as many, they are the selection
-    uint32_t t = 0;
+    lo = ~wave_max_u32(~lo);
+    hi = wave_max_u32(hi);
+    // The largest t with n_select keys or more at or above it, from the first
+    // bit in which the keys differ; where there are just as many, they are the
+    // selection.
+    const int top = lo == hi ? -1 : 31 - __clz(lo ^ hi);
+    uint32_t t = top < 0 ? hi : hi & ~((2u << top) - 1u);
     int at_least = n_p;
-    for (int bit = 31; bit >= 0 && at_least != a.n_select; --bit) {
+    for (int bit = top; bit >= 0 && at_least != a.n_select; --bit) {
       const int n = count_ge(t | (1u << bit));
       if (n >= a.n_select) t |= 1u << bit, at_least = n;
     }
     // of the keys equal to t the first `ties` are taken (at_least == n_select: all)
-    const int above = at_least == a.n_select || t == 0xFFFFFFFFu ? 0 : count_ge(t + 1u);
-    const int ties = a.n_select - above;
     const bool all = at_least == a.n_select;
+    const int ties = all ? 0 : a.n_select - (t == 0xFFFFFFFFu ? 0 : count_ge(t + 1u));
     int base = 0, tie_base = 0;
-    const unsigned long long below = (1ull << lane) - 1ull;
 #pragma unroll
     for (int j = 0; j < KPL; ++j) {
       const unsigned long long tie = __ballot(kr[j] != 0u && kr[j] == t);
@@ -582,7 +649,8 @@ hipError_t launch_paged_select(DType dt, int32_t head_dim, PagedSelectArgs a, hi
   a.rows_per = std::max(1, std::min({16 / a.group, 8192 / a.p_cap, mean}));
   const unsigned grid = (unsigned)(((int64_t)a.q_total + a.rows_per - 1) / a.rows_per * a.n_heads);
   // a wavefront per two tiles of 16 pages, or per four rows where that is more
-  const int waves = std::min(16, std::max((a.max_pages + 31) / 32, (a.rows_per + 3) / 4));
+  // (two at least: one finds the rows' sequences, another quantises)
+  const int waves = std::min(16, std::max({2, (a.max_pages + 31) / 32, (a.rows_per + 3) / 4}));
   const uint32_t lds = (uint32_t)a.rows_per * a.p_cap * 4;
   return by_shape(BF, head_dim, [&](auto, auto dh) {
     auto go = [&](auto kpl) {
@@ -594,6 +662,7 @@ hipError_t launch_paged_select(DType dt, int32_t head_dim, PagedSelectArgs a, hi
     const int kpl = a.p_cap / 64;
     if (kpl <= 1) go(std::integral_constant<int, 1>());
     else if (kpl <= 4) go(std::integral_constant<int, 4>());
+    else if (kpl <= 8) go(std::integral_constant<int, 8>());
     else if (kpl <= 16) go(std::integral_constant<int, 16>());
     else go(std::integral_constant<int, 64>());
   });
