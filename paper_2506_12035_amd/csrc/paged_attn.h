@@ -50,6 +50,21 @@ __device__ __forceinline__ float quad_max(float v) {
   return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
 }
 
+// Global memory at a uniform address that the compiler takes as it is.
+typedef __attribute__((address_space(1))) char gbyte;
+__device__ __forceinline__ const gbyte *scalar(const void *p) {
+  const gbyte *q = (const gbyte *)p;
+  asm("" : "+s"(q));
+  return q;
+}
+// (the lane offset is kept from being widened outside the loop, where the
+// addressing mode would no longer be seen)
+template <typename V>
+__device__ __forceinline__ V at(const gbyte *p, uint32_t lane_offset, int offset) {
+  asm("" : "+v"(lane_offset));
+  return *(const __attribute__((address_space(1))) V *)(p + lane_offset + offset);
+}
+
 // Raw registers of 32 keys of a lane: K for its key c of each half, V for its
 // eight keys, exponent bytes.
 template <int FMT, int DH>
@@ -73,42 +88,43 @@ struct KvRaw {
   // half u of the tile: 16 tokens from `slot` (uniform) on
   __device__ __forceinline__ void load(int u, const void *kb, const void *vb, const uint8_t *kx,
                                        const uint8_t *vx, size_t slot, int c, int g) {
-    const char *kp = static_cast<const char *>(kb) + slot * (DH * ES);
-    const char *vp = static_cast<const char *>(vb) + slot * (DH * ES);
-    // (unsigned 32-bit lane offsets: the loads take them beside a scalar base)
+    // Uniform bases in scalar registers, lane offsets of 32 bits: left to itself
+    // the compiler adds the lane offsets to the pool's base once and keeps a
+    // 64-bit address per load (30 registers and eight additions per tile).
+    const gbyte *kp = scalar(static_cast<const char *>(kb) + slot * (DH * ES));
+    const gbyte *vp = scalar(static_cast<const char *>(vb) + slot * (DH * ES));
     const uint32_t ko = (uint32_t)(c * DH * ES + 16 * g);
 #pragma unroll
-    for (int m = 0; m < KQ; ++m) k[u][m] = *reinterpret_cast<const u32x4 *>(kp + (ko + 64 * m));
+    for (int m = 0; m < KQ; ++m) k[u][m] = at<u32x4>(kp, ko, 64 * m);
     if constexpr (T) {
       const uint32_t to = (uint32_t)(c * DH * ES + 64 * ES + 4 * ES * g);
-      if constexpr (W) kt[u] = *reinterpret_cast<const u32x2 *>(kp + to);
-      else kt[u].x = *reinterpret_cast<const uint32_t *>(kp + to);
+      if constexpr (W) kt[u] = at<u32x2>(kp, to, 0);
+      else kt[u].x = at<uint32_t>(kp, to, 0);
     }
     const uint32_t vo = (uint32_t)(4 * g * DH * ES + c * VC * ES);
     const uint32_t vto = (uint32_t)(4 * g * DH * ES + 64 * ES + c * ES);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const char *p = vp + (vo + r * DH * ES);
       uint32_t(&x)[VW] = v[4 * u + r];
       if constexpr (VW == 1) {
-        x[0] = *reinterpret_cast<const uint32_t *>(p);
+        x[0] = at<uint32_t>(vp, vo, r * DH * ES);
       } else if constexpr (VW == 2) {
-        const u32x2 y = *reinterpret_cast<const u32x2 *>(p);
+        const u32x2 y = at<u32x2>(vp, vo, r * DH * ES);
         x[0] = y.x, x[1] = y.y;
       } else {
-        const u32x4 y = *reinterpret_cast<const u32x4 *>(p);
+        const u32x4 y = at<u32x4>(vp, vo, r * DH * ES);
         x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;
       }
       if constexpr (T) {
-        const char *t = vp + (vto + r * DH * ES);
-        if constexpr (W) vt[4 * u + r] = *reinterpret_cast<const uint16_t *>(t);
-        else vt[4 * u + r] = *reinterpret_cast<const uint8_t *>(t);
+        if constexpr (W) vt[4 * u + r] = at<uint16_t>(vp, vto, r * DH * ES);
+        else vt[4 * u + r] = at<uint8_t>(vp, vto, r * DH * ES);
       }
     }
     if constexpr (!W) {
-      if constexpr (FMT == E4) ke[u] = (kx + slot)[(uint32_t)c];
-      else ke[u] = *reinterpret_cast<const uint32_t *>(kx + slot + (uint32_t)(4 * g));
-      ve[u] = *reinterpret_cast<const uint32_t *>(vx + slot + (uint32_t)(4 * g));
+      const gbyte *ep = scalar(kx + slot), *xp = scalar(vx + slot);
+      if constexpr (FMT == E4) ke[u] = at<uint8_t>(ep, (uint32_t)c, 0);
+      else ke[u] = at<uint32_t>(ep, (uint32_t)(4 * g), 0);
+      ve[u] = at<uint32_t>(xp, (uint32_t)(4 * g), 0);
     }
   }
   // V of keys n .. 15 of half u becomes zero (they hold nothing, or another
