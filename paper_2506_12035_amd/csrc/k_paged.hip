@@ -686,9 +686,16 @@ void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
            << a.page_log2;
   const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32);
   const int64_t units = std::max<int64_t>(1, (int64_t)a.n_seqs * a.n_heads * a.row_blocks);
-  // Wavefronts per unit: enough of them to fill the chip, two tiles each at
-  // least; beyond a workgroup's, the keys are split over workgroups.
-  const int64_t want = std::min<int64_t>((4096 + units - 1) / units, (tiles + 1) / 2);
+  // Wavefronts per unit: two for each of the chip's 1024 SIMDs in all, two tiles
+  // each at least; beyond a workgroup's, the keys are split over workgroups.
+  // More of them repeat the start and the end of a wavefront, some 6 us of
+  // latency: with 4096 one row over 32 caches of 1088 tokens (int8, 8 key heads
+  // of 128) takes 24.9 us for 16.4, 36 .. 100 rows over 32 bf16 caches 65.5 for 53.2.
+  // fp32 rows of several blocks take three times the products a tile, and
+  // sequences with fewer blocks than the longest leave some of the units empty:
+  // 35.8 us with 4096 for 46.3 (1 .. 333 rows, 6 caches up to 1503 tokens).
+  const int64_t fill = dt == DType::F32 && a.row_blocks > 1 ? 4096 : 2048;
+  const int64_t want = std::min<int64_t>((fill + units - 1) / units, (tiles + 1) / 2);
   const int most = a.row_tiles == 1 ? 8 : 4;
   a.waves = 1;
   while (a.waves < most && a.waves < want) a.waves *= 2;
