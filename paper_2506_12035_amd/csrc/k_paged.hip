@@ -22,99 +22,165 @@ namespace marche {
 
 // ------------------------------------------------------------------ write
 
+// Largest over a group of 8 or 16 neighbouring lanes.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true));
+}
+template <int GROUP>
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  v = dpp_max<0xB1>(v);                           // quad_perm [1,0,3,2]
+  v = dpp_max<0x4E>(v);                           // quad_perm [2,3,0,1]
+  v = dpp_max<0x141>(v);                          // row_half_mirror: 8 lanes
+  if constexpr (GROUP == 16) v = dpp_max<0x140>(v);  // row_mirror
+  return v;
+}
+
+// Largest over the wavefront, uniform (no LDS crossbar).
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = group_max<16>(v);
+  auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(p[0], p[1]);
+  auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __builtin_amdgcn_readfirstlane(max(q[0], q[1]));
+}
+
+// Four int8 numbers from floats whose low bytes hold them.
+__device__ __forceinline__ int pack_low(float a, float b, float c, float d) {
+  const uint32_t x = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x0C0C0400u);
+  const uint32_t y = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x04000C0Cu);
+  return (int)(x | y);
+}
+// x 2^-e, exact, rounded to a whole number (ties to even) in the low byte: the
+// sum with 1.5 2^23 has no bits below 1, and its low bits are two's complement.
+__device__ __forceinline__ float round_low(float x, float inv) { return fmaf(x, inv, 12582912.f); }
+
+// Largest magnitude of eight values as float bits, which order like the
+// magnitudes and place NaN above infinity (bf16: in pairs of 16-bit halves).
+template <typename InT, int NV>
+__device__ __forceinline__ uint32_t largest(const u32x4 (&x)[NV]) {
+  if constexpr (sizeof(InT) == 2) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x[0][i] & 0x7FFF7FFFu));
+    return (uint32_t)max(m[0], m[1]) << 16;
+  } else {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, x[i / 4][i % 4] & 0x7FFFFFFFu);
+    return m;
+  }
+}
+
+// Eight values of a row with exponent code `code` in the format.
+template <int FMT, typename InT, int NV>
+__device__ __forceinline__ u32x2 pack8(const u32x4 (&x)[NV], int code) {
+  u32x2 o;
+  if (code == 255) {  // the whole row reads back as NaN
+    o.x = o.y = FMT == E4 ? 0x7F7F7F7Fu : 0u;
+    return o;
+  }
+  const float inv = exp_inv(code);
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    if constexpr (FMT == E4 && sizeof(InT) == 2) {
+      // the conversion divides by the scale's power of two
+      typedef short s16x2 __attribute__((ext_vector_type(2)));
+      s16x2 q = {0, 0};
+      q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(bf16x2, +x[0][2 * w]), exp_scale(code), false);
+      q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(bf16x2, +x[0][2 * w + 1]), exp_scale(code), true);
+      o[w] = __builtin_bit_cast(uint32_t, q);
+      continue;
+    }
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(InT) == 4) f[i] = __uint_as_float(x[w % NV][i]);
+      else f[i] = __uint_as_float(i % 2 ? x[0][2 * w + i / 2] & 0xFFFF0000u : x[0][2 * w + i / 2] << 16);
+    }
+    if constexpr (FMT == E4) {
+      int q = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] * inv, f[1] * inv, 0, false);
+      q = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] * inv, f[3] * inv, q, true);
+      o[w] = (uint32_t)q;
+    } else {
+      o[w] = (uint32_t)pack_low(round_low(f[0], inv), round_low(f[1], inv), round_low(f[2], inv), round_low(f[3], inv));
+    }
+  }
+  return o;
+}
+
 // One (row, head) of new keys and values per GROUP lanes, 8 elements of each
-// per lane: the row's largest magnitude by a DPP reduction, its exponent, one
-// rounding, one 8-byte (16 for bf16) store.  Bound by bytes: each new row is read once and its
-// slot written once.
-template <int FMT, int DH, typename InT>
+// per lane: the row's largest magnitude by lane exchanges, its exponent, one
+// rounding, one 8-byte (16 for bf16) store.  Bound by bytes: each new row is
+// read once and its slot written once.  (Two or four pairs a thread, to find
+// the rows' sequences less often: 59.0 and 64.6 us for 56.4 on 40960 rows of 16
+// heads of 64, bf16 to int8; with STREAM 52.2, 4.8 TB/s.)  STREAM: the rows
+// are loaded past the caches, for calls whose rows do not fit them anyway.
+template <int FMT, int DH, typename InT, bool STREAM>
 __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
   constexpr int GROUP = DH == 64 ? 8 : 16, PER = 256 / GROUP;
+  constexpr int NV = sizeof(InT) == 4 ? 2 : 1;  // 16-byte loads of 8 elements
   __shared__ int s_b0;
   const int tid = threadIdx.x, lane = tid & 63, c = tid % GROUP;
-  const uint32_t u0 = blockIdx.x * PER, unit = u0 + tid / GROUP;  // below 2^31
-  const int r = unit / (uint32_t)a.n_heads, h = unit - (uint32_t)r * a.n_heads;
+  const uint32_t u0 = blockIdx.x * PER, unit = u0 + tid / GROUP;  // pairs are below 2^31
+  const int r = (int)a.d_heads.div(unit), h = (int)(unit - (uint32_t)r * a.n_heads);
   const bool on = r < a.a_total && c < DH / 8;
+  const int rr = r < a.a_total ? r : 0;
 
-  // the row's values, in flight while its sequence is found
-  float kx[8], vx[8];
+  // the values and the token, in flight while the row's sequence is found
+  u32x4 kx[NV], vx[NV];
+  {
+    const size_t at = (size_t)rr * a.row_stride + (size_t)h * DH + (c < DH / 8 ? 8 * c : 0);
+    const u32x4 *kp = reinterpret_cast<const u32x4 *>(static_cast<const InT *>(a.k_new) + at);
+    const u32x4 *vp = reinterpret_cast<const u32x4 *>(static_cast<const InT *>(a.v_new) + at);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) kx[i] = vx[i] = 0.f;
-  if (on) {
-    const size_t at = (size_t)r * a.row_stride + (size_t)h * DH + 8 * c;
-    const InT *kp = static_cast<const InT *>(a.k_new) + at, *vp = static_cast<const InT *>(a.v_new) + at;
-    load8(kp, kx);
-    load8(vp, vx);
+    for (int i = 0; i < NV; ++i) {
+      kx[i] = STREAM ? __builtin_nontemporal_load(kp + i) : kp[i];
+      vx[i] = STREAM ? __builtin_nontemporal_load(vp + i) : vp[i];
+    }
   }
-  const int tok = on ? a.a_idx[r] : -1;
+  const int tok = a.a_idx[rr];
   int b;
   if (a.a_off) {
+    const int first = a.a_off[0];
     if (tid < 64) {
-      const int f = wave_find_seq(a.a_off, a.n_seqs, min((int)(u0 / (uint32_t)a.n_heads), a.a_total - 1), lane);
+      const int f = wave_find_seq(a.a_off, a.n_seqs, min((int)a.d_heads.div(u0), a.a_total - 1), lane);
       if (tid == 0) s_b0 = f;
     }
     __syncthreads();
-    b = s_b0;
-    while (b < a.n_seqs && a.a_off[b + 1] <= r) ++b;
-    if (b < a.n_seqs && r < a.a_off[b]) b = a.n_seqs;  // before the first sequence
+    b = s_b0;  // of the workgroup's first row; on from there
+    while (b < a.n_seqs && a.a_off[b + 1] <= rr) ++b;
+    if (rr < first) b = a.n_seqs;
   } else {
-    b = r / a.rows_each;
+    b = (int)a.d_rows.div((uint32_t)rr);
   }
-  float km = 0.f, vm = 0.f;
+  const bool ok = on && b < a.n_seqs && tok >= 0 && (tok >> a.page_log2) < a.max_pages;
+  const int page = ok ? a.table[(size_t)b * a.max_pages + (tok >> a.page_log2)] : -1;
+  int kc = 0, vc = 0;
   if constexpr (FMT != BF) {
-    // magnitudes as bits, which order like them and place NaN above infinity
-    uint32_t ku = 0, vu = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      ku = max(ku, __float_as_uint(kx[i]) & 0x7FFFFFFFu);
-      vu = max(vu, __float_as_uint(vx[i]) & 0x7FFFFFFFu);
-    }
-#pragma unroll
-    for (int o = GROUP / 2; o > 0; o >>= 1) {
-      ku = max(ku, (uint32_t)__shfl_xor((int)ku, o, 64));
-      vu = max(vu, (uint32_t)__shfl_xor((int)vu, o, 64));
-    }
-    km = __uint_as_float(ku);
-    vm = __uint_as_float(vu);
+    kc = exp_code<FMT>(__uint_as_float(group_max<GROUP>(on ? largest<InT>(kx) : 0u)));
+    vc = exp_code<FMT>(__uint_as_float(group_max<GROUP>(on ? largest<InT>(vx) : 0u)));
   }
-  if (!on || b >= a.n_seqs || tok < 0 || (tok >> a.page_log2) >= a.max_pages) return;
-  const int page = a.table[(size_t)b * a.max_pages + (tok >> a.page_log2)];
   if ((unsigned)page >= (unsigned)a.n_pages) return;
   const size_t slot = (((size_t)page * a.n_heads + h) << a.page_log2) + (tok & ((1 << a.page_log2) - 1));
   const size_t at = slot * DH + 8 * c;
   if constexpr (FMT == BF) {
-    bf16x8 ko, vo;
+    u32x4 ko = kx[0], vo = vx[0];
+    if constexpr (sizeof(InT) == 4) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ko[i] = (bf16)kx[i], vo[i] = (bf16)vx[i];
-    *reinterpret_cast<bf16x8 *>(static_cast<bf16 *>(a.k) + at) = ko;
-    *reinterpret_cast<bf16x8 *>(static_cast<bf16 *>(a.v) + at) = vo;
+      for (int i = 0; i < 4; ++i) {
+        const int w = i / 2, e = i % 2 * 2;
+        ko[i] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)__uint_as_float(kx[w][e]), (bf16)__uint_as_float(kx[w][e + 1])});
+        vo[i] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)__uint_as_float(vx[w][e]), (bf16)__uint_as_float(vx[w][e + 1])});
+      }
+    }
+    *reinterpret_cast<u32x4 *>(static_cast<bf16 *>(a.k) + at) = ko;
+    *reinterpret_cast<u32x4 *>(static_cast<bf16 *>(a.v) + at) = vo;
   } else {
-    auto pack = [](const float (&x)[8], int code) {
-      u32x2 o;
-      if (code == 255) {  // the whole row reads back as NaN
-        o.x = o.y = FMT == E4 ? 0x7F7F7F7Fu : 0u;
-        return o;
-      }
-      const float inv = exp_inv(code);
-      if constexpr (FMT == E4) {
-        int w0 = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
-        w0 = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, w0, true);
-        int w1 = __builtin_amdgcn_cvt_pk_fp8_f32(x[4] * inv, x[5] * inv, 0, false);
-        w1 = __builtin_amdgcn_cvt_pk_fp8_f32(x[6] * inv, x[7] * inv, w1, true);
-        o.x = (uint32_t)w0;
-        o.y = (uint32_t)w1;
-      } else {
-        uint32_t w[2] = {0, 0};
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          w[i / 4] |= ((uint32_t)(int)rintf(x[i] * inv) & 0xFFu) << (8 * (i % 4));
-        o.x = w[0];
-        o.y = w[1];
-      }
-      return o;
-    };
-    const int kc = exp_code<FMT>(km), vc = exp_code<FMT>(vm);
-    *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.k) + at) = pack(kx, kc);
-    *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.v) + at) = pack(vx, vc);
+    *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.k) + at) = pack8<FMT, InT>(kx, kc);
+    *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.v) + at) = pack8<FMT, InT>(vx, vc);
     if (c == 0) {
       a.k_exp[slot] = (uint8_t)kc;
       a.v_exp[slot] = (uint8_t)vc;
@@ -124,55 +190,77 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
 
 // ------------------------------------------------------------------ read
 
-// TB tokens of one (sequence, head) of K and of V per workgroup.  Within a
+// PAGED_READ_TOKENS tokens of one (sequence, head) of K and of V per workgroup.  Within a
 // page the tokens of a head lie one after another on both sides, so a thread
-// takes 16 consecutive elements whatever the head width.  Bound by bytes.
-template <int FMT, int DH, typename OutT>
+// takes EP consecutive elements whatever the head width, EP such that its
+// stores are 16 bytes and a wavefront's are contiguous.  Bound by bytes.  STREAM:
+// past the caches, for outputs that do not fit them (64 sequences of 1088
+// tokens, e4m3 to bf16: 83.3 us without, 77.0 with, 5.6 TB/s).
+template <int FMT, int DH, typename OutT, bool STREAM>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
-  constexpr int CH = DH / 16;
+  constexpr int EP = 16 / sizeof(OutT), CH = DH / EP, N = 4;  // N pieces in flight
   const int blk = blockIdx.x % a.blocks, bh = blockIdx.x / a.blocks;
   const int b = bh / a.n_heads, h = bh - b * a.n_heads;
   const int len = min(paged_len(a.lens[b], a.max_pages, a.page_log2), a.n_tokens);
   const int t0 = blk * PAGED_READ_TOKENS;
   if (t0 >= len) return;
   const int n = min(len - t0, PAGED_READ_TOKENS) * CH;
-  for (int x = threadIdx.x; x < n; x += 256) {
-    const int t = t0 + x / CH, d = (x % CH) * 16;
-    const int page = a.table[(size_t)b * a.max_pages + (t >> a.page_log2)];
-    if ((unsigned)page >= (unsigned)a.n_pages) continue;
-    const size_t slot = (((size_t)page * a.n_heads + h) << a.page_log2) + (t & ((1 << a.page_log2) - 1));
-    const size_t from = slot * DH + d, to = ((size_t)bh * a.n_tokens + t) * DH + d;
+  const int32_t *tab = a.table + (size_t)b * a.max_pages;
+  using In = std::conditional_t<FMT == BF, std::conditional_t<EP == 8, u32x4, u32x2>,
+                                std::conditional_t<EP == 8, u32x2, uint32_t>>;
+  for (int x0 = threadIdx.x; x0 < n; x0 += 256 * N) {
+    size_t slot[N];
+    bool on[N];
+    In in[2][N];
+    uint32_t code[2][N];
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      const void *src = w ? a.v : a.k;
-      OutT *o = static_cast<OutT *>(w ? a.v_out : a.k_out) + to;
-      float f[16];
-      if constexpr (FMT == BF) {
-        const bf16x8 *p = reinterpret_cast<const bf16x8 *>(static_cast<const bf16 *>(src) + from);
-        if constexpr (sizeof(OutT) == 2) {
-          reinterpret_cast<bf16x8 *>(o)[0] = p[0];
-          reinterpret_cast<bf16x8 *>(o)[1] = p[1];
-          continue;
-        }
-        const bf16x8 x0 = p[0], x1 = p[1];
+    for (int j = 0; j < N; ++j) {
+      const int t = t0 + min(x0 + 256 * j, n - 1) / CH;
+      const int page = tab[t >> a.page_log2];
+      on[j] = x0 + 256 * j < n && (unsigned)page < (unsigned)a.n_pages;
+      slot[j] = (((size_t)(on[j] ? page : 0) * a.n_heads + h) << a.page_log2) + (t & ((1 << a.page_log2) - 1));
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = (float)x0[i], f[8 + i] = (float)x1[i];
-      } else {
-        const u32x4 q = *reinterpret_cast<const u32x4 *>(static_cast<const uint8_t *>(src) + from);
-        const float s = exp_scale((w ? a.v_exp : a.k_exp)[slot]);
+    for (int j = 0; j < N; ++j) {
+      const int d = min(x0 + 256 * j, n - 1) % CH * EP;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) unpack4<FMT>(q[i], s, f + 4 * i);
+      for (int w = 0; w < 2; ++w) {
+        const char *src = static_cast<const char *>(w ? a.v : a.k) + (slot[j] * DH + d) * (FMT == BF ? 2 : 1);
+        const In *from = reinterpret_cast<const In *>(src);
+        in[w][j] = STREAM ? __builtin_nontemporal_load(from) : *from;
+        if constexpr (FMT != BF) code[w][j] = (w ? a.v_exp : a.k_exp)[slot[j]];
       }
-      if constexpr (sizeof(OutT) == 4) {
+    }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          reinterpret_cast<float4 *>(o)[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-      } else {
-        bf16x8 y0, y1;
+    for (int j = 0; j < N; ++j) {
+      if (!on[j]) continue;
+      const int x = x0 + 256 * j;
+      const size_t to = ((size_t)bh * a.n_tokens + t0) * DH + (size_t)x * EP;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y0[i] = (bf16)f[i], y1[i] = (bf16)f[8 + i];
-        reinterpret_cast<bf16x8 *>(o)[0] = y0;
-        reinterpret_cast<bf16x8 *>(o)[1] = y1;
+      for (int w = 0; w < 2; ++w) {
+        const uint32_t *q = reinterpret_cast<const uint32_t *>(&in[w][j]);
+        u32x4 o;
+        if constexpr (FMT == BF && EP == 8) {
+          o = in[w][j];
+        } else {
+          float f[EP];
+          if constexpr (FMT == BF) {
+#pragma unroll
+            for (int i = 0; i < EP; ++i) f[i] = __uint_as_float(i % 2 ? q[i / 2] & 0xFFFF0000u : q[i / 2] << 16);
+          } else {
+            const float s = exp_scale(code[w][j]);
+#pragma unroll
+            for (int i = 0; i < EP / 4; ++i) unpack4<FMT>(q[i], s, f + 4 * i);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (EP == 4) o[i] = __float_as_uint(f[i]);
+            else o[i] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)f[2 * i], (bf16)f[2 * i + 1]});
+          }
+        }
+        u32x4 *out = reinterpret_cast<u32x4 *>(static_cast<OutT *>(w ? a.v_out : a.k_out) + to);
+        if constexpr (STREAM) __builtin_nontemporal_store(o, out);
+        else *out = o;
       }
     }
   }
@@ -182,15 +270,19 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
 
 // One wavefront per (sequence, page, head): lanes hold four channels, LPT lanes
 // a token and TPW tokens a load, each lane the largest and smallest of its
-// channels over its tokens; the TPW parts are joined by lane exchanges at the
-// end.  Bound by bytes: every key once, 2 dh + 1 bytes out per page.
-template <int FMT, int DH>
+// channels over its tokens; the TPW parts are joined by lane swaps at the
+// end.  Bound by bytes and, close behind, by the comparisons: two per key
+// element (two tokens at a time share a three-operand one).  STREAM: keys
+// past the caches, where they do not fit them: 29.9 us without, 24.8 with on
+// 142 MB of bf16 keys, but 18.4 without, 19.7 with on 71 MB.
+template <int FMT, int DH, bool STREAM>
 __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
-  constexpr int LPT = DH / 4, TPW = 64 / LPT;
+  constexpr int LPT = DH / 4, TPW = 64 / LPT, ES = FMT == BF ? 2 : 1;
+  using In = std::conditional_t<FMT == BF, u32x2, uint32_t>;
   const int lane = threadIdx.x & 63;
-  const uint32_t unit = blockIdx.x * 4 + (threadIdx.x >> 6);  // below 2^31
-  const uint32_t bp = unit / (uint32_t)a.n_heads;
-  const int h = unit - bp * a.n_heads, b = bp / (uint32_t)a.span;
+  const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // below 2^31
+  const uint32_t bp = a.d_heads.div(unit);
+  const int h = unit - bp * a.n_heads, b = a.d_span.div(bp);
   if (b >= a.n_seqs) return;
   const int len = paged_len(a.lens[b], a.max_pages, a.page_log2);
   const int first = a.first ? max(a.first[b], 0) : 0;
@@ -200,57 +292,91 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
   if ((unsigned)page >= (unsigned)a.n_pages) return;
   const int n = min(len - (p << a.page_log2), 1 << a.page_log2);
   const size_t slot0 = ((size_t)page * a.n_heads + h) << a.page_log2;
-  const int t_in = lane / LPT, l = lane - t_in * LPT;
+  const int t_in = min(lane / LPT, TPW - 1), l = lane % LPT;  // (left-over lanes repeat a token's)
+  const char *src = static_cast<const char *>(a.k) + slot0 * (DH * ES);
+  const uint8_t *ex = FMT == BF ? nullptr : a.k_exp + slot0;
   float hi[4], lo[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) hi[i] = -INFINITY, lo[i] = INFINITY;
-  bool bad = false;
-  if (t_in < TPW) {
-    const size_t es = FMT == BF ? 2 : 1;
-    const char *src = static_cast<const char *>(a.k) + (slot0 * DH + 4 * l) * es;
-#pragma unroll 4
-    for (int t = t_in; t < n; t += TPW) {
-      float f[4];
-      if constexpr (FMT == BF) {
-        const bf16x4 q = *reinterpret_cast<const bf16x4 *>(src + (size_t)t * DH * 2);
-        float z = 0.f;
+  uint32_t most = 0;  // exponent codes; bf16: the values' bits without sign, in halves
+  // eight loads in flight; tokens behind the last repeat it
+  for (int t0 = t_in; t0 < n; t0 += 8 * TPW) {
+    In in[8];
+    uint32_t code[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = (float)q[i], z = fmaf(f[i], 0.f, z);
-        bad |= z != 0.f;  // NaN: some value was not finite
-      } else {
-        const uint32_t code = a.k_exp[slot0 + t];
-        unpack4<FMT>(*reinterpret_cast<const uint32_t *>(src + (size_t)t * DH), exp_scale(code), f);
-        bad |= code == 255;
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t t = min(t0 + j * TPW, n - 1);
+      const In *from = reinterpret_cast<const In *>(src + (t * (DH * ES) + 4 * ES * l));
+      in[j] = STREAM ? __builtin_nontemporal_load(from) : *from;
+      if constexpr (FMT != BF) code[j] = ex[t];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+      float f[2][4];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if constexpr (FMT == BF) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t w = in[j + u][i];
+            f[u][2 * i] = __uint_as_float(w << 16);
+            f[u][2 * i + 1] = __uint_as_float(w & 0xFFFF0000u);
+            most |= (w & 0x7F807F80u) + 0x00800080u;  // bit 15 or 31: an exponent of all ones
+          }
+        } else if constexpr (FMT == E4) {
+          const float s = exp_scale(code[j + u]);
+          const auto x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(in[j + u], s, false);
+          const auto y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(in[j + u], s, true);
+          f[u][0] = x[0], f[u][1] = x[1], f[u][2] = y[0], f[u][3] = y[1];
+          most = max(most, code[j + u]);
+        } else {
+          unpack4<FMT>(in[j + u], exp_scale(code[j + u]), f[u]);
+          most = max(most, code[j + u]);
+        }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) hi[i] = fmaxf(hi[i], f[i]), lo[i] = fminf(lo[i], f[i]);
+      for (int i = 0; i < 4; ++i) {
+        hi[i] = fmaxf(hi[i], fmaxf(f[0][i], f[1][i]));
+        lo[i] = fminf(lo[i], fminf(f[0][i], f[1][i]));
+      }
     }
   }
-  // join the tokens' parts into the first LPT lanes, then the largest magnitude
+  bool bad = FMT == BF ? (most & 0x80008000u) != 0 : most == 255;
+  // join the tokens' parts, then the largest magnitude
   float amax = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float h0 = hi[i], l0 = lo[i];
+    if constexpr (LPT == 20) {
+      const float h0 = hi[i], l0 = lo[i];
 #pragma unroll
-    for (int k = 1; k < TPW; ++k) {
-      hi[i] = fmaxf(hi[i], __shfl(h0, min(lane + k * LPT, 63), 64));
-      lo[i] = fminf(lo[i], __shfl(l0, min(lane + k * LPT, 63), 64));
+      for (int k = 1; k < TPW; ++k) {
+        hi[i] = fmaxf(hi[i], __shfl(h0, min(lane + k * LPT, 63), 64));
+        lo[i] = fminf(lo[i], __shfl(l0, min(lane + k * LPT, 63), 64));
+      }
+    } else {
+      if constexpr (LPT == 16) {
+        auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(hi[i]), __float_as_uint(hi[i]), false, false);
+        auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(lo[i]), __float_as_uint(lo[i]), false, false);
+        hi[i] = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+        lo[i] = fminf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+      }
+      auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(hi[i]), __float_as_uint(hi[i]), false, false);
+      auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(lo[i]), __float_as_uint(lo[i]), false, false);
+      hi[i] = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+      lo[i] = fminf(__uint_as_float(q[0]), __uint_as_float(q[1]));
     }
     amax = fmaxf(amax, fmaxf(fabsf(hi[i]), fabsf(lo[i])));
   }
   bad = __ballot(bad) != 0;
-  amax = wave_max(lane < LPT ? amax : 0.f);
+  amax = __uint_as_float(wave_max_u32(lane < LPT ? __float_as_uint(amax) & 0x7FFFFFFFu : 0u));
   const int code = bad ? 255 : exp_code<I8>(amax);
   const size_t out = (size_t)page * a.n_heads + h;
   if (lane < LPT) {
     uint32_t wh = 0, wl = 0;
     if (code != 255) {
       const float inv = exp_inv(code);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        wh |= ((uint32_t)(int)rintf(hi[i] * inv) & 0xFFu) << (8 * i);
-        wl |= ((uint32_t)(int)rintf(lo[i] * inv) & 0xFFu) << (8 * i);
-      }
+      wh = (uint32_t)pack_low(round_low(hi[0], inv), round_low(hi[1], inv), round_low(hi[2], inv), round_low(hi[3], inv));
+      wl = (uint32_t)pack_low(round_low(lo[0], inv), round_low(lo[1], inv), round_low(lo[2], inv), round_low(lo[3], inv));
     }
     uint32_t *o = reinterpret_cast<uint32_t *>(a.bounds + out * 2 * DH);
     o[l] = wh;
@@ -268,30 +394,6 @@ __device__ __forceinline__ uint32_t score_key(float f) {
   if (f == 0.0f) f = 0.0f;
   const uint32_t u = __float_as_uint(f);
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-
-// Largest over the wavefront, uniform (lane exchanges inside 16 lanes as DPP
-// modifiers, then row swaps: no LDS crossbar).
-template <int CTRL>
-__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
-  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true));
-}
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-  v = dpp_max<0xB1>(v);   // quad_perm [1,0,3,2]
-  v = dpp_max<0x4E>(v);   // quad_perm [2,3,0,1]
-  v = dpp_max<0x141>(v);  // row_half_mirror
-  v = dpp_max<0x140>(v);  // row_mirror
-  auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = max(p[0], p[1]);
-  auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return __builtin_amdgcn_readfirstlane(max(q[0], q[1]));
-}
-
-// Four int8 numbers from floats whose low bytes hold them.
-__device__ __forceinline__ int pack_low(float a, float b, float c, float d) {
-  const uint32_t x = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x0C0C0400u);
-  const uint32_t y = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x04000C0Cu);
-  return (int)(x | y);
 }
 
 // Page selection.  One workgroup per (rows_per consecutive rows, key head): the
@@ -379,12 +481,10 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           float y[4];
-          // x inv is exact; adding 1.5 2^23 rounds it to a whole number (ties to
-          // even), whose two's complement is the sum's low byte
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float v = x[s % XN][4 * w + e];
-            y[e] = fmaf(neg ? fminf(v, 0.f) : fmaxf(v, 0.f), inv, 12582912.f);
+            y[e] = round_low(neg ? fminf(v, 0.f) : fmaxf(v, 0.f), inv);
           }
           q[w] = k0 < 2 * DH ? pack_low(y[0], y[1], y[2], y[3]) : 0;
         }
@@ -609,14 +709,23 @@ static hipError_t by_shape(int32_t format, int32_t head_dim, F f) {
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_paged_write(DType dt, int32_t format, int32_t head_dim, const PagedWriteArgs &a,
-                              hipStream_t s) {
+hipError_t launch_paged_write(DType dt, int32_t format, int32_t head_dim, PagedWriteArgs a, hipStream_t s) {
   if (a.a_total == 0) return hipSuccess;
+  a.d_heads = FastDiv::of(a.n_heads);
+  a.d_rows = FastDiv::of(std::max(1, a.rows_each));
   const int per = 256 / (head_dim == 64 ? 8 : 16);
   const unsigned grid = (unsigned)(((int64_t)a.a_total * a.n_heads + per - 1) / per);
+  // Rows of 64 MB and more are loaded past the caches.  Smaller ones may still
+  // lie there from the product that made them: 10.7 us streamed for 9.6 on 20 MB.
+  const bool stream = 2.0 * a.a_total * a.n_heads * head_dim * (dt == DType::BF16 ? 2 : 4) >= 64e6;
   return by_shape(format, head_dim, [&](auto fmt, auto dh) {
-    if (dt == DType::BF16) launch_kernel(paged_write_kernel<fmt.value, dh.value, bf16>, grid, 256, 0, s, a);
-    else launch_kernel(paged_write_kernel<fmt.value, dh.value, float>, grid, 256, 0, s, a);
+    auto go = [&](auto st) {
+      constexpr bool S = st.value;
+      if (dt == DType::BF16) launch_kernel(paged_write_kernel<fmt.value, dh.value, bf16, S>, grid, 256, 0, s, a);
+      else launch_kernel(paged_write_kernel<fmt.value, dh.value, float, S>, grid, 256, 0, s, a);
+    };
+    if (stream) go(std::true_type());
+    else go(std::false_type());
   });
 }
 
@@ -625,18 +734,29 @@ hipError_t launch_paged_read(DType dt, int32_t format, int32_t head_dim, PagedRe
   if (a.n_seqs == 0 || a.n_tokens == 0) return hipSuccess;
   a.blocks = (a.n_tokens + PAGED_READ_TOKENS - 1) / PAGED_READ_TOKENS;
   const unsigned grid = (unsigned)((int64_t)a.n_seqs * a.n_heads * a.blocks);
+  // as if every sequence had n_tokens tokens (lengths are on the device)
+  const bool stream = 2.0 * a.n_seqs * a.n_heads * a.n_tokens * head_dim * (dt == DType::BF16 ? 2 : 4) >= 64e6;
   return by_shape(format, head_dim, [&](auto fmt, auto dh) {
-    if (dt == DType::BF16) launch_kernel(paged_read_kernel<fmt.value, dh.value, bf16>, grid, 256, 0, s, a);
-    else launch_kernel(paged_read_kernel<fmt.value, dh.value, float>, grid, 256, 0, s, a);
+    auto go = [&](auto st) {
+      constexpr bool S = st.value;
+      if (dt == DType::BF16) launch_kernel(paged_read_kernel<fmt.value, dh.value, bf16, S>, grid, 256, 0, s, a);
+      else launch_kernel(paged_read_kernel<fmt.value, dh.value, float, S>, grid, 256, 0, s, a);
+    };
+    if (stream) go(std::true_type());
+    else go(std::false_type());
   });
 }
 
-hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, const PagedBoundsArgs &a,
-                               hipStream_t s) {
+hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, PagedBoundsArgs a, hipStream_t s) {
   if (a.n_seqs == 0 || a.span == 0) return hipSuccess;
+  a.d_heads = FastDiv::of(a.n_heads);
+  a.d_span = FastDiv::of(a.span);
   const unsigned grid = (unsigned)(((int64_t)a.n_seqs * a.n_heads * a.span + 3) / 4);
+  const double keys = (double)a.n_seqs * a.span * a.n_heads * head_dim * (format == BF ? 2 : 1);
+  const bool stream = keys * (1 << a.page_log2) >= 128e6;
   return by_shape(format, head_dim, [&](auto fmt, auto dh) {
-    launch_kernel(paged_bounds_kernel<fmt.value, dh.value>, grid, 256, 0, s, a);
+    if (stream) launch_kernel(paged_bounds_kernel<fmt.value, dh.value, true>, grid, 256, 0, s, a);
+    else launch_kernel(paged_bounds_kernel<fmt.value, dh.value, false>, grid, 256, 0, s, a);
   });
 }
 

@@ -1278,7 +1278,7 @@ marche_status_t marche_paged_write(const marche_paged_cache_t *cache, int32_t la
   lists.total = lists.row_max = a_total;
   if ((st = validate_paged(lists, cache, stream)) != MARCHE_OK) return st;
   const PagedWriteArgs a{l.k, l.v, l.k_exp, l.v_exp, page_table, a_idx, a_off, k_new, v_new, row_stride,
-                         cache->n_pages, H, l.page_log2, max_pages, n_seqs, a_total, a_total / n_seqs};
+                         cache->n_pages, H, l.page_log2, max_pages, n_seqs, a_total, a_total / n_seqs, {}, {}};
   // Algorithmic traffic: every new row read once, its slot written once.
   LAUNCH(K_PAGED_WRITE, 0, 2.0 * a_total * ((double)H * dh * elem_size(dtype) + l.row_bytes) + 8.0 * a_total,
          launch_paged_write(dtype == MARCHE_BF16 ? DType::BF16 : DType::F32, raw_enum(cache->format), dh, a,
@@ -1343,7 +1343,7 @@ marche_status_t marche_paged_bounds(const marche_paged_cache_t *cache, int32_t l
   lists.max_pages = max_pages;
   if ((st = validate_paged(lists, cache, stream)) != MARCHE_OK) return st;
   const PagedBoundsArgs a{l.k, l.k_exp, l.bounds, l.bounds_exp, page_table, lens, first, cache->n_pages,
-                          cache->n_heads, l.page_log2, max_pages, n_seqs, span};
+                          cache->n_heads, l.page_log2, max_pages, n_seqs, span, {}, {}};
   LAUNCH(K_PAGED_BOUNDS, 0,
          (double)n_seqs * span * (cache->page_size * (double)l.row_bytes +
                                   cache->n_heads * (2.0 * cache->head_dim + 1)),

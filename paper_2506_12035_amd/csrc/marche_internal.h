@@ -250,6 +250,20 @@ hipError_t launch_select_topk(const float *scores, int32_t n_parts, const int32_
 // ---- paged cache (k_paged.hip, k_paged_attn_*.hip) ----
 // Pointers are one layer's; formats are marche_cache_format_t; a page holds
 // 1 << page_log2 tokens.  *_off NULL: every sequence has rows_each rows.
+// Division of numbers below 2^31 by a constant known at launch: with s the
+// bits of d - 1 and m = ceil(2^(32 + s) / d) - 2^32 < 2^32,
+// n / d = (n m / 2^32 + n) / 2^s.
+struct FastDiv {
+  uint32_t m, s;
+  static FastDiv of(uint32_t d) {
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    return {(uint32_t)(((1ull << (32 + s)) + d - 1) / d - (1ull << 32)), s};
+  }
+  __host__ __device__ uint32_t div(uint32_t n) const {
+    return (uint32_t)(((((uint64_t)n * m) >> 32) + n) >> s);
+  }
+};
 struct PagedWriteArgs {
   void *k, *v;
   uint8_t *k_exp, *v_exp;
@@ -257,8 +271,9 @@ struct PagedWriteArgs {
   const void *k_new, *v_new;
   int64_t row_stride;
   int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, a_total, rows_each;
+  FastDiv d_heads, d_rows;  // set by the launch
 };
-hipError_t launch_paged_write(DType dt, int32_t format, int32_t head_dim, const PagedWriteArgs &a,
+hipError_t launch_paged_write(DType dt, int32_t format, int32_t head_dim, PagedWriteArgs a,
                               hipStream_t s);
 constexpr int PAGED_READ_TOKENS = 128;  // tokens per workgroup of the read kernel
 struct PagedReadArgs {
@@ -277,9 +292,9 @@ struct PagedBoundsArgs {
   uint8_t *bounds_exp;
   const int32_t *table, *lens, *first;
   int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, span;
+  FastDiv d_heads, d_span;  // set by the launch
 };
-hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, const PagedBoundsArgs &a,
-                               hipStream_t s);
+hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, PagedBoundsArgs a, hipStream_t s);
 constexpr int PAGED_MAX_PAGES = 4096;  // pages of a sequence, where pages are selected
 struct PagedSelectArgs {
   const int8_t *bounds;
@@ -292,20 +307,6 @@ struct PagedSelectArgs {
   int32_t rows_per, p_cap;  // set by the launch: rows per workgroup, keys per row in LDS
 };
 hipError_t launch_paged_select(DType dt, int32_t head_dim, PagedSelectArgs a, hipStream_t s);
-// Division of numbers below 2^31 by a constant known at launch: with s the
-// bits of d - 1 and m = ceil(2^(32 + s) / d) - 2^32 < 2^32,
-// n / d = (n m / 2^32 + n) / 2^s.
-struct FastDiv {
-  uint32_t m, s;
-  static FastDiv of(uint32_t d) {
-    uint32_t s = 0;
-    while ((1ull << s) < d) ++s;
-    return {(uint32_t)(((1ull << (32 + s)) + d - 1) / d - (1ull << 32)), s};
-  }
-  __host__ __device__ uint32_t div(uint32_t n) const {
-    return (uint32_t)(((((uint64_t)n * m) >> 32) + n) >> s);
-  }
-};
 constexpr int PAGED_MAX_SHARED = 256;  // sequences of a call whose ranges are shared out on the device
 struct PagedAttnArgs {
   const void *k, *v;
