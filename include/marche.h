@@ -412,7 +412,8 @@ typedef enum {
  *                   cache whose pages are never selected)
  * n_heads counts key/value heads; the calls with queries take n_q_heads, a multiple
  * of it, and query head h reads key head h / (n_q_heads / n_heads).  head_dim in
- * {64, 80, 128}; page_size in {16, 32, 64, 128, 256}; pointers 16-byte aligned.
+ * {64, 80, 128}; page_size in {16, 32, 64, 128, 256}; pointers 16-byte aligned;
+ * n_layers * n_pages * n_heads * page_size * head_dim < 2^50.
  * The struct may be filled directly or by marche_paged_cache_init, which places the
  * parts one after the other in one buffer in the order k, v, k_exp, v_exp
  * (8-bit formats only), bounds, bounds_exp (with_bounds only), each at
@@ -484,7 +485,9 @@ marche_status_t marche_paged_read(const marche_paged_cache_t *cache, int32_t lay
  * head_dim values; code 255 where a key is not finite).  Updates the pages of
  * sequence b from the one of token first[b] on (first NULL: from page 0), at
  * most `span` of them: after one appended token, first[b] = lens[b] - 1 and
- * span = 1; after rows written anywhere, first NULL and span = max_pages.
+ * span = 1; after rows written anywhere, first NULL and span = max_pages (a
+ * negative first[b] counts as 0).  A page that several sequences share gets the
+ * bounds of one of them: it should lie below lens for all of them.
  * n_seqs * span * n_heads < 2^31.  Needs cache->bounds. */
 marche_status_t marche_paged_bounds(const marche_paged_cache_t *cache, int32_t layer,
                                     const int32_t *page_table, int32_t max_pages,
@@ -496,12 +499,12 @@ marche_status_t marche_paged_bounds(const marche_paged_cache_t *cache, int32_t l
  * rows, and
  *   score = max over the query heads of the key head of
  *           2^(eq + eb) * sum_d (q_d > 0 ? q_d * hi_d : q_d * lo_d),
- * a whole number times a power of two: exact, whatever the order (scores below
- * the float32 range count as 0).  Equal scores go to the lower page, NaN (a
+ * a whole number times a power of two: exact, whatever the order (below the
+ * float32 range: 0, above it: infinity).  Equal scores go to the lower page, NaN (a
  * query or a key that is not finite) ranks below every number.  Logical pages are written in ascending
  * order to pages[r][head][0 .. n_select), then -1 where the sequence has fewer.
  * q: rows of [n_q_heads][head_dim], q_stride apart.  1 <= n_select,
- * max_pages <= 4096.  Needs cache->bounds, up to date for every page below lens. */
+ * max_pages <= 4096; q_total * n_q_heads < 2^30.  Needs cache->bounds, up to date for every page below lens. */
 marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t layer,
                                     const int32_t *page_table, int32_t max_pages,
                                     const int32_t *lens, int32_t n_seqs, const void *q,
@@ -519,9 +522,13 @@ marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t l
  * them) run the same code; long caches are split over workgroups and the
  * parts joined, so a row's rounding may depend on the sizes of its call.
  * q_max is the largest number of rows of a sequence and len_max the largest
- * length (host copies, for launch geometry).  o: [q_total][n_q_heads * head_dim].
+ * length (host copies, for launch geometry, and preconditions as the lists
+ * are; q_total * n_q_heads < 2^30).  The weighted sum is float32 and divided by
+ * the weights' sum last: values near 2^128 / (256 * tokens) may overflow in it.  o: [q_total][n_q_heads * head_dim].
  * pages NULL: n_select is 0.  With pages: max_pages <= 4096.  workspace:
- * marche_paged_attention_workspace_bytes, 256-byte aligned (may be 0 bytes). */
+ * marche_paged_attention_workspace_bytes, 256-byte aligned (may be 0 bytes;
+ * for these sizes: a smaller len_max can need more; 0 for sizes that the call
+ * refuses; the cache's pointers are not looked at). */
 size_t marche_paged_attention_workspace_bytes(const marche_paged_cache_t *cache, int32_t n_seqs,
                                               int32_t q_total, int32_t q_max, int32_t n_q_heads,
                                               int32_t len_max, int32_t n_select);

@@ -387,10 +387,9 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
 
 // ------------------------------------------------------------------ select
 
-// Order-preserving image of a score: larger score, larger value; NaN with
-// -inf, below every number; -0 ties with +0; never 0.
+// Order-preserving image of a score that is no NaN: larger score, larger value;
+// -0 ties with +0; never 0.
 __device__ __forceinline__ uint32_t score_key(float f) {
-  if (f != f) f = -INFINITY;
   if (f == 0.0f) f = 0.0f;
   const uint32_t u = __float_as_uint(f);
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
@@ -403,8 +402,9 @@ __device__ __forceinline__ uint32_t score_key(float f) {
 //   score = sum_d (q_d > 0 ? q_d hi_d : q_d lo_d) = [q+ ; q-] . [hi ; lo]
 // is an int8 product on the matrix cores (16 pages x 16 columns x 64 deep per
 // instruction) against the bounds as they lie in memory: whole numbers below
-// 2^24, so the sum is exact in any order and scaling it by the two powers of
-// two is too.  The largest over a row's heads is taken in LDS.  Then one
+// 2^24, so the sum is exact in any order, and so is scaling it by the sum of the
+// two exponents (one after the other could overflow in between).  The largest
+// over a row's heads is taken in LDS.  Then one
 // wavefront per row finds the n_select-th largest key by its bits, from the
 // top, and compacts the pages above it (and the first of those equal to it) in
 // ascending order.
@@ -418,7 +418,8 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
   constexpr int XN = DH % 64 == 0 ? ST / 2 : ST;
   __shared__ int s_len[16], s_seq[16];
   __shared__ i32x4 s_q[ST][64];
-  __shared__ float s_qs[16];
+  __shared__ int s_qe[16];
+  constexpr int NOT_FINITE = 1 << 16;  // for an exponent; past every sum of two
   const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g = lane >> 4;
@@ -490,14 +491,13 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
         }
         s_q[s][lane] = q;
       }
-      // a query that is not finite: NaN for every score
-      if (g == 0) s_qs[c] = qc == 255 ? NAN : exp_scale(qc);
+      if (g == 0) s_qe[c] = qc == 255 ? NOT_FINITE : qc - 254;  // both exponents' biases
     }
     __syncthreads();
     i32x4 qf[ST];
 #pragma unroll
     for (int s = 0; s < ST; ++s) qf[s] = s_q[s][lane];
-    const float qs = s_qs[c];
+    const int qe = s_qe[c];
 
     // runs of rows of one sequence are scored at once
     const int seq = lane < rows ? s_seq[lane] : -1;
@@ -509,7 +509,7 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
       const bool mine = on && i >= lo && i < end;
       const int32_t *tab = a.table + (size_t)b * a.max_pages;
       for (int p0 = 16 * wave; p0 < n_p; p0 += 16 * NT * waves) {
-        float be[NT];
+        int be[NT];
         i32x4 bf[NT][ST];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -523,8 +523,7 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
             if (64 * s + 48 < 2 * DH || 64 * s + 16 * g < 2 * DH)
               bf[t][s] = *reinterpret_cast<const i32x4 *>(a.bounds + at * 2 * DH + 64 * s + 16 * g);
           }
-          // bounds that are not finite, and pages outside the pool: NaN
-          be[t] = ok && code != 255 ? exp_scale(code) : NAN;
+          be[t] = ok && code != 255 ? (int)code : NOT_FINITE;  // (pages outside the pool as well)
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -535,8 +534,9 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             // lane's page 4 g + j: its exponent sits in lane 4 g + j
-            const float bs = __shfl(be[t], 4 * g + j, 64);
-            const uint32_t key = score_key((float)acc[j] * bs * qs);
+            const int e = __shfl(be[t], 4 * g + j, 64) + qe;
+            const float score = __builtin_amdgcn_ldexpf((float)acc[j], e);
+            const uint32_t key = score_key(e < NOT_FINITE / 2 ? score : -INFINITY);
             const int p = pt + 4 * g + j;
             if (mine && p < n_p) {
               uint32_t *to = &s_key[i * a.p_cap + p];
@@ -765,7 +765,7 @@ hipError_t launch_paged_select(DType dt, int32_t head_dim, PagedSelectArgs a, hi
   a.p_cap = (a.max_pages + 63) / 64 * 64;
   // consecutive rows that a sequence is likely to own, as far as they fit the
   // 16 columns and their keys 32 KB of LDS
-  const int mean = (a.q_total + a.n_seqs - 1) / a.n_seqs;
+  const int mean = (int)(((int64_t)a.q_total + a.n_seqs - 1) / a.n_seqs);
   a.rows_per = std::max(1, std::min({16 / a.group, 8192 / a.p_cap, mean}));
   const unsigned grid = (unsigned)(((int64_t)a.q_total + a.rows_per - 1) / a.rows_per * a.n_heads);
   // a wavefront per two tiles of 16 pages, or per four rows where that is more
@@ -828,7 +828,7 @@ void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
   // equal ranges, shared out on the device, over 512 workgroups (two of 4
   // wavefronts per compute unit; measured against 256 to 1024 of 2 to 8).
   const int64_t per = (int64_t)a.n_heads * a.row_blocks;
-  if (a.n_select == 0 && a.n_seqs <= PAGED_MAX_SHARED && tiles * a.n_seqs < (1LL << 31) &&
+  if (a.n_select == 0 && a.n_seqs <= PAGED_MAX_SHARED && tiles * a.n_seqs < (1LL << 30) &&
       a.splits > 1) {
     a.waves = std::min(a.waves, 4);
     a.budget = (int32_t)std::max<int64_t>(2 * a.n_seqs, (512 + per - 1) / per);

@@ -10,6 +10,7 @@
 #include <cstdio>
 #include <cstring>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -1034,6 +1035,11 @@ bool paged_shape(int32_t n_layers, int32_t n_pages, int32_t n_heads, int32_t pag
     return bad(MARCHE_ERR_UNSUPPORTED, "head_dim", head_dim);
   if (format != MARCHE_CACHE_BF16 && format != MARCHE_CACHE_E4M3 && format != MARCHE_CACHE_INT8)
     return bad(MARCHE_ERR_UNSUPPORTED, "format", format);
+  // far past any memory, and the sizes below stay within 64 bits
+  if ((double)n_layers * n_pages * n_heads * page_size * head_dim >= 0x1p50) {
+    *st = fail(MARCHE_ERR_UNSUPPORTED, "cache.n_layers*n_pages*n_heads*page_size*head_dim reaches 2^50");
+    return false;
+  }
   return true;
 }
 
@@ -1137,7 +1143,6 @@ const char *check_lists(const PagedLists &l, const marche_paged_cache_t *c, int3
     const int32_t p = l.page_table[(size_t)b * l.max_pages + tok / c->page_size];
     return p >= 0 && p < c->n_pages;
   };
-  if (l.off && (l.off[0] != 0 || l.off[l.n_seqs] != l.total)) return say("row offsets inconsistent with the total", 0);
   for (int b = 0; b < l.n_seqs; ++b) {
     const int32_t each = l.total / l.n_seqs;
     const int32_t r0 = l.off ? l.off[b] : b * each, r1 = l.off ? l.off[b + 1] : r0 + each;
@@ -1147,7 +1152,7 @@ const char *check_lists(const PagedLists &l, const marche_paged_cache_t *c, int3
       for (int64_t t = 0; t < l.lens[b]; t += c->page_size)
         if (!page_ok(b, t)) return say("page outside the pool", b);
     }
-    if (l.first && (l.first[b] < 0 || l.first[b] > l.lens[b])) return say("first token out of range", b);
+    if (l.first && l.first[b] > l.lens[b]) return say("first token out of range", b);
     if (l.idx) {
       std::vector<int32_t> seen(l.idx + r0, l.idx + r1);
       std::sort(seen.begin(), seen.end());
@@ -1166,7 +1171,7 @@ const char *check_lists(const PagedLists &l, const marche_paged_cache_t *c, int3
   return nullptr;
 }
 
-marche_status_t validate_paged(PagedLists l, const marche_paged_cache_t *c, hipStream_t stream) {
+marche_status_t validate_paged(PagedLists l, const marche_paged_cache_t *c, hipStream_t stream) try {
   if (!validate_requested() || l.n_seqs == 0) return MARCHE_OK;
   std::vector<std::vector<int32_t>> kept;
   hipError_t e = hipSuccess;
@@ -1188,6 +1193,8 @@ marche_status_t validate_paged(PagedLists l, const marche_paged_cache_t *c, hipS
   int32_t seq = 0;
   const char *what = check_lists(l, c, &seq);
   return what ? fail(MARCHE_ERR_INVALID_ARG, "paged lists: %s (sequence %d)", what, seq) : MARCHE_OK;
+} catch (const std::bad_alloc &) {
+  return fail_hip(hipErrorOutOfMemory, "paged-list validation");
 }
 
 // The kernel arguments that the workspace query and the call share.
@@ -1381,8 +1388,8 @@ marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t l
     return fail(MARCHE_ERR_UNSUPPORTED, "max_pages=%d > %d", max_pages, PAGED_MAX_PAGES);
   if (n_select < 1 || n_select > PAGED_MAX_PAGES)
     return fail(MARCHE_ERR_INVALID_ARG, "n_select=%d outside [1, %d]", n_select, PAGED_MAX_PAGES);
-  if ((int64_t)q_total * n_q_heads >= (1LL << 31))
-    return fail(MARCHE_ERR_UNSUPPORTED, "q_total*n_q_heads reaches 2^31");
+  if ((int64_t)q_total * n_q_heads >= PAGED_MAX_ROWS)
+    return fail(MARCHE_ERR_UNSUPPORTED, "q_total*n_q_heads reaches 2^30");
   if (q_total == 0) return MARCHE_OK;
   if (!page_table || !lens || !q || !pages)
     return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_select");
@@ -1426,9 +1433,12 @@ marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t l
 size_t marche_paged_attention_workspace_bytes(const marche_paged_cache_t *cache, int32_t n_seqs,
                                               int32_t q_total, int32_t q_max, int32_t n_q_heads,
                                               int32_t len_max, int32_t n_select) {
-  PagedLayer l;
-  if (check_paged(cache, 0, 1, n_seqs, &l) != MARCHE_OK || q_total < 1 || q_max < 1 || len_max < 0 ||
-      n_select < 0 || n_q_heads < 1 || n_q_heads % cache->n_heads)
+  marche_status_t st;
+  if (!cache || !paged_shape(cache->n_layers, cache->n_pages, cache->n_heads, cache->page_size,
+                             cache->head_dim, raw_enum(cache->format), &st) ||
+      n_seqs < 1 || q_total < 1 || q_max < 1 || q_max > q_total || len_max < 0 || len_max > 1 << 30 ||
+      n_select < 0 || n_select > PAGED_MAX_PAGES || n_q_heads < 1 || n_q_heads % cache->n_heads ||
+      (int64_t)q_total * n_q_heads >= PAGED_MAX_ROWS)
     return 0;
   size_t need = 0;
   for (DType dt : {DType::BF16, DType::F32}) {  // either type of rows
@@ -1465,8 +1475,8 @@ marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_
   if (pages && max_pages > PAGED_MAX_PAGES)
     return fail(MARCHE_ERR_UNSUPPORTED, "max_pages=%d > %d with selected pages", max_pages, PAGED_MAX_PAGES);
   const int32_t H = cache->n_heads, dh = cache->head_dim;
-  if ((int64_t)q_total * n_q_heads >= (1LL << 31))
-    return fail(MARCHE_ERR_UNSUPPORTED, "q_total*n_q_heads reaches 2^31");
+  if ((int64_t)q_total * n_q_heads >= PAGED_MAX_ROWS)
+    return fail(MARCHE_ERR_UNSUPPORTED, "q_total*n_q_heads reaches 2^30");
   if (q_total == 0) return MARCHE_OK;
   const DType dt = dtype == MARCHE_BF16 ? DType::BF16 : DType::F32;
   PagedAttnArgs a{};

@@ -295,6 +295,7 @@ struct PagedBoundsArgs {
   FastDiv d_heads, d_span;  // set by the launch
 };
 hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, PagedBoundsArgs a, hipStream_t s);
+constexpr int64_t PAGED_MAX_ROWS = 1 << 30;  // rows of queries times their heads
 constexpr int PAGED_MAX_PAGES = 4096;  // pages of a sequence, where pages are selected
 struct PagedSelectArgs {
   const int8_t *bounds;

@@ -36,8 +36,8 @@ __device__ __forceinline__ float exp_inv(int code) { return __uint_as_float((uin
 template <int FMT>
 __device__ __forceinline__ void unpack4(uint32_t w, float scale, float *o) {
   if constexpr (FMT == E4) {
-    // (the conversion's own scale operand is 1: times a power of two after it
-    // is exact, and keeps the code 255 a NaN)
+    // (times a power of two after the conversion is exact, and keeps the code 255
+    // a NaN)
     o[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0) * scale;
     o[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * scale;
     o[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * scale;

@@ -78,6 +78,7 @@ CALLS = [_write, _read, _bounds, _select, _attend]
     (dict(page_size=48), UNSUPPORTED, "page_size"), (dict(page_size=8), UNSUPPORTED, "page_size"),
     (dict(page_size=512), UNSUPPORTED, "page_size"), (dict(page_size=-64), UNSUPPORTED, "page_size"),
     (dict(head_dim=96), UNSUPPORTED, "head_dim"), (dict(fmt=3), UNSUPPORTED, "format"), (dict(fmt=-1), UNSUPPORTED, "format"),
+    (dict(n_pages=2147483647, n_heads=60000, page_size=256), UNSUPPORTED, "2^50"),
     (dict(k=None), INVALID, "cache.k"), (dict(v_exp=None), INVALID, "v_exp"), (dict(k=FAKE + 8), INVALID, "aligned"),
     (dict(k_exp=FAKE + 4), INVALID, "aligned"), (dict(bounds_exp=None), INVALID, "bounds"),
     (dict(bounds=FAKE + 8), INVALID, "aligned")])
@@ -146,6 +147,7 @@ def test_select_refusals():
         assert _select(**{name: None}) == INVALID
     assert _select(q=FAKE + 4) == INVALID
     assert _select(total=1 << 28) == UNSUPPORTED
+    assert _select(total=1 << 27) == UNSUPPORTED and "2^30" in binding.last_error()
     assert _select(total=0) == OK
 
 
@@ -165,6 +167,7 @@ def test_attention_refusals():
         assert _attend(**{name: None}) == INVALID
     assert _attend(q=FAKE + 8) == INVALID and _attend(o=FAKE + 8) == INVALID
     assert _attend(ws=FAKE + 64, ws_bytes=1 << 30) == INVALID
+    assert _attend(total=1 << 27) == UNSUPPORTED and "2^30" in binding.last_error()
     assert _attend(total=0, q_max=0) == OK
 
 
@@ -178,7 +181,11 @@ def test_attention_workspace():
     assert _attend(c, **call) == WORKSPACE and "workspace" in binding.last_error()
     assert _attend(c, ws=FAKE, ws_bytes=256, **call) == WORKSPACE
     assert binding.paged_attention_workspace_bytes(c, 64, 64 * 320, 320, 8, 320) == 0
-    for bad in (dict(n_seqs=-1), dict(q_total=0), dict(q_max=0), dict(n_q_heads=6), dict(len_max=-1), dict(n_select=-1)):
+    # sizes alone decide: a pool that is not there yet will do
+    assert binding.paged_attention_workspace_bytes(_cache(k=None, v=None, k_exp=None, v_exp=None, bounds=None), 1, 1, 1,
+                                                   8, 32768) == n
+    for bad in (dict(n_seqs=-1), dict(n_seqs=0), dict(q_total=0), dict(q_max=0), dict(q_max=2), dict(n_q_heads=6), dict(len_max=-1),
+                dict(len_max=2147483647), dict(n_select=-1), dict(n_select=4097), dict(q_total=1 << 27)):
         a = dict(n_seqs=1, q_total=1, q_max=1, n_q_heads=8, len_max=100, n_select=0)
         a.update(bad)
         assert binding.paged_attention_workspace_bytes(c, **a) == 0
@@ -192,6 +199,7 @@ def test_cache_in_one_buffer():
     assert binding.paged_cache_bytes(*args, INT8, False) == 2 * kv + 2 * ex
     assert binding.paged_cache_bytes(*args, BF16C, False) == 2 * up(2 * 5 * 3 * 16 * 80 * 2)
     assert binding.paged_cache_bytes(2, 5, 3, 20, 80, INT8, True) == 0
+    assert binding.paged_cache_bytes(2147483647, 2147483647, 65535, 256, 128, BF16C, True) == 0
     n = 2 * kv + 2 * ex + bd + be
     c = binding.paged_cache_init(*args, INT8, True, FAKE, n)
     assert [c.k, c.v, c.k_exp, c.v_exp, c.bounds, c.bounds_exp] == [

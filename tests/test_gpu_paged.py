@@ -451,6 +451,7 @@ PAGES_CASES = [
     ([500, 120], [70, 20], 1, 1, 64, 16, 4),
     ([260], [9], 7, 1, 64, 64, 2),
     ([900], [30], 3, 1, 128, 16, 5),
+    ([6000], [2], 2, 1, 80, 32, 40),
 ]
 
 
@@ -722,6 +723,160 @@ def test_cached_tokens_meet_the_segment_attention():
     assert attention_errors(pool, o.view(B * n_a, -1).double().cpu().numpy(), q, [n_a, n_a], 1, "bf16") <= 1
 
 
+# ------------------------------------------------------------------ large calls, many sequences
+
+@pytest.mark.parametrize("fmt,dtype,H,dh", [("e4m3", "bf16", 16, 64), ("int8", "f32", 8, 80), ("bf16", "f32", 4, 128),
+                                            ("int8", "bf16", 16, 64)])
+def test_large_writes_and_reads_are_small_ones_together(fmt, dtype, H, dh):
+    """Rows and outputs of more than 64 MB at once and in pieces: the same bytes."""
+    say(f"paged large write and read {fmt} {dtype} {dh}")
+    page, n_seqs = 64, 20
+    elem = 2 if dtype == "bf16" else 4
+    n = 1 + 64_000_000 // (2 * H * dh * elem * n_seqs)
+    per = -(-n // page)
+    n_pages = n_seqs * per
+    es, new = (2, torch.bfloat16) if fmt == "bf16" else (1, torch.uint8)
+    table = i32(np.random.default_rng(1).permutation(n_pages).reshape(n_seqs, per))
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(n_seqs * n, 2 * H * dh, device="cuda", generator=g).to(TORCH[dtype])
+    idx = i32(np.tile(np.arange(n), n_seqs))
+    off = offsets([n] * n_seqs)
+    pools = []
+    for pieces in (1, n_seqs):
+        kv = [torch.zeros(n_pages, H, page, dh, dtype=new, device="cuda") for _ in range(2)]
+        ex = [torch.zeros(n_pages, H, page, dtype=torch.uint8, device="cuda") for _ in range(2)] if es == 1 else [None] * 2
+        cache = binding.paged_cache(1, n_pages, H, page, dh, FMT[fmt], *kv, *ex, None, None)
+        if pieces == 1:
+            binding.paged_write(cache, 0, table, per, n_seqs, idx, i32(off), n_seqs * n, x, x[:, H * dh:], 2 * H * dh, DT[dtype])
+        else:
+            for b in range(n_seqs):
+                r = x[off[b]:off[b + 1]]
+                binding.paged_write(cache, 0, table[b:], per, 1, idx, None, n, r, r[:, H * dh:], 2 * H * dh, DT[dtype])
+        torch.cuda.synchronize()
+        pools.append(kv + [e for e in ex if e is not None])
+    for a, b in zip(*pools):
+        assert torch.equal(a, b)
+    lens = i32([n - (b % 3) for b in range(n_seqs)])
+    whole = [torch.full((n_seqs, H, n, dh), 7.0, dtype=TORCH[dtype], device="cuda") for _ in range(2)]
+    parts = [torch.full((n_seqs, H, n, dh), 7.0, dtype=TORCH[dtype], device="cuda") for _ in range(2)]
+    binding.paged_read(cache, 0, table, per, lens, n_seqs, n, whole[0], whole[1], DT[dtype])
+    for b in range(n_seqs):
+        binding.paged_read(cache, 0, table[b:], per, lens[b:], 1, n, parts[0][b], parts[1][b], DT[dtype])
+    torch.cuda.synchronize()
+    for a, b in zip(whole, parts):
+        assert torch.equal(a, b)
+    some = slice(3 * n + 5, 3 * n + 45)  # and right: sequence 3's tokens 5 .. 44
+    for w in range(2):
+        rows = x[some, w * H * dh:(w + 1) * H * dh].double().cpu().numpy().reshape(40, H, dh)
+        want = rows if fmt == "bf16" else ref.value(*ref.quantise(rows, fmt))
+        np.testing.assert_array_equal(whole[w][3, :, 5:45].double().cpu().numpy().transpose(1, 0, 2),
+                                      rnd(want, "bf16") if fmt == "bf16" else want)
+
+
+@pytest.mark.parametrize("fmt,dh", [("e4m3", 64), ("int8", 80), ("bf16", 128)])
+def test_large_bounds_are_small_ones_together(fmt, dh):
+    """Bounds of more than 128 MB of keys at once and sequence by sequence."""
+    say(f"paged large bounds {fmt} {dh}")
+    H, page, n_seqs, es = 16, 64, 24, 2 if fmt == "bf16" else 1
+    per = 1 + 128_000_000 // (H * page * dh * es * n_seqs)
+    n_pages = n_seqs * per
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(n_pages, H, page, dh, device="cuda", generator=g)
+    if fmt == "bf16":
+        k, ke = x.bfloat16(), None
+    else:
+        k = x.to(torch.float8_e4m3fn).view(torch.uint8) if fmt == "e4m3" else (40 * x).clamp(-127, 127).to(torch.int8).view(torch.uint8)
+        ke = torch.randint(120, 131, (n_pages, H, page), generator=g, device="cuda", dtype=torch.uint8)
+    out = []
+    table = i32(np.random.default_rng(1).permutation(n_pages).reshape(n_seqs, per))
+    lens = i32([per * page - 7 * b for b in range(n_seqs)])
+    for pieces in (1, n_seqs):
+        bd = torch.zeros(n_pages, H, 2, dh, dtype=torch.int8, device="cuda")
+        be = torch.zeros(n_pages, H, dtype=torch.uint8, device="cuda")
+        cache = binding.paged_cache(1, n_pages, H, page, dh, FMT[fmt], k, k, ke, ke, bd, be)
+        for b in range(pieces):
+            binding.paged_bounds(cache, 0, table[b:], per, lens[b:], None, per, n_seqs // pieces)
+        torch.cuda.synchronize()
+        out.append((bd, be))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+    p = int(table[2, 1])
+    keys = k[p].double().cpu().numpy() if fmt == "bf16" else ref.value(
+        k[p].view(torch.float8_e4m3fn if fmt == "e4m3" else torch.int8).float().cpu().numpy().astype(np.float64),
+        ke[p].cpu().numpy().astype(np.int64))
+    want, code = ref.bounds(keys.transpose(1, 0, 2))
+    np.testing.assert_array_equal(out[0][0][p].cpu().numpy(), want)
+    np.testing.assert_array_equal(out[0][1][p].cpu().numpy(), code)
+
+
+MANY_CASES = [
+    # sequences, rows of each, dtype: caches cut into ranges of one length (up to
+    # 256 sequences) or each by itself
+    (65, 1, "bf16"), (100, 1, "f32"), (128, 1, "bf16"), (200, 20, "bf16"), (256, 20, "bf16"), (257, 20, "bf16"), (70, 20, "f32"),
+]
+
+
+@pytest.mark.parametrize("n,rows,dtype", MANY_CASES)
+def test_attention_of_many_uneven_sequences(n, rows, dtype):
+    say(f"paged attention of {n} sequences, {rows} rows, {dtype}")
+    rng = np.random.default_rng(n)
+    lens = rng.integers(0, 40, n)
+    lens[rng.permutation(n)[:n // 8]] = 0
+    lens[rng.permutation(n)[:5]] = rng.integers(300, 1500, 5)
+    lens[-1] = 1700
+    pool = Pool("e4m3", lens.tolist(), 1, 64, 32, seed=9)
+    q = rnd(2 * rng.standard_normal((n * rows, 64)), dtype)
+    for off in ("csr", None):
+        got = attention(pool, dev(q, TORCH[dtype]), [rows] * n, 1, dtype, off=off).double().cpu().numpy()
+        assert np.isfinite(got).all()
+        assert attention_errors(pool, got, q, [rows] * n, 1, dtype) <= 1
+
+
+def test_attention_of_nothing_cached():
+    """Every sequence empty, len_max 0: zeros, whatever the pool holds."""
+    say("paged attention, nothing cached")
+    pool = Pool("bf16", [0, 0, 0], 2, 64, 16)
+    q = dev(np.ones((5, 256)), torch.bfloat16)
+    for pages in (None, i32(np.zeros((5, 2, 3)))):
+        o = attention(pool, q, [3, 0, 2], 2, "bf16", pages, len_max=0)
+        assert (o == 0).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_sequences_that_share_pages(fmt):
+    """Two sequences with a common first part in the same pages, and one that is
+    the common part alone."""
+    say(f"paged shared pages {fmt}")
+    pool = Pool(fmt, [90, 70, 32], 2, 64, 16, seed=4, with_bounds=True)
+    pool.table[1, :2] = pool.table[2, :2] = pool.table[0, :2]
+    pool.dtable = i32(pool.table)
+    binding.paged_bounds(pool.cache, 0, pool.dtable, pool.width, pool.dlens, None, pool.width, 3)
+    rng = np.random.default_rng(6)
+    rows = [2, 1, 3]
+    q = rnd(rng.standard_normal((6, 256)), "bf16")
+    pages = _select(pool, dev(q, torch.bfloat16), rows, 2, 3, "bf16")
+    np.testing.assert_array_equal(pages.cpu().numpy(), _oracle_pages(pool, q, rows, 2, 3))
+    for pg in (None, pages):
+        got = attention(pool, dev(q, torch.bfloat16), rows, 2, "bf16", pg).double().cpu().numpy()
+        look = None if pg is None else _look(pool, pages.cpu().numpy(), rows)
+        assert attention_errors(pool, got, q, rows, 2, "bf16", look) <= 1
+
+
+@pytest.mark.parametrize("big,small", [(118, 40), (40, 118)])
+def test_scores_of_far_exponents(big, small):
+    """Scores within range whose factors, applied one by one, are not."""
+    say(f"paged select, exponents {big} {small}")
+    pool = Pool("int8", [16 * 8] * 2, 1, 64, 16, with_bounds=True)
+    rng = np.random.default_rng(8)
+    pool.db[:] = dev(rng.integers(-127, 128, pool.db.shape).astype(np.int8))
+    pool.dbe[:] = 127 + big
+    q = rnd(rng.standard_normal((2, 64)) * 2.0 ** -small, "bf16")
+    if big < small:
+        pool.dbe[:] = 127 - small
+        q = rnd(rng.standard_normal((2, 64)) * 2.0 ** big, "bf16")
+    pages = _select(pool, dev(q, torch.bfloat16), [1, 1], 1, 3, "bf16")
+    np.testing.assert_array_equal(pages.cpu().numpy(), _oracle_pages(pool, q, [1, 1], 1, 3))
+
+
 # ------------------------------------------------------------------ debug validation
 
 @pytest.mark.parametrize("bad,word", [
@@ -768,3 +923,23 @@ def test_validated_write(monkeypatch, idx, word):
         return
     with pytest.raises(binding.MarcheError, match=word):
         call()
+
+
+def test_validation_takes_what_the_calls_take(monkeypatch):
+    """Rows of no sequence before and behind the others, and the first token of
+    an empty sequence."""
+    say("paged validate padding")
+    monkeypatch.setenv("MARCHE_VALIDATE", "1")
+    pool = Pool("int8", [64, 0], 1, 64, 16, width_extra=0, with_bounds=True)
+    x = torch.ones(6, 64, dtype=torch.bfloat16, device="cuda")
+    o = torch.full_like(x, 7.0)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    off, bf = i32([1, 3, 4]), DT["bf16"]
+    binding.paged_write(pool.cache, 0, pool.dtable, 4, 2, i32([-1, 3, 9, 5, 99, 99]), i32([1, 3, 3]), 6, x, x, 64, bf)
+    binding.paged_bounds(pool.cache, 0, pool.dtable, 4, pool.dlens, i32([63, -1]), 1, 2)
+    pages = torch.full((6, 1, 2), -5, dtype=torch.int32, device="cuda")
+    binding.paged_select(pool.cache, 0, pool.dtable, 4, pool.dlens, 2, x, 64, off, 6, 1, bf, 2, pages)
+    binding.paged_attention(pool.cache, 0, pool.dtable, 4, pool.dlens, 64, 2, x, 64, off, 6, 2, 1, bf, o, pages, 2, ws, 1 << 20)
+    torch.cuda.synchronize()
+    assert (o[[0, 4, 5]] == 7).all() and (o[3] == 0).all() and not (o[1:3] == 7).any()
+    assert (pages[[0, 4, 5]] == -5).all() and (pages[3] == -1).all()
