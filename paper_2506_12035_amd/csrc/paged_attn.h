@@ -67,11 +67,15 @@ __device__ __forceinline__ V at(const gbyte *p, uint32_t lane_offset, int offset
 
 // Raw registers of 32 keys of a lane: K for its key c of each half, V for its
 // eight keys, exponent bytes.
-template <int FMT, int DH>
+template <int FMT, int DH, bool STAGE>
 struct KvRaw {
   static constexpr bool W = FMT == BF;               // 2-byte elements
   static constexpr int ES = W ? 2 : 1;
-  static constexpr int KQ = W ? DH / 32 : DH / 64;   // 16-byte loads per key
+  static constexpr int KQ = W ? DH / 32 : DH / 64;   // 16-byte pieces per key and lane
+  static constexpr int RB = DH * ES;                 // bytes of a row
+  static constexpr int RP = RB / 16;                 // 16-byte pieces of a row
+  static constexpr int KL = RB / 64;                 // 16-byte loads of 16 keys,
+  static constexpr int KT = RB % 64 / 16;            // and dwords of one more
   static constexpr bool T = DH % 32 != 0;            // a 16-channel tail (dh 80)
   static constexpr int NC = DH / 32 + T;             // 32-deep products of S; the tail fills half of one
   static constexpr int VC = DH == 128 ? 8 : 4;       // channels per lane
@@ -79,8 +83,8 @@ struct KvRaw {
   static constexpr int M = DH / 16;                  // 16-channel tiles of O
   static_assert(DH == 64 || DH == 80 || DH == 128, "head width");
 
-  u32x4 k[2][KQ];
-  u32x2 kt[2];
+  u32x4 k[2][KL];
+  uint32_t kt[2][2];
   uint32_t v[8][VW];
   uint32_t vt[8];
   uint32_t ke[2], ve[2];  // ke: the byte of key c (e4m3), the four of keys 4g.. (int8)
@@ -93,13 +97,30 @@ struct KvRaw {
     // 64-bit address per load (30 registers and eight additions per tile).
     const gbyte *kp = scalar(static_cast<const char *>(kb) + slot * (DH * ES));
     const gbyte *vp = scalar(static_cast<const char *>(vb) + slot * (DH * ES));
-    const uint32_t ko = (uint32_t)(c * DH * ES + 16 * g);
+    if constexpr (!STAGE) {
+      const uint32_t ko = (uint32_t)(c * RB + 16 * g), to = (uint32_t)(c * RB + 64 * ES + 4 * ES * g);
 #pragma unroll
-    for (int m = 0; m < KQ; ++m) k[u][m] = at<u32x4>(kp, ko, 64 * m);
-    if constexpr (T) {
-      const uint32_t to = (uint32_t)(c * DH * ES + 64 * ES + 4 * ES * g);
-      if constexpr (W) kt[u] = at<u32x2>(kp, to, 0);
-      else kt[u].x = at<uint32_t>(kp, to, 0);
+      for (int m = 0; m < KQ; ++m) k[u][m] = at<u32x4>(kp, ko, 64 * m);
+      if constexpr (T && W) {
+        const u32x2 y = at<u32x2>(kp, to, 0);
+        kt[u][0] = y.x, kt[u][1] = y.y;
+      } else if constexpr (T) {
+        kt[u][0] = at<uint32_t>(kp, to, 0);
+      }
+    } else {
+      const uint32_t lane = 16 * g + c;
+#pragma unroll
+      for (int m = 0; m < KL; ++m) {
+        const uint32_t key = RP == 10 || RP == 5 ? 0 : (64 / RP * m + lane / RP), in = lane % RP;
+        const uint32_t ko = RP == 10 || RP == 5 ? 16 * lane : (key - 64 / RP * m) * RB + 16 * (in ^ swizzle(key));
+        k[u][m] = at<u32x4>(kp, ko, 1024 * m);
+      }
+      if constexpr (KT == 2) {
+        const u32x2 y = at<u32x2>(kp, 8 * lane, 1024 * KL);
+        kt[u][0] = y.x, kt[u][1] = y.y;
+      } else if constexpr (KT == 1) {
+        kt[u][0] = at<uint32_t>(kp, 4 * lane, 1024 * KL);
+      }
     }
     const uint32_t vo = (uint32_t)(4 * g * DH * ES + c * VC * ES);
     const uint32_t vto = (uint32_t)(4 * g * DH * ES + 64 * ES + c * ES);
@@ -127,6 +148,19 @@ struct KvRaw {
       ve[u] = at<uint32_t>(xp, (uint32_t)(4 * g), 0);
     }
   }
+  // Piece i of key c's row lies at piece i ^ swizzle(c), so that 8 keys' pieces i
+  // are in different banks (rows of 80 channels are so by themselves, or nearly).
+  static __device__ __forceinline__ uint32_t swizzle(uint32_t key) { return RP == 4 ? key / 2 % 4 : RP % 8 == 0 ? key % 8 : 0; }
+  // K to the wavefront's LDS, rows side by side
+  __device__ __forceinline__ void stage(char *s_k, int lane) const {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int m = 0; m < KL; ++m) *reinterpret_cast<u32x4 *>(s_k + 16 * RB * u + 1024 * m + 16 * lane) = k[u][m];
+      if constexpr (KT == 2) *reinterpret_cast<u32x2 *>(s_k + 16 * RB * u + 1024 * KL + 8 * lane) = u32x2{kt[u][0], kt[u][1]};
+      else if constexpr (KT == 1) *reinterpret_cast<uint32_t *>(s_k + 16 * RB * u + 1024 * KL + 4 * lane) = kt[u][0];
+    }
+  }
   // V of keys n .. 15 of half u becomes zero (they hold nothing, or another
   // sequence's leavings, which may not even be finite).
   __device__ __forceinline__ void clear(int u, int n, int g) {
@@ -142,20 +176,27 @@ struct KvRaw {
   // K of half u as operands: product n covers the eight channels from chan(n, g)
   // on (the tail's: four, and zeros.  Its own 16-deep instruction is no faster,
   // and following a 32-deep one on the same accumulators gave wrong sums).
-  __device__ __forceinline__ void keys(int u, bf16x8 (&f)[NC]) const {
+  __device__ __forceinline__ void keys(int u, const char *s_k, int c, int g, bf16x8 (&f)[NC]) const {
+    u32x4 k[KQ];
+    u32x2 kt = {this->kt[u][0], this->kt[u][1]};
+    const char *row = s_k + 16 * RB * u + c * RB;
+#pragma unroll
+    for (int m = 0; m < KQ; ++m) k[m] = STAGE ? *reinterpret_cast<const u32x4 *>(row + 16 * ((4 * m + g) ^ swizzle(c))) : this->k[u][m];
+    if constexpr (STAGE && T && W) kt = *reinterpret_cast<const u32x2 *>(row + 128 + 8 * g);
+    if constexpr (STAGE && T && !W) kt.x = *reinterpret_cast<const uint32_t *>(row + 64 + 4 * g);
     if constexpr (W) {
 #pragma unroll
-      for (int n = 0; n < DH / 32; ++n) f[n] = __builtin_bit_cast(bf16x8, k[u][n]);
-      if constexpr (T) f[NC - 1] = __builtin_bit_cast(bf16x8, u32x4{kt[u].x, kt[u].y, 0u, 0u});
+      for (int n = 0; n < DH / 32; ++n) f[n] = __builtin_bit_cast(bf16x8, k[n]);
+      if constexpr (T) f[NC - 1] = __builtin_bit_cast(bf16x8, u32x4{kt.x, kt.y, 0u, 0u});
     } else {
       const float sc = FMT == E4 ? exp_scale(ke[u]) : 1.f;
 #pragma unroll
       for (int n = 0; n < DH / 32; ++n) {
-        const uint32_t a = k[u][n / 2][2 * (n % 2)], b = k[u][n / 2][2 * (n % 2) + 1];
+        const uint32_t a = k[n / 2][2 * (n % 2)], b = k[n / 2][2 * (n % 2) + 1];
         f[n] = __builtin_bit_cast(bf16x8, u32x4{pair(a, sc, 0), pair(a, sc, 1), pair(b, sc, 0), pair(b, sc, 1)});
       }
       if constexpr (T)
-        f[NC - 1] = __builtin_bit_cast(bf16x8, u32x4{pair(kt[u].x, sc, 0), pair(kt[u].x, sc, 1), 0u, 0u});
+        f[NC - 1] = __builtin_bit_cast(bf16x8, u32x4{pair(kt.x, sc, 0), pair(kt.x, sc, 1), 0u, 0u});
     }
   }
   // bytes 2 h, 2 h + 1 of a dword as two bf16 (e4m3: times the scale)
@@ -220,6 +261,9 @@ __device__ __forceinline__ void split(float x, bf16 (&o)[T]) {
     x -= (float)o[i];
   }
 }
+
+template <int FMT, int DH, int RT, typename RowT>
+constexpr bool paged_stage = DH * (FMT == BF ? 2 : 1) > 64 && (RT == 2 || sizeof(RowT) == 4);
 
 // Attention of a block's packed rows [p0, p1) over the pages that each of them
 // looks at, a wavefront per row, 16 keys at a time (lanes 0 .. 15 a key each):
@@ -289,7 +333,8 @@ __device__ __forceinline__ void one_by_one(const PagedAttnArgs &a, const int32_t
 template <int FMT, int DH, int RT, typename RowT, bool SEL>
 __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAttnArgs a,
                                                                          const int32_t *__restrict__ table) {
-  using Raw = KvRaw<FMT, DH>;
+  constexpr bool STAGE = paged_stage<FMT, DH, RT, RowT>;
+  using Raw = KvRaw<FMT, DH, STAGE>;
   constexpr int TERMS = sizeof(RowT) == 4 ? 3 : 1;
   constexpr int NC = Raw::NC, M = Raw::M;
   constexpr int OS = DH + 4;              // row stride of the joined parts
@@ -341,7 +386,8 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   // places in the output (several wavefronts only), then the page bits of the
   // block's rows and the list of pages that any of them looks at
   float *s_o = reinterpret_cast<float *>(smem);             // [waves][RT*16][OS]
-  float *s_m = s_o + (waves > 1 ? waves * RT * 16 * OS : 0);  // [waves][RT*16]
+  char *s_k = reinterpret_cast<char *>(s_o + wave * RT * 16 * OS);  // the wavefront's keys
+  float *s_m = s_o + (waves > 1 ? waves * RT * 16 * OS : STAGE ? 8 * Raw::RB : 0);  // [waves][RT*16]
   float *s_l = s_m + (waves > 1 ? waves * RT * 16 : 0);       // [waves][RT*16]
   int *s_row = reinterpret_cast<int *>(s_l + (waves > 1 ? waves * RT * 16 : 0));  // [RT*16]
   uint32_t *s_bits = reinterpret_cast<uint32_t *>(s_row + (waves > 1 ? RT * 16 : 0));
@@ -494,11 +540,15 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
       // Every step runs over all row tiles before the next begins: their chains
       // of dependent instructions overlap (a lone chain leaves most issue
       // slots empty).
+      if constexpr (STAGE) {
+        raw.stage(s_k, lane);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
       f32x4 s[RT][2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         bf16x8 kf[NC];
-        raw.keys(u, kf);
+        raw.keys(u, s_k, c, g, kf);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) s[rt][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -714,7 +764,7 @@ template <int FMT, int DH, int RT, typename RowT, bool SEL>
 hipError_t launch_paged_attn(const PagedAttnArgs &a, hipStream_t s) {
   constexpr int OS = DH + 4;
   const int words = (a.max_pages + 31) / 32;
-  size_t lds = a.waves > 1 ? ((size_t)a.waves * (RT * 16 * OS + 2 * RT * 16) + RT * 16) * 4 : 0;
+  size_t lds = a.waves > 1 ? ((size_t)a.waves * (RT * 16 * OS + 2 * RT * 16) + RT * 16) * 4 : paged_stage<FMT, DH, RT, RowT> ? 32 * DH * (FMT == BF ? 2 : 1) : 0;
   if (SEL) lds += ((size_t)(a.bit_rows + 1) * words) * 4 + (size_t)words * 64;
   auto kernel = paged_attn_kernel<FMT, DH, RT, RowT, SEL>;
   if (lds > 65536) {
