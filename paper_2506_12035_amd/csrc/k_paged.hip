@@ -795,22 +795,29 @@ int64_t paged_grid(const PagedAttnArgs &a) {
 
 void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
   const int rows = a.q_max * a.group;  // packed rows of a sequence and key head
-  a.row_tiles = rows <= 16 || dt == DType::F32 ? 1 : 2;
-  a.row_blocks = (rows + 16 * a.row_tiles - 1) / (16 * a.row_tiles);
+  // Two 16-row tiles a wavefront share what is loaded (36 .. 100 rows over 32
+  // caches of 1088 bf16 tokens: 46 us, 56 with one); float32 rows have no registers
+  // for them.  Where rows list fewer pages than there are, one tile's rows list
+  // fewer than two tiles': 64 rows of 32 heads, 16 pages of 469: 127 us with
+  // two, 87 with one; where a tile's lists may cover the cache (8 pages of 34) 78
+  // and 85, the selection included.
+  const int tile_rows = (16 + a.group - 2) / a.group + 1;  // rows that have a part in a tile
+  const int64_t cached = ((int64_t)a.len_max + (1 << a.page_log2) - 1) >> a.page_log2;
+  const bool sparse = a.n_select > 0 && cached > (int64_t)a.n_select * tile_rows;
+  a.row_tiles = rows <= 16 || dt == DType::F32 || sparse ? 1 : 2;
+  a.row_blocks = (rows - 1) / (16 * a.row_tiles) + 1;
   const int block_rows = std::min(a.q_max, (16 * a.row_tiles + a.group - 2) / a.group + 1);
   a.bit_rows = block_rows;
   int64_t keys = a.len_max;
   if (a.n_select > 0)
-    keys = std::min<int64_t>((int64_t)((a.len_max + (1 << a.page_log2) - 1) >> a.page_log2),
-                             (int64_t)a.n_select * block_rows)
-           << a.page_log2;
+    keys = std::min(cached, (int64_t)a.n_select * block_rows) << a.page_log2;
   const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32);
   const int64_t units = std::max<int64_t>(1, (int64_t)a.n_seqs * a.n_heads * a.row_blocks);
   // Wavefronts per unit: two for each of the chip's 1024 SIMDs in all, two tiles
   // each at least; beyond a workgroup's, the keys are split over workgroups.
   // More of them repeat the start and the end of a wavefront, some 6 us of
   // latency: with 4096 one row over 32 caches of 1088 tokens (int8, 8 key heads
-  // of 128) takes 24.9 us for 16.4, 36 .. 100 rows over 32 bf16 caches 65.5 for 53.2.
+  // of 128) takes 24.9 us for 16.4, 36 .. 100 rows over 32 bf16 caches 55.6 for 46.4.
   // fp32 rows of several blocks take three times the products a tile, and
   // sequences with fewer blocks than the longest leave some of the units empty:
   // 35.8 us with 4096 for 46.3 (1 .. 333 rows, 6 caches up to 1503 tokens).

@@ -1474,7 +1474,7 @@ marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_
     return fail(MARCHE_ERR_INVALID_ARG, "n_select=%d outside [1, %d]", n_select, PAGED_MAX_PAGES);
   if (pages && max_pages > PAGED_MAX_PAGES)
     return fail(MARCHE_ERR_UNSUPPORTED, "max_pages=%d > %d with selected pages", max_pages, PAGED_MAX_PAGES);
-  const int32_t H = cache->n_heads, dh = cache->head_dim;
+  const int32_t dh = cache->head_dim;
   if ((int64_t)q_total * n_q_heads >= PAGED_MAX_ROWS)
     return fail(MARCHE_ERR_UNSUPPORTED, "q_total*n_q_heads reaches 2^30");
   if (q_total == 0) return MARCHE_OK;

@@ -16,9 +16,18 @@
 // channel per lane where a row of memory has the channels side by side: a lane
 // loads four (head width 128: eight) channels of its eight keys and
 // transposes them among its own registers, one byte permutation per two
-// elements.  Nothing goes through LDS until the wavefronts' parts are joined
-// at the end, so the main loop has no barrier and each wavefront keeps the next
-// tile's loads in flight while it computes.
+// elements.  The main loop has no barrier: a wavefront keeps the next tile's loads
+// in flight while it computes, and meets the others only when their parts are
+// joined at the end.
+//
+// K's operand wants 16 keys side by side in the lanes, whose rows lie apart: read
+// straight from memory each load touches a line per lane.  Where a wavefront
+// has 32 rows or float32 ones, rows of more than 64 bytes are therefore loaded
+// in order, whole lines at a time, and change places in LDS of the wavefront's own
+// (paged_stage; 4 x 16 heads of 64 bf16, 512 rows over 4096 tokens: 90.9 us
+// straight, 65.6 staged; int8 rows of 80, 36 .. 100 rows over 1088 tokens:
+// 62.4, 44.5).  Rows of 64 bytes lose by it (38.7, 39.9), and for 16 rows memory is
+// the bound either way (one row over 64 caches of 4096 tokens: 176.8, 178.6).
 //
 // Softmax statistics and O are float32; the maximum that P is taken against
 // trails the true one by at most 2^8, which saves most rescales.  P is rounded
@@ -26,8 +35,12 @@
 // is exact in bf16 for every format).  float32 rows are split into three bf16
 // parts (24 bits, nothing lost) and so is P.
 //
-// Bound: single rows by the cache's bytes, many rows by the softmax's vector
-// work.
+// Bound: single rows by the cache's bytes (16 long e4m3 caches: 119 us for a
+// copy's rate of 118); many rows by the latency of loads and of dependent instructions
+// at two or three wavefronts a SIMD (100 rows over 32 caches of 1088 bf16
+// tokens: 49 us; with its loads from the caches' nearest levels 37, without them
+// 27, and without its exponentials no less).  Handing page ids and row bits
+// on from tile to tile, or loading two tiles ahead, took no less time.
 #pragma once
 
 #include <algorithm>
@@ -65,8 +78,9 @@ __device__ __forceinline__ V at(const gbyte *p, uint32_t lane_offset, int offset
   return *(const __attribute__((address_space(1))) V *)(p + lane_offset + offset);
 }
 
-// Raw registers of 32 keys of a lane: K for its key c of each half, V for its
-// eight keys, exponent bytes.
+// Raw registers of 32 keys of a lane: K for its key c of each half (STAGE: every
+// 64th piece of the half, in the order of memory), V for its eight keys,
+// exponent bytes.
 template <int FMT, int DH, bool STAGE>
 struct KvRaw {
   static constexpr bool W = FMT == BF;               // 2-byte elements
@@ -74,8 +88,8 @@ struct KvRaw {
   static constexpr int KQ = W ? DH / 32 : DH / 64;   // 16-byte pieces per key and lane
   static constexpr int RB = DH * ES;                 // bytes of a row
   static constexpr int RP = RB / 16;                 // 16-byte pieces of a row
-  static constexpr int KL = RB / 64;                 // 16-byte loads of 16 keys,
-  static constexpr int KT = RB % 64 / 16;            // and dwords of one more
+  static constexpr int KL = RB / 64;                 // whole-line loads of 16 keys: of 16 bytes,
+  static constexpr int KT = RB % 64 / 16;            // and one more of KT dwords
   static constexpr bool T = DH % 32 != 0;            // a 16-channel tail (dh 80)
   static constexpr int NC = DH / 32 + T;             // 32-deep products of S; the tail fills half of one
   static constexpr int VC = DH == 128 ? 8 : 4;       // channels per lane
@@ -111,8 +125,8 @@ struct KvRaw {
       const uint32_t lane = 16 * g + c;
 #pragma unroll
       for (int m = 0; m < KL; ++m) {
-        const uint32_t key = RP == 10 || RP == 5 ? 0 : (64 / RP * m + lane / RP), in = lane % RP;
-        const uint32_t ko = RP == 10 || RP == 5 ? 16 * lane : (key - 64 / RP * m) * RB + 16 * (in ^ swizzle(key));
+        const uint32_t key = 64 / RP * m + lane / RP;  // (rows of 8 or 16 pieces)
+        const uint32_t ko = RP % 8 ? 16 * lane : 16 * (lane ^ swizzle(key));
         k[u][m] = at<u32x4>(kp, ko, 1024 * m);
       }
       if constexpr (KT == 2) {
@@ -148,17 +162,18 @@ struct KvRaw {
       ve[u] = at<uint32_t>(xp, (uint32_t)(4 * g), 0);
     }
   }
-  // Piece i of key c's row lies at piece i ^ swizzle(c), so that 8 keys' pieces i
+  // Piece i of key c's row lies at piece i ^ swizzle(c) in LDS, so that 8 keys' pieces i
   // are in different banks (rows of 80 channels are so by themselves, or nearly).
-  static __device__ __forceinline__ uint32_t swizzle(uint32_t key) { return RP == 4 ? key / 2 % 4 : RP % 8 == 0 ? key % 8 : 0; }
+  static __device__ __forceinline__ uint32_t swizzle(uint32_t key) { return RP % 8 == 0 ? key % 8 : 0; }
   // K to the wavefront's LDS, rows side by side
   __device__ __forceinline__ void stage(char *s_k, int lane) const {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
 #pragma unroll
       for (int m = 0; m < KL; ++m) *reinterpret_cast<u32x4 *>(s_k + 16 * RB * u + 1024 * m + 16 * lane) = k[u][m];
-      if constexpr (KT == 2) *reinterpret_cast<u32x2 *>(s_k + 16 * RB * u + 1024 * KL + 8 * lane) = u32x2{kt[u][0], kt[u][1]};
-      else if constexpr (KT == 1) *reinterpret_cast<uint32_t *>(s_k + 16 * RB * u + 1024 * KL + 4 * lane) = kt[u][0];
+      char *rest = s_k + 16 * RB * u + 1024 * KL;
+      if constexpr (KT == 2) *reinterpret_cast<u32x2 *>(rest + 8 * lane) = u32x2{kt[u][0], kt[u][1]};
+      else if constexpr (KT == 1) *reinterpret_cast<uint32_t *>(rest + 4 * lane) = kt[u][0];
     }
   }
   // V of keys n .. 15 of half u becomes zero (they hold nothing, or another
@@ -181,7 +196,8 @@ struct KvRaw {
     u32x2 kt = {this->kt[u][0], this->kt[u][1]};
     const char *row = s_k + 16 * RB * u + c * RB;
 #pragma unroll
-    for (int m = 0; m < KQ; ++m) k[m] = STAGE ? *reinterpret_cast<const u32x4 *>(row + 16 * ((4 * m + g) ^ swizzle(c))) : this->k[u][m];
+    for (int m = 0; m < KQ; ++m)
+      k[m] = STAGE ? *reinterpret_cast<const u32x4 *>(row + 16 * ((4 * m + g) ^ swizzle(c))) : this->k[u][m];
     if constexpr (STAGE && T && W) kt = *reinterpret_cast<const u32x2 *>(row + 128 + 8 * g);
     if constexpr (STAGE && T && !W) kt.x = *reinterpret_cast<const uint32_t *>(row + 64 + 4 * g);
     if constexpr (W) {
@@ -262,6 +278,7 @@ __device__ __forceinline__ void split(float x, bf16 (&o)[T]) {
   }
 }
 
+// Whether K goes through LDS (the text above).
 template <int FMT, int DH, int RT, typename RowT>
 constexpr bool paged_stage = DH * (FMT == BF ? 2 : 1) > 64 && (RT == 2 || sizeof(RowT) == 4);
 
@@ -382,11 +399,13 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   const int p0 = rb * 16 * RT;
   if (p0 >= packed) return;
 
-  // LDS: joined O parts, maxima and sums of every wavefront and the rows'
-  // places in the output (several wavefronts only), then the page bits of the
-  // block's rows and the list of pages that any of them looks at
+  // LDS: joined O parts (before: the wavefront's staged keys, which need no
+  // more), maxima and sums of every wavefront and the rows' places in the output
+  // (several wavefronts only), then the page bits of the block's rows and the
+  // list of pages that any of them looks at
+  static_assert(32 * Raw::RB <= 16 * OS * 4, "staged keys in the place of O");
   float *s_o = reinterpret_cast<float *>(smem);             // [waves][RT*16][OS]
-  char *s_k = reinterpret_cast<char *>(s_o + wave * RT * 16 * OS);  // the wavefront's keys
+  char *s_k = reinterpret_cast<char *>(s_o + wave * RT * 16 * OS);
   float *s_m = s_o + (waves > 1 ? waves * RT * 16 * OS : STAGE ? 8 * Raw::RB : 0);  // [waves][RT*16]
   float *s_l = s_m + (waves > 1 ? waves * RT * 16 : 0);       // [waves][RT*16]
   int *s_row = reinterpret_cast<int *>(s_l + (waves > 1 ? waves * RT * 16 : 0));  // [RT*16]
@@ -764,7 +783,8 @@ template <int FMT, int DH, int RT, typename RowT, bool SEL>
 hipError_t launch_paged_attn(const PagedAttnArgs &a, hipStream_t s) {
   constexpr int OS = DH + 4;
   const int words = (a.max_pages + 31) / 32;
-  size_t lds = a.waves > 1 ? ((size_t)a.waves * (RT * 16 * OS + 2 * RT * 16) + RT * 16) * 4 : paged_stage<FMT, DH, RT, RowT> ? 32 * DH * (FMT == BF ? 2 : 1) : 0;
+  size_t lds = paged_stage<FMT, DH, RT, RowT> ? 32 * DH * (FMT == BF ? 2 : 1) : 0;
+  if (a.waves > 1) lds = ((size_t)a.waves * (RT * 16 * OS + 2 * RT * 16) + RT * 16) * 4;
   if (SEL) lds += ((size_t)(a.bit_rows + 1) * words) * 4 + (size_t)words * 64;
   auto kernel = paged_attn_kernel<FMT, DH, RT, RowT, SEL>;
   if (lds > 65536) {
