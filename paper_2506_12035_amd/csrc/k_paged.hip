@@ -116,7 +116,7 @@ __device__ __forceinline__ u32x2 pack8(const u32x4 (&x)[NV], int code) {
 // rounding, one 8-byte (16 for bf16) store.  Bound by bytes: each new row is
 // read once and its slot written once.  (Two or four pairs a thread, to find
 // the rows' sequences less often: 59.0 and 64.6 us for 56.4 on 40960 rows of 16
-// heads of 64, bf16 to int8; with STREAM 52.2, 4.8 TB/s.)  STREAM: the rows
+// heads of 64, bf16 to int8; with STREAM 51.3, 4.9 TB/s.)  STREAM: the rows
 // are loaded past the caches, for calls whose rows do not fit them anyway.
 template <int FMT, int DH, typename InT, bool STREAM>
 __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
@@ -272,7 +272,8 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedReadArgs a) {
 // a token and TPW tokens a load, each lane the largest and smallest of its
 // channels over its tokens; the TPW parts are joined by lane swaps at the
 // end.  Bound by bytes and, close behind, by the comparisons: two per key
-// element (two tokens at a time share a three-operand one).  STREAM: keys
+// element (two tokens at a time share a three-operand one); 64 sequences of 1024
+// .. 1088 tokens, 16 heads of 64 in e4m3: 18.1 us, 4.1 TB/s.  STREAM: keys
 // past the caches, where they do not fit them: 29.9 us without, 24.8 with on
 // 142 MB of bf16 keys, but 18.4 without, 19.7 with on 71 MB.
 template <int FMT, int DH, bool STREAM>
@@ -408,6 +409,11 @@ __device__ __forceinline__ uint32_t score_key(float f) {
 // wavefront per row finds the n_select-th largest key by its bits, from the
 // top, and compacts the pages above it (and the first of those equal to it) in
 // ascending order.
+//
+// Bound by latency: row offsets, length, page ids and bounds are loaded one after
+// the other.  8 rows of 32 heads over 512 pages (64 workgroups) 12.1 us, 36 .. 100
+// rows of 16 heads over 34 pages of 32 sequences 17.9 us (the workgroups fill the
+// chip twice); the bounds and queries alone are 1.8 and 1.3 us of bytes.
 template <int DH, typename InT, int KPL>
 __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
   constexpr int ST = (2 * DH + 63) / 64;
@@ -628,7 +634,8 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
 // Joins the key ranges' parts: part s of a row counts exp2(m_s - m) of it, m the
 // largest m_s.  One workgroup per (row, head); each of its four wavefronts
 // holds every part's maximum and sum (lane s part s: there are at most 64) and
-// sums every fourth part, four of them in flight.
+// sums every fourth part, four of them in flight.  Latency alone: 4.7 us for 8
+// rows of 32 heads of 128 in 4 parts, 5.5 us for 16 in up to 64.
 template <int DH, typename RowT>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   constexpr int C = DH == 64 ? 1 : 2;  // channels per lane, C lane + e

@@ -21,7 +21,7 @@
 // joined at the end.
 //
 // K's operand wants 16 keys side by side in the lanes, whose rows lie apart: read
-// straight from memory each load touches a line per lane.  Where a wavefront
+// straight from memory, 16 neighbouring lanes touch 16 lines.  Where a wavefront
 // has 32 rows or float32 ones, rows of more than 64 bytes are therefore loaded
 // in order, whole lines at a time, and change places in LDS of the wavefront's own
 // (paged_stage; 4 x 16 heads of 64 bf16, 512 rows over 4096 tokens: 90.9 us
@@ -35,12 +35,12 @@
 // is exact in bf16 for every format).  float32 rows are split into three bf16
 // parts (24 bits, nothing lost) and so is P.
 //
-// Bound: single rows by the cache's bytes (16 long e4m3 caches: 119 us for a
-// copy's rate of 118); many rows by the latency of loads and of dependent instructions
-// at two or three wavefronts a SIMD (100 rows over 32 caches of 1088 bf16
-// tokens: 49 us; with its loads from the caches' nearest levels 37, without them
-// 27, and without its exponentials no less).  Handing page ids and row bits
-// on from tile to tile, or loading two tiles ahead, took no less time.
+// Bound: single rows by the cache's bytes (16 int8 caches of 4000 .. 32768
+// tokens, 607 MB: 119 us, 118 at a copy's rate); many rows by the latency of
+// loads and of dependent instructions at two or three wavefronts a SIMD (100
+// rows over 32 caches of 1088 bf16 tokens: 49 us; all from the same few pages
+// 36, without loads 27, and without exponentials no less).  Handing page ids and
+// row bits on from tile to tile, or loading two tiles ahead, took no less time.
 #pragma once
 
 #include <algorithm>
