@@ -39,8 +39,8 @@
 // tokens, 607 MB: 119 us, 118 at a copy's rate); many rows by the latency of
 // loads and of dependent instructions at two or three wavefronts a SIMD (100
 // rows over 32 caches of 1088 bf16 tokens: 49 us; all from the same few pages
-// 36, without loads 27, and without exponentials no less).  Handing page ids and
-// row bits on from tile to tile, or loading two tiles ahead, took no less time.
+// 36, without loads 27, and without exponentials no less).  Handing page ids
+// on from tile to tile, or loading two tiles ahead, took no less time.
 #pragma once
 
 #include <algorithm>
@@ -521,6 +521,25 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
     return x;
   };
 
+  // The words that say which rows look at a tile's pages (bit lp & 31), read from
+  // LDS a tile ahead: read where they are used, 36 .. 100 rows over 8 pages each
+  // of 32 x 16 heads of 64, the selection included, take 78 us for 72 (34 bf16
+  // pages), 217 for 187 (63 e4m3 pages).  Two row tiles of 128 bf16 have no
+  // registers for that.
+  constexpr bool AHEAD = SEL && !(FMT == BF && DH == 128 && RT == 2);
+  struct Bits {
+    uint32_t w[RT][2];
+  };
+  auto row_bits = [&](const Tile &x) {
+    Bits b;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      b.w[rt][0] = s_bits[loc[rt] * words + (x.lp[0] >> 5)];
+      b.w[rt][1] = a.page_log2 > 4 ? b.w[rt][0] : s_bits[loc[rt] * words + (x.lp[1] >> 5)];
+    }
+    return b;
+  };
+
   f32x4 acc[RT][M];
   float m_run[RT], l_run[RT];
   bool seen[RT];
@@ -541,6 +560,8 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
     raw.load(0, a.k, a.v, a.k_exp, a.v_exp, x.slot[0], c, g);
     raw.load(1, a.k, a.v, a.k_exp, a.v_exp, x.slot[1], c, g);
     Tile y = t + waves < t1 ? place(t + waves, false) : x;
+    Bits bits, bits_next;
+    if constexpr (AHEAD) bits = row_bits(x);
     while (true) {
       // the next tile's loads, and the page ids of the one after it
       const bool more = t + waves < t1;
@@ -549,6 +570,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
       if (more) {
         next.load(0, a.k, a.v, a.k_exp, a.v_exp, y.slot[0], c, g);
         next.load(1, a.k, a.v, a.k_exp, a.v_exp, y.slot[1], c, g);
+        if constexpr (AHEAD) bits_next = row_bits(y);
         if (t + 2 * waves < t1) z = place(t + 2 * waves, false);
       }
       const bool part = x.n[0] + x.n[1] < 32;
@@ -606,7 +628,10 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           bool look = true;
-          if constexpr (SEL) look = (s_bits[loc[rt] * words + (x.lp[u] >> 5)] >> (x.lp[u] & 31)) & 1u;
+          if constexpr (SEL) {
+            const uint32_t w = AHEAD ? bits.w[rt][u] : s_bits[loc[rt] * words + (x.lp[u] >> 5)];
+            look = (w >> (x.lp[u] & 31)) & 1u;
+          }
           seen[rt] |= look && x.n[u] > 0;
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
@@ -666,6 +691,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
       if (!more) break;
       t += waves;
       raw = next;
+      if constexpr (AHEAD) bits = bits_next;
       x = y;
       y = z;
     }
