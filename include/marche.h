@@ -463,7 +463,7 @@ marche_status_t marche_paged_cache_init(marche_paged_cache_t *cache, int32_t n_l
  * caches: rounded to nearest even).  k_new, v_new: rows of [n_heads][head_dim]
  * elements of `dtype` at distance row_stride, so slices of a fused projection's
  * output will do.  A token at or past max_pages * page_size is not written.
- * a_total * n_heads < 2^31. */
+ * a_total * n_heads < 2^28. */
 marche_status_t marche_paged_write(const marche_paged_cache_t *cache, int32_t layer,
                                    const int32_t *page_table, int32_t max_pages, int32_t n_seqs,
                                    const int32_t *a_idx, const int32_t *a_off, int32_t a_total,
@@ -472,7 +472,8 @@ marche_status_t marche_paged_write(const marche_paged_cache_t *cache, int32_t la
 
 /* Reads cached tokens back in the resident layout of marche_attention_segments:
  * k_out, v_out [n_seqs][n_heads][n_tokens][head_dim] of `dtype`, tokens
- * j < min(lens[b], n_tokens) written, the others left as they are. */
+ * j < min(lens[b], n_tokens) written, the others left as they are.
+ * n_seqs * n_heads * ceil(n_tokens / 128) < 2^24. */
 marche_status_t marche_paged_read(const marche_paged_cache_t *cache, int32_t layer,
                                   const int32_t *page_table, int32_t max_pages,
                                   const int32_t *lens, int32_t n_seqs, int32_t n_tokens,
@@ -488,7 +489,7 @@ marche_status_t marche_paged_read(const marche_paged_cache_t *cache, int32_t lay
  * span = 1; after rows written anywhere, first NULL and span = max_pages (a
  * negative first[b] counts as 0).  A page that several sequences share gets the
  * bounds of one of them: it should lie below lens for all of them.
- * n_seqs * span * n_heads < 2^31.  Needs cache->bounds. */
+ * n_seqs * span * n_heads < 2^26.  Needs cache->bounds. */
 marche_status_t marche_paged_bounds(const marche_paged_cache_t *cache, int32_t layer,
                                     const int32_t *page_table, int32_t max_pages,
                                     const int32_t *lens, const int32_t *first, int32_t span,
@@ -504,7 +505,8 @@ marche_status_t marche_paged_bounds(const marche_paged_cache_t *cache, int32_t l
  * query or a key that is not finite) ranks below every number.  Logical pages are written in ascending
  * order to pages[r][head][0 .. n_select), then -1 where the sequence has fewer.
  * q: rows of [n_q_heads][head_dim], q_stride apart.  1 <= n_select,
- * max_pages <= 4096; q_total * n_q_heads < 2^30.  Needs cache->bounds, up to date for every page below lens. */
+ * max_pages <= 4096; q_total * n_q_heads < 2^30, less where a launch of 2^32 threads would
+ * not do (UNSUPPORTED).  Needs cache->bounds, up to date for every page below lens. */
 marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t layer,
                                     const int32_t *page_table, int32_t max_pages,
                                     const int32_t *lens, int32_t n_seqs, const void *q,
@@ -523,7 +525,7 @@ marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t l
  * parts joined, so a row's rounding may depend on the sizes of its call.
  * q_max is the largest number of rows of a sequence and len_max the largest
  * length (host copies, for launch geometry, and preconditions as the lists
- * are; q_total * n_q_heads < 2^30).  The weighted sum is float32 and divided by
+ * are; q_total * n_q_heads < 2^30, with the same exception).  The weighted sum is float32 and divided by
  * the weights' sum last: values near 2^128 / (256 * tokens) may overflow in it.  o: [q_total][n_q_heads * head_dim].
  * pages NULL: n_select is 0.  With pages: max_pages <= 4096.  workspace:
  * marche_paged_attention_workspace_bytes, 256-byte aligned (may be 0 bytes;

@@ -767,23 +767,27 @@ hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, PagedBoundsArgs
   });
 }
 
-hipError_t launch_paged_select(DType dt, int32_t head_dim, PagedSelectArgs a, hipStream_t s) {
-  if (a.q_total == 0) return hipSuccess;
+int64_t paged_select_grid(PagedSelectArgs &a) {
   a.p_cap = (a.max_pages + 63) / 64 * 64;
   // consecutive rows that a sequence is likely to own, as far as they fit the
   // 16 columns and their keys 32 KB of LDS
   const int mean = (int)(((int64_t)a.q_total + a.n_seqs - 1) / a.n_seqs);
   a.rows_per = std::max(1, std::min({16 / a.group, 8192 / a.p_cap, mean}));
-  const unsigned grid = (unsigned)(((int64_t)a.q_total + a.rows_per - 1) / a.rows_per * a.n_heads);
   // a wavefront per two tiles of 16 pages, or per four rows where that is more
   // (two at least: one finds the rows' sequences, another quantises)
-  const int waves = std::min(16, std::max({2, (a.max_pages + 31) / 32, (a.rows_per + 3) / 4}));
+  a.waves = std::min(16, std::max({2, (a.max_pages + 31) / 32, (a.rows_per + 3) / 4}));
+  return ((int64_t)a.q_total + a.rows_per - 1) / a.rows_per * a.n_heads;
+}
+
+hipError_t launch_paged_select(DType dt, int32_t head_dim, const PagedSelectArgs &a, int64_t grid,
+                               hipStream_t s) {
+  const dim3 g((unsigned)grid), b(64 * a.waves);
   const uint32_t lds = (uint32_t)a.rows_per * a.p_cap * 4;
   return by_shape(BF, head_dim, [&](auto, auto dh) {
     auto go = [&](auto kpl) {
       constexpr int K = kpl.value;
-      if (dt == DType::BF16) launch_kernel(paged_select_kernel<dh.value, bf16, K>, grid, 64 * waves, lds, s, a);
-      else launch_kernel(paged_select_kernel<dh.value, float, K>, grid, 64 * waves, lds, s, a);
+      if (dt == DType::BF16) launch_kernel(paged_select_kernel<dh.value, bf16, K>, g, b, lds, s, a);
+      else launch_kernel(paged_select_kernel<dh.value, float, K>, g, b, lds, s, a);
     };
     // keys per lane of a row's wavefront: the fewest that hold max_pages
     const int kpl = a.p_cap / 64;
@@ -803,11 +807,11 @@ int64_t paged_grid(const PagedAttnArgs &a) {
 void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
   const int rows = a.q_max * a.group;  // packed rows of a sequence and key head
   // Two 16-row tiles a wavefront share what is loaded (36 .. 100 rows over 32
-  // caches of 1088 bf16 tokens: 46 us, 56 with one); float32 rows have no registers
+  // caches of 1088 bf16 tokens: 46 us, 69 with one); float32 rows have no registers
   // for them.  Where rows list fewer pages than there are, one tile's rows list
-  // fewer than two tiles': 64 rows of 32 heads, 16 pages of 469: 127 us with
-  // two, 87 with one; where a tile's lists may cover the cache (8 pages of 34) 78
-  // and 85, the selection included.
+  // fewer than two tiles': 64 rows of 32 heads, 16 pages of 469: 128 us with
+  // two, 86 with one; where a tile's lists may cover the cache (8 pages of 34) 72
+  // and 88, the selection included.
   const int tile_rows = (16 + a.group - 2) / a.group + 1;  // rows that have a part in a tile
   const int64_t cached = ((int64_t)a.len_max + (1 << a.page_log2) - 1) >> a.page_log2;
   const bool sparse = a.n_select > 0 && cached > (int64_t)a.n_select * tile_rows;

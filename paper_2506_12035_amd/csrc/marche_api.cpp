@@ -1268,8 +1268,8 @@ marche_status_t marche_paged_write(const marche_paged_cache_t *cache, int32_t la
   if (st != MARCHE_OK || (st = check_row_dtype(dtype)) != MARCHE_OK) return st;
   const int32_t H = cache->n_heads, dh = cache->head_dim;
   if ((st = check_rows("a", a_total, a_off, n_seqs, row_stride, (int64_t)H * dh)) != MARCHE_OK) return st;
-  if ((int64_t)a_total * H >= (1LL << 31))
-    return fail(MARCHE_ERR_UNSUPPORTED, "a_total*n_heads reaches 2^31");
+  if ((int64_t)a_total * H >= (1LL << 28))
+    return fail(MARCHE_ERR_UNSUPPORTED, "a_total*n_heads reaches 2^28");
   if (a_total == 0) return MARCHE_OK;
   if (!page_table || !a_idx || !k_new || !v_new)
     return fail(MARCHE_ERR_INVALID_ARG, "NULL input to marche_paged_write");
@@ -1303,8 +1303,8 @@ marche_status_t marche_paged_read(const marche_paged_cache_t *cache, int32_t lay
   if (st != MARCHE_OK || (st = check_row_dtype(dtype)) != MARCHE_OK) return st;
   const int32_t H = cache->n_heads, dh = cache->head_dim;
   if (n_tokens < 0) return fail(MARCHE_ERR_INVALID_ARG, "n_tokens=%d < 0", n_tokens);
-  if ((int64_t)n_seqs * H * ((n_tokens + PAGED_READ_TOKENS - 1LL) / PAGED_READ_TOKENS) >= (1LL << 31))
-    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs*n_heads*n_tokens too large");
+  if ((double)n_seqs * H * (((int64_t)n_tokens + PAGED_READ_TOKENS - 1) / PAGED_READ_TOKENS) >= 0x1p24)
+    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs*n_heads*ceil(n_tokens/%d) reaches 2^24", PAGED_READ_TOKENS);
   if (n_seqs == 0 || n_tokens == 0) return MARCHE_OK;
   if (!page_table || !lens || !k_out || !v_out)
     return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_read");
@@ -1337,8 +1337,8 @@ marche_status_t marche_paged_bounds(const marche_paged_cache_t *cache, int32_t l
   if (!l.bounds) return fail(MARCHE_ERR_INVALID_ARG, "the cache has no bounds");
   if (span < 0) return fail(MARCHE_ERR_INVALID_ARG, "span=%d < 0", span);
   span = std::min(span, max_pages);
-  if ((int64_t)n_seqs * span * cache->n_heads >= (1LL << 31))
-    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs*span*n_heads reaches 2^31");
+  if ((double)n_seqs * span * cache->n_heads >= 0x1p26)
+    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs*span*n_heads reaches 2^26");
   if (n_seqs == 0 || span == 0) return MARCHE_OK;
   if (!page_table || !lens) return fail(MARCHE_ERR_INVALID_ARG, "NULL input to marche_paged_bounds");
   hipStream_t stream = static_cast<hipStream_t>(stream_);
@@ -1391,6 +1391,16 @@ marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t l
   if ((int64_t)q_total * n_q_heads >= PAGED_MAX_ROWS)
     return fail(MARCHE_ERR_UNSUPPORTED, "q_total*n_q_heads reaches 2^30");
   if (q_total == 0) return MARCHE_OK;
+  const int32_t H = cache->n_heads, dh = cache->head_dim;
+  PagedSelectArgs a{};
+  a.n_heads = H;
+  a.max_pages = max_pages;
+  a.n_seqs = n_seqs;
+  a.q_total = q_total;
+  a.group = n_q_heads / H;
+  const int64_t grid = paged_select_grid(a);
+  if (grid >= PAGED_MAX_THREADS / (64 * a.waves))
+    return fail(MARCHE_ERR_UNSUPPORTED, "q_total=%d rows are too many for one call", q_total);
   if (!page_table || !lens || !q || !pages)
     return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_select");
   if (misaligned(q)) return fail(MARCHE_ERR_INVALID_ARG, "q must be 16-byte aligned");
@@ -1403,8 +1413,6 @@ marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t l
   lists.max_pages = max_pages;
   lists.total = lists.row_max = q_total;
   if ((st = validate_paged(lists, cache, stream)) != MARCHE_OK) return st;
-  const int32_t H = cache->n_heads, dh = cache->head_dim;
-  PagedSelectArgs a{};
   a.bounds = l.bounds;
   a.bounds_exp = l.bounds_exp;
   a.table = page_table;
@@ -1414,19 +1422,14 @@ marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t l
   a.pages = pages;
   a.q_stride = q_stride;
   a.n_pages = cache->n_pages;
-  a.n_heads = H;
   a.page_log2 = l.page_log2;
-  a.max_pages = max_pages;
-  a.n_seqs = n_seqs;
-  a.q_total = q_total;
   a.rows_each = q_total / n_seqs;
-  a.group = n_q_heads / H;
   a.n_select = n_select;
   // Algorithmic work and traffic as if every sequence had max_pages pages.
   LAUNCH(K_PAGED_SELECT, 4.0 * q_total * (double)n_q_heads * dh * max_pages,
          (double)n_seqs * max_pages * (H * (2.0 * dh + 1) + 4) +
              (double)q_total * ((double)n_q_heads * dh * elem_size(dtype) + 4.0 * H * n_select),
-         launch_paged_select(dtype == MARCHE_BF16 ? DType::BF16 : DType::F32, dh, a, stream));
+         launch_paged_select(dtype == MARCHE_BF16 ? DType::BF16 : DType::F32, dh, a, grid, stream));
   return MARCHE_OK;
 }
 
@@ -1482,8 +1485,8 @@ marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_
   PagedAttnArgs a{};
   a.max_pages = max_pages;
   paged_attn_sizes(a, cache, n_seqs, q_total, q_max, n_q_heads, len_max, n_select, dt);
-  if (paged_grid(a) >= (1LL << 31))
-    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs*n_heads*rows too large");
+  if (paged_grid(a) >= PAGED_MAX_THREADS / (64 * a.waves))
+    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs=%d sequences of up to q_max=%d rows are too many for one call", n_seqs, q_max);
   if (!page_table || !lens || !q || !o)
     return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_attention");
   if (misaligned(q) || misaligned(o)) return fail(MARCHE_ERR_INVALID_ARG, "q and o must be 16-byte aligned");

@@ -295,6 +295,7 @@ struct PagedBoundsArgs {
   FastDiv d_heads, d_span;  // set by the launch
 };
 hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, PagedBoundsArgs a, hipStream_t s);
+constexpr int64_t PAGED_MAX_THREADS = 1LL << 32;  // of a launch
 constexpr int64_t PAGED_MAX_ROWS = 1 << 30;  // rows of queries times their heads
 constexpr int PAGED_MAX_PAGES = 4096;  // pages of a sequence, where pages are selected
 struct PagedSelectArgs {
@@ -305,9 +306,12 @@ struct PagedSelectArgs {
   int32_t *pages;
   int64_t q_stride;
   int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, q_total, rows_each, group, n_select;
-  int32_t rows_per, p_cap;  // set by the launch: rows per workgroup, keys per row in LDS
+  int32_t rows_per, p_cap, waves;  // paged_select_grid: rows per workgroup, keys per row in LDS, wavefronts
 };
-hipError_t launch_paged_select(DType dt, int32_t head_dim, PagedSelectArgs a, hipStream_t s);
+// Fills these and returns the workgroups of the launch.
+int64_t paged_select_grid(PagedSelectArgs &a);
+hipError_t launch_paged_select(DType dt, int32_t head_dim, const PagedSelectArgs &a, int64_t grid,
+                               hipStream_t s);
 constexpr int PAGED_MAX_SHARED = 256;  // sequences of a call whose ranges are shared out on the device
 struct PagedAttnArgs {
   const void *k, *v;

@@ -109,6 +109,7 @@ def test_write_refusals():
     for name in ("k", "v"):
         assert _write(**{name: FAKE + 8}) == INVALID and "aligned" in binding.last_error()
     assert _write(total=1 << 29) == UNSUPPORTED  # 2^29 rows of 4 heads
+    assert _write(total=1 << 26) == UNSUPPORTED and "2^28" in binding.last_error()
     assert _write(total=0) == OK
     assert _write(total=0, n_seqs=0) == OK
     # a bf16 cache has no exponents, a cache that is only written no bounds
@@ -122,6 +123,8 @@ def test_read_refusals():
         assert _read(**{name: None}) == INVALID
     assert _read(k=FAKE + 2) == INVALID and "aligned" in binding.last_error()
     assert _read(n_seqs=1 << 16, n=1 << 24) == UNSUPPORTED
+    assert _read(n_seqs=1 << 22, n=1) == UNSUPPORTED and "2^24" in binding.last_error()
+    assert _read(n_seqs=2147483647, n=2147483647) == UNSUPPORTED
     assert _read(n=0) == OK and _read(n_seqs=0) == OK
 
 
@@ -130,6 +133,9 @@ def test_bounds_refusals():
     assert _bounds(span=-1) == INVALID and "span" in binding.last_error()
     assert _bounds(lens=None) == INVALID
     assert _bounds(n_seqs=1 << 25, max_pages=1 << 20, span=1 << 20) == UNSUPPORTED
+    assert _bounds(n_seqs=1 << 24, span=1) == UNSUPPORTED and "2^26" in binding.last_error()
+    assert _bounds(_cache(n_heads=65535, n_pages=4, page_size=16), n_seqs=2147483647, max_pages=2147483647,
+                   span=2147483647) == UNSUPPORTED
     assert _bounds(span=0) == OK and _bounds(n_seqs=0) == OK
 
 
@@ -148,6 +154,7 @@ def test_select_refusals():
     assert _select(q=FAKE + 4) == INVALID
     assert _select(total=1 << 28) == UNSUPPORTED
     assert _select(total=1 << 27) == UNSUPPORTED and "2^30" in binding.last_error()
+    assert _select(total=1 << 24, max_pages=4096) == UNSUPPORTED and "too many" in binding.last_error()
     assert _select(total=0) == OK
 
 
@@ -167,6 +174,7 @@ def test_attention_refusals():
         assert _attend(**{name: None}) == INVALID
     assert _attend(q=FAKE + 8) == INVALID and _attend(o=FAKE + 8) == INVALID
     assert _attend(ws=FAKE + 64, ws_bytes=1 << 30) == INVALID
+    assert _attend(total=1 << 22, q_max=1 << 22, n_seqs=8192, heads=4, stride=256) == UNSUPPORTED and "too many" in binding.last_error()
     assert _attend(total=1 << 27) == UNSUPPORTED and "2^30" in binding.last_error()
     assert _attend(total=0, q_max=0) == OK
 
