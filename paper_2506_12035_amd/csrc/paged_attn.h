@@ -522,11 +522,14 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   };
 
   // The words that say which rows look at a tile's pages (bit lp & 31), read from
-  // LDS a tile ahead: read where they are used, 36 .. 100 rows over 8 pages each
-  // of 32 x 16 heads of 64, the selection included, take 78 us for 72 (34 bf16
-  // pages), 217 for 187 (63 e4m3 pages).  Two row tiles of 128 bf16 have no
-  // registers for that.
-  constexpr bool AHEAD = SEL && !(FMT == BF && DH == 128 && RT == 2);
+  // LDS a tile ahead by two row tiles: read where they are used, 36 .. 100 rows
+  // over 8 pages each of 32 x 16 heads of 64, the selection included, take 78 us
+  // for 72 (34 bf16 pages), 217 for 187 (63 e4m3 pages).  One row tile has the same
+  // latency once and more wavefronts to hide it, and the words' registers cost
+  // more (20 .. 60 fp32 rows over 8 of 34 int8 pages, 16 x 16 heads of 80: 60.1 us
+  // ahead, 53.2 in place; one row of 32 heads over 32 of 512 pages 27.4 and 26.6).
+  // Two row tiles of 128 bf16 have no registers for them.
+  constexpr bool AHEAD = SEL && RT == 2 && !(FMT == BF && DH == 128);
   struct Bits {
     uint32_t w[RT][2];
   };
