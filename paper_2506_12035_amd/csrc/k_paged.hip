@@ -389,7 +389,8 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
 // ------------------------------------------------------------------ select
 
 // Order-preserving image of a score that is no NaN: larger score, larger value;
-// -0 ties with +0; never 0.
+// -0 ties with +0; at least 0x7FFFFF (-infinity).
+constexpr uint32_t NAN_KEY = 1;  // below every number's, above "no page" (0)
 __device__ __forceinline__ uint32_t score_key(float f) {
   if (f == 0.0f) f = 0.0f;
   const uint32_t u = __float_as_uint(f);
@@ -542,7 +543,7 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
             // lane's page 4 g + j: its exponent sits in lane 4 g + j
             const int e = __shfl(be[t], 4 * g + j, 64) + qe;
             const float score = __builtin_amdgcn_ldexpf((float)acc[j], e);
-            const uint32_t key = score_key(e < NOT_FINITE / 2 ? score : -INFINITY);
+            const uint32_t key = e < NOT_FINITE / 2 ? score_key(score) : NAN_KEY;
             const int p = pt + 4 * g + j;
             if (mine && p < n_p) {
               uint32_t *to = &s_key[i * a.p_cap + p];
