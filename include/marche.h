@@ -463,7 +463,7 @@ marche_status_t marche_paged_cache_init(marche_paged_cache_t *cache, int32_t n_l
  * caches: rounded to nearest even).  k_new, v_new: rows of [n_heads][head_dim]
  * elements of `dtype` at distance row_stride, so slices of a fused projection's
  * output will do.  A token at or past max_pages * page_size is not written.
- * a_total * n_heads < 2^28. */
+ * a_total * n_heads < 2^28, for head_dim 80 and 128 <= 2^28 - 16. */
 marche_status_t marche_paged_write(const marche_paged_cache_t *cache, int32_t layer,
                                    const int32_t *page_table, int32_t max_pages, int32_t n_seqs,
                                    const int32_t *a_idx, const int32_t *a_off, int32_t a_total,
@@ -489,7 +489,7 @@ marche_status_t marche_paged_read(const marche_paged_cache_t *cache, int32_t lay
  * span = 1; after rows written anywhere, first NULL and span = max_pages (a
  * negative first[b] counts as 0).  A page that several sequences share gets the
  * bounds of one of them: it should lie below lens for all of them.
- * n_seqs * span * n_heads < 2^26.  Needs cache->bounds. */
+ * n_seqs * span * n_heads <= 2^26 - 4.  Needs cache->bounds. */
 marche_status_t marche_paged_bounds(const marche_paged_cache_t *cache, int32_t layer,
                                     const int32_t *page_table, int32_t max_pages,
                                     const int32_t *lens, const int32_t *first, int32_t span,

@@ -120,7 +120,7 @@ __device__ __forceinline__ u32x2 pack8(const u32x4 (&x)[NV], int code) {
 // are loaded past the caches, for calls whose rows do not fit them anyway.
 template <int FMT, int DH, typename InT, bool STREAM>
 __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
-  constexpr int GROUP = DH == 64 ? 8 : 16, PER = 256 / GROUP;
+  constexpr int PER = paged_write_pairs(DH), GROUP = 256 / PER;
   constexpr int NV = sizeof(InT) == 4 ? 2 : 1;  // 16-byte loads of 8 elements
   __shared__ int s_b0;
   const int tid = threadIdx.x, lane = tid & 63, c = tid % GROUP;
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
   constexpr int LPT = DH / 4, TPW = 64 / LPT, ES = FMT == BF ? 2 : 1;
   using In = std::conditional_t<FMT == BF, u32x2, uint32_t>;
   const int lane = threadIdx.x & 63;
-  const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // below 2^31
+  const uint32_t unit = blockIdx.x * PAGED_BOUNDS_PAIRS + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // below 2^31
   const uint32_t bp = a.d_heads.div(unit);
   const int h = unit - bp * a.n_heads, b = a.d_span.div(bp);
   if (b >= a.n_seqs) return;
@@ -638,7 +638,7 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
 // sums every fourth part, four of them in flight.  Latency alone: 4.7 us for 8
 // rows of 32 heads of 128 in 4 parts, 5.5 us for 16 in up to 64.
 template <int DH, typename RowT>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(PAGED_JOIN_THREADS) void paged_join_kernel(PagedAttnArgs a) {
   constexpr int C = DH == 64 ? 1 : 2;  // channels per lane, C lane + e
   __shared__ float s_sum[4][2 * 64];
   const int lane = threadIdx.x & 63;
@@ -721,7 +721,7 @@ hipError_t launch_paged_write(DType dt, int32_t format, int32_t head_dim, PagedW
   if (a.a_total == 0) return hipSuccess;
   a.d_heads = FastDiv::of(a.n_heads);
   a.d_rows = FastDiv::of(std::max(1, a.rows_each));
-  const int per = 256 / (head_dim == 64 ? 8 : 16);
+  const int per = paged_write_pairs(head_dim);
   const unsigned grid = (unsigned)(((int64_t)a.a_total * a.n_heads + per - 1) / per);
   // Rows of 64 MB and more are loaded past the caches.  Smaller ones may still
   // lie there from the product that made them: 10.7 us streamed for 9.6 on 20 MB.
@@ -759,7 +759,7 @@ hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, PagedBoundsArgs
   if (a.n_seqs == 0 || a.span == 0) return hipSuccess;
   a.d_heads = FastDiv::of(a.n_heads);
   a.d_span = FastDiv::of(a.span);
-  const unsigned grid = (unsigned)(((int64_t)a.n_seqs * a.n_heads * a.span + 3) / 4);
+  const unsigned grid = (unsigned)(((int64_t)a.n_seqs * a.n_heads * a.span + PAGED_BOUNDS_PAIRS - 1) / PAGED_BOUNDS_PAIRS);
   const double keys = (double)a.n_seqs * a.span * a.n_heads * head_dim * (format == BF ? 2 : 1);
   const bool stream = keys * (1 << a.page_log2) >= 128e6;
   return by_shape(format, head_dim, [&](auto fmt, auto dh) {
@@ -873,8 +873,8 @@ hipError_t launch_paged_attention(DType dt, int32_t format, int32_t head_dim, co
 hipError_t launch_paged_join(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)a.q_total * a.n_heads * a.group);
   return by_shape(BF, head_dim, [&](auto, auto dh) {
-    if (dt == DType::BF16) launch_kernel(paged_join_kernel<dh.value, bf16>, grid, 256, 0, s, a);
-    else launch_kernel(paged_join_kernel<dh.value, float>, grid, 256, 0, s, a);
+    if (dt == DType::BF16) launch_kernel(paged_join_kernel<dh.value, bf16>, grid, PAGED_JOIN_THREADS, 0, s, a);
+    else launch_kernel(paged_join_kernel<dh.value, float>, grid, PAGED_JOIN_THREADS, 0, s, a);
   });
 }
 

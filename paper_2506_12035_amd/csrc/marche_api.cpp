@@ -1123,6 +1123,9 @@ marche_status_t check_rows(const char *what, int32_t total, const int32_t *off, 
   return MARCHE_OK;
 }
 
+// Whether `n` units, `per` to a workgroup of 256 threads, are too many for a launch.
+bool too_many_threads(int64_t n, int64_t per) { return (n + per - 1) / per * 256 >= PAGED_MAX_THREADS; }
+
 bool misaligned(const void *p) { return reinterpret_cast<uintptr_t>(p) & 15; }
 
 // MARCHE_VALIDATE: the device lists of a call, copied to the host.
@@ -1212,6 +1215,12 @@ void paged_attn_sizes(PagedAttnArgs &p, const marche_paged_cache_t *c, int32_t n
   paged_plan(dt, c->head_dim, p);
 }
 
+// Whether the plan's launches stay below the largest.
+bool paged_launchable(const PagedAttnArgs &p) {
+  return paged_grid(p) < PAGED_MAX_THREADS / (64 * p.waves) &&
+         (p.splits == 1 || (int64_t)p.q_total * p.n_heads * p.group < PAGED_MAX_THREADS / PAGED_JOIN_THREADS);
+}
+
 size_t paged_part_rows(const PagedAttnArgs &p) {
   return p.splits > 1 ? (size_t)p.splits * p.q_total * p.n_heads * p.group : 0;
 }
@@ -1268,8 +1277,9 @@ marche_status_t marche_paged_write(const marche_paged_cache_t *cache, int32_t la
   if (st != MARCHE_OK || (st = check_row_dtype(dtype)) != MARCHE_OK) return st;
   const int32_t H = cache->n_heads, dh = cache->head_dim;
   if ((st = check_rows("a", a_total, a_off, n_seqs, row_stride, (int64_t)H * dh)) != MARCHE_OK) return st;
-  if ((int64_t)a_total * H >= (1LL << 28))
-    return fail(MARCHE_ERR_UNSUPPORTED, "a_total*n_heads reaches 2^28");
+  // (workgroups are whole: the last few pairs below 2^28 of wide heads make 2^32 threads)
+  if ((int64_t)a_total * H >= (1LL << 28) || too_many_threads((int64_t)a_total * H, paged_write_pairs(dh)))
+    return fail(MARCHE_ERR_UNSUPPORTED, "a_total*n_heads reaches 2^28, or all but");
   if (a_total == 0) return MARCHE_OK;
   if (!page_table || !a_idx || !k_new || !v_new)
     return fail(MARCHE_ERR_INVALID_ARG, "NULL input to marche_paged_write");
@@ -1337,8 +1347,9 @@ marche_status_t marche_paged_bounds(const marche_paged_cache_t *cache, int32_t l
   if (!l.bounds) return fail(MARCHE_ERR_INVALID_ARG, "the cache has no bounds");
   if (span < 0) return fail(MARCHE_ERR_INVALID_ARG, "span=%d < 0", span);
   span = std::min(span, max_pages);
-  if ((double)n_seqs * span * cache->n_heads >= 0x1p26)
-    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs*span*n_heads reaches 2^26");
+  if ((double)n_seqs * span * cache->n_heads >= 0x1p26 ||
+      too_many_threads((int64_t)n_seqs * span * cache->n_heads, PAGED_BOUNDS_PAIRS))
+    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs*span*n_heads exceeds 2^26 - 4");
   if (n_seqs == 0 || span == 0) return MARCHE_OK;
   if (!page_table || !lens) return fail(MARCHE_ERR_INVALID_ARG, "NULL input to marche_paged_bounds");
   hipStream_t stream = static_cast<hipStream_t>(stream_);
@@ -1447,6 +1458,7 @@ size_t marche_paged_attention_workspace_bytes(const marche_paged_cache_t *cache,
   for (DType dt : {DType::BF16, DType::F32}) {  // either type of rows
     PagedAttnArgs p{};
     paged_attn_sizes(p, cache, n_seqs, q_total, q_max, n_q_heads, len_max, n_select, dt);
+    if (!paged_launchable(p)) continue;
     const size_t rows = paged_part_rows(p);
     need = std::max(need, align256(rows * cache->head_dim * 4) + align256(rows * 8));
   }
@@ -1485,8 +1497,9 @@ marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_
   PagedAttnArgs a{};
   a.max_pages = max_pages;
   paged_attn_sizes(a, cache, n_seqs, q_total, q_max, n_q_heads, len_max, n_select, dt);
-  if (paged_grid(a) >= PAGED_MAX_THREADS / (64 * a.waves))
-    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs=%d sequences of up to q_max=%d rows are too many for one call", n_seqs, q_max);
+  if (!paged_launchable(a))
+    return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs=%d sequences of up to q_max=%d rows, q_total=%d, are too many for one call",
+                n_seqs, q_max, q_total);
   if (!page_table || !lens || !q || !o)
     return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_attention");
   if (misaligned(q) || misaligned(o)) return fail(MARCHE_ERR_INVALID_ARG, "q and o must be 16-byte aligned");

@@ -273,6 +273,8 @@ struct PagedWriteArgs {
   int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, a_total, rows_each;
   FastDiv d_heads, d_rows;  // set by the launch
 };
+// (row, head) pairs of a workgroup of 256 threads
+constexpr int paged_write_pairs(int32_t head_dim) { return head_dim == 64 ? 32 : 16; }
 hipError_t launch_paged_write(DType dt, int32_t format, int32_t head_dim, PagedWriteArgs a,
                               hipStream_t s);
 constexpr int PAGED_READ_TOKENS = 128;  // tokens per workgroup of the read kernel
@@ -294,6 +296,7 @@ struct PagedBoundsArgs {
   int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, span;
   FastDiv d_heads, d_span;  // set by the launch
 };
+constexpr int PAGED_BOUNDS_PAIRS = 4;  // (page, head) pairs of a workgroup of 256 threads
 hipError_t launch_paged_bounds(int32_t format, int32_t head_dim, PagedBoundsArgs a, hipStream_t s);
 constexpr int64_t PAGED_MAX_THREADS = 1LL << 32;  // of a launch
 constexpr int64_t PAGED_MAX_ROWS = 1 << 30;  // rows of queries times their heads
@@ -312,6 +315,7 @@ struct PagedSelectArgs {
 int64_t paged_select_grid(PagedSelectArgs &a);
 hipError_t launch_paged_select(DType dt, int32_t head_dim, const PagedSelectArgs &a, int64_t grid,
                                hipStream_t s);
+constexpr int PAGED_JOIN_THREADS = 256;  // of the join's workgroup, one per (row, query head)
 constexpr int PAGED_MAX_SHARED = 256;  // sequences of a call whose ranges are shared out on the device
 struct PagedAttnArgs {
   const void *k, *v;
