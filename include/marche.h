@@ -449,7 +449,7 @@ marche_status_t marche_paged_cache_init(marche_paged_cache_t *cache, int32_t n_l
  *   rows in CSR form as marche_step's active lists: sequence b owns rows
  *     off[b] .. off[b+1] (device; NULL: every sequence owns total / n_seqs rows,
  *     which must divide evenly).  Rows that belong to no sequence are
- *     neither read nor written.
+ *     neither read nor written (those behind the last sequence's need not be there).
  * dtype is the type of the rows outside the cache (queries, outputs, new keys
  * and values): MARCHE_F32 or MARCHE_BF16.  Strides count elements between
  * consecutive rows, are at least a row's length and a multiple of 8;

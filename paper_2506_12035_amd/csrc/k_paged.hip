@@ -126,8 +126,10 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, c = tid % GROUP;
   const uint32_t u0 = blockIdx.x * PER, unit = u0 + tid / GROUP;  // pairs are below 2^31
   const int r = (int)a.d_heads.div(unit), h = (int)(unit - (uint32_t)r * a.n_heads);
-  const bool on = r < a.a_total && c < DH / 8;
-  const int rr = r < a.a_total ? r : 0;
+  const RowRange own(a.a_off, a.n_seqs, a.a_total);
+  if (own.none()) return;
+  const int rr = own.nearest(r);  // (what is loaded for others is not used)
+  const bool on = r == rr && c < DH / 8;
 
   // the values and the token, in flight while the row's sequence is found
   u32x4 kx[NV], vx[NV];
@@ -144,7 +146,6 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
   const int tok = a.a_idx[rr];
   int b;
   if (a.a_off) {
-    const int first = a.a_off[0];
     if (tid < 64) {
       const int f = wave_find_seq(a.a_off, a.n_seqs, min((int)a.d_heads.div(u0), a.a_total - 1), lane);
       if (tid == 0) s_b0 = f;
@@ -152,7 +153,6 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
     __syncthreads();
     b = s_b0;  // of the workgroup's first row; on from there
     while (b < a.n_seqs && a.a_off[b + 1] <= rr) ++b;
-    if (rr < first) b = a.n_seqs;
   } else {
     b = (int)a.d_rows.div((uint32_t)rr);
   }
@@ -434,6 +434,9 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
   const int r0 = (blockIdx.x / a.n_heads) * a.rows_per;
   const int rows = min(a.rows_per, a.q_total - r0), cols = rows * a.group;
 
+  const RowRange own(a.q_off, a.n_seqs, a.q_total);
+  if (own.none()) return;
+
   for (int x = 4 * tid; x < a.rows_per * a.p_cap; x += 4 * blockDim.x)
     *reinterpret_cast<u32x4 *>(s_key + x) = u32x4{0, 0, 0, 0};
   // the rows' sequences, by the first wavefront (the last one sees to the queries)
@@ -462,7 +465,7 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
     if (wave == waves - 1) {
       // The columns' queries as the products' operand, for all wavefronts: a lane holds
       // its 16-element groups of [q+ ; q-] (columns past the last repeat the first).
-      const InT *qp = static_cast<const InT *>(a.q) + (size_t)(r0 + i) * a.q_stride +
+      const InT *qp = static_cast<const InT *>(a.q) + (size_t)own.nearest(r0 + i) * a.q_stride +
                       (size_t)(h * a.group + hg) * DH;
       float x[XN][16];
       uint32_t am = 0;

@@ -1133,6 +1133,7 @@ struct PagedLists {
   const int32_t *page_table = nullptr, *lens = nullptr, *off = nullptr, *idx = nullptr,
                 *first = nullptr, *pages = nullptr;
   int32_t n_seqs = 0, max_pages = 0, total = 0, row_max = 0, len_max = INT32_MAX, n_select = 0;
+  int32_t rows = 0;  // of idx and pages on the host: none behind the last sequence's
 };
 
 // What is wrong with the lists (host arrays), or NULL; `seq`: where.
@@ -1149,7 +1150,7 @@ const char *check_lists(const PagedLists &l, const marche_paged_cache_t *c, int3
   for (int b = 0; b < l.n_seqs; ++b) {
     const int32_t each = l.total / l.n_seqs;
     const int32_t r0 = l.off ? l.off[b] : b * each, r1 = l.off ? l.off[b + 1] : r0 + each;
-    if (r0 < 0 || r1 < r0 || r1 > l.total || r1 - r0 > l.row_max) return say("row offsets inconsistent", b);
+    if (r0 < 0 || r1 < r0 || r1 > l.rows || r1 - r0 > l.row_max) return say("row offsets inconsistent", b);
     if (l.lens) {
       if (l.lens[b] < 0 || l.lens[b] > cap || l.lens[b] > l.len_max) return say("length out of range", b);
       for (int64_t t = 0; t < l.lens[b]; t += c->page_size)
@@ -1188,9 +1189,12 @@ marche_status_t validate_paged(PagedLists l, const marche_paged_cache_t *c, hipS
   fetch(l.page_table, (size_t)l.n_seqs * l.max_pages);
   fetch(l.lens, l.n_seqs);
   fetch(l.off, (size_t)l.n_seqs + 1);
-  fetch(l.idx, l.total);
   fetch(l.first, l.n_seqs);
-  fetch(l.pages, (size_t)l.total * c->n_heads * l.n_select);
+  l.rows = l.total;
+  if (l.off && e == hipSuccess && (e = hipStreamSynchronize(stream)) == hipSuccess)
+    l.rows = std::min(std::max(l.off[l.n_seqs], 0), l.total);
+  fetch(l.idx, l.rows);
+  fetch(l.pages, (size_t)l.rows * c->n_heads * l.n_select);
   if (e == hipSuccess) e = hipStreamSynchronize(stream);
   if (e != hipSuccess) return fail_hip(e, "paged-list validation");
   int32_t seq = 0;

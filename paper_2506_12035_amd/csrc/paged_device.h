@@ -58,6 +58,17 @@ __device__ __forceinline__ int paged_len(int len, int max_pages, int page_log2) 
   return max(0, (int)(len < cap ? len : cap));
 }
 
+// The rows that belong to any sequence: [lo, hi) of [0, total).  What lies
+// outside may not even be there.
+struct RowRange {
+  int lo, hi;
+  __device__ __forceinline__ RowRange(const int32_t *off, int n_seqs, int total) : lo(0), hi(total) {
+    if (off) lo = max(off[0], 0), hi = min(off[n_seqs], total);
+  }
+  __device__ __forceinline__ bool none() const { return hi <= lo; }
+  __device__ __forceinline__ int nearest(int r) const { return min(max(r, lo), hi - 1); }
+};
+
 // Eight consecutive values of a row.
 __device__ __forceinline__ void load8(const float *p, float *o) {
   const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];

@@ -6,7 +6,7 @@ import torch
 from paper_2506_12035_amd import binding
 
 from gpu_util import say
-from paged_util import DT, Pool, dev
+from paged_util import DT, Pool, dev, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +29,34 @@ def test_scores_below_the_range_rank_above_nan(n_pages):
         binding.paged_select(pool.cache, 0, pool.dtable, pool.width, pool.dlens, 1, q, 64, None, 1, 1, DT["bf16"], k,
                              pages)
         assert pages[0, 0].tolist() == want
+
+
+# ------------------------------------------------------------------ rows of no sequence
+
+@pytest.mark.parametrize("validate", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_behind_the_last_sequence_need_not_be_there(monkeypatch, dtype, validate):
+    """Totals of a larger batch over buffers that end with the last sequence's rows."""
+    say(f"paged rows that are not there {dtype} {validate}")
+    if validate:
+        monkeypatch.setenv("MARCHE_VALIDATE", "1")
+    pool = Pool("int8", [40, 0, 17], 2, 64, 16, seed=1, with_bounds=True)
+    off, n, total = i32([1, 4, 4, 6]), 6, 1 << 20
+    rng = np.random.default_rng(2)
+    x = dev(rng.standard_normal((n, 128)), torch.bfloat16 if dtype == "bf16" else torch.float32)
+    idx = i32([-1, 39, 0, 5, 16, 2])
+    binding.paged_bounds(pool.cache, 0, pool.dtable, pool.width, pool.dlens, None, pool.width, 3)
+    out = []
+    for rows in (n, total):
+        pages = torch.full((n, 2, 2), -5, dtype=torch.int32, device="cuda")
+        o = torch.full((n, 128), 7.0, dtype=x.dtype, device="cuda")
+        binding.paged_write(pool.cache, 0, pool.dtable, pool.width, 3, idx, off, rows, x, x, 128, DT[dtype])
+        binding.paged_select(pool.cache, 0, pool.dtable, pool.width, pool.dlens, 3, x, 128, off, rows, 2, DT[dtype], 2, pages)
+        binding.paged_attention(pool.cache, 0, pool.dtable, pool.width, pool.dlens, 40, 3, x, 128, off, rows, 3, 2,
+                                DT[dtype], o, pages, 2)
+        torch.cuda.synchronize()
+        assert (pages[0] == -5).all() and (o[0] == 7).all() and not (o[1:] == 7).any()
+        out.append((pages, o, pool.layer_of("k")[0], pool.layer_of("v")[0]))
+        assert (pool.seq("k", 0)[39] != 0).any()
+    for a, b in zip(*out):
+        np.testing.assert_array_equal(np.asarray(torch.as_tensor(a).double().cpu()), np.asarray(torch.as_tensor(b).double().cpu()))
