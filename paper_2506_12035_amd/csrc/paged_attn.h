@@ -265,16 +265,20 @@ struct KvRaw {
   static __device__ __forceinline__ int vchan(int m, int x) { return m < VC ? VC * x + m : 64 + x; }
 };
 
-// T parts of a float32 whose sum is the value to 8 T bits (an infinity's other
-// parts are zero).
+// One bf16, or three whose sum is the float32 value: its first 8 bits cut off (rounded,
+// the largest finite values would become infinite) and the 16 behind them in two
+// parts (an infinity's are zero; a NaN's are NaN, should the first part not be).
 template <int T>
 __device__ __forceinline__ void split(float x, bf16 (&o)[T]) {
-  o[0] = (bf16)x;
-  if constexpr (T > 1) x = fabsf(x) == INFINITY ? 0.f : x - (float)o[0];
-#pragma unroll
-  for (int i = 1; i < T; ++i) {
-    o[i] = (bf16)x;
-    x -= (float)o[i];
+  static_assert(T == 1 || T == 3, "parts");
+  if constexpr (T == 1) {
+    o[0] = (bf16)x;
+  } else {
+    const float top = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+    o[0] = __builtin_bit_cast(bf16, (uint16_t)(__float_as_uint(x) >> 16));
+    x = fabsf(x) == INFINITY ? 0.f : x - top;
+    o[1] = (bf16)x;
+    o[2] = (bf16)(x - (float)o[1]);
   }
 }
 

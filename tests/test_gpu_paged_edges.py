@@ -6,9 +6,11 @@ import torch
 from paper_2506_12035_amd import binding
 
 from gpu_util import say
-from paged_util import DT, Pool, dev, i32
+from paged_util import DT, Pool, attention, attention_errors, dev, i32, rnd
 
 pytestmark = pytest.mark.gpu
+
+F32_MAX = float(np.finfo(np.float32).max)
 
 
 # ------------------------------------------------------------------ select
@@ -60,3 +62,28 @@ def test_rows_behind_the_last_sequence_need_not_be_there(monkeypatch, dtype, val
         assert (pool.seq("k", 0)[39] != 0).any()
     for a, b in zip(*out):
         np.testing.assert_array_equal(np.asarray(torch.as_tensor(a).double().cpu()), np.asarray(torch.as_tensor(b).double().cpu()))
+
+
+# ------------------------------------------------------------------ fp32 queries
+
+@pytest.mark.parametrize("rows", [1, 20])
+@pytest.mark.parametrize("dh", [64, 80, 128])
+def test_largest_fp32_queries(dh, rows):
+    """Finite queries above the largest bf16 over keys so small that the logits
+    are ordinary: every part of a query is finite."""
+    say(f"paged attention, largest fp32 queries {dh} {rows}")
+    pool = Pool("bf16", [90], 1, dh, 16, seed=31)
+    rng = np.random.default_rng(32)
+    for p in pool.table[0, :6]:  # two channels' keys, normal bf16 numbers
+        for d in {0, min(dh - 1, 70)}:
+            pool.dk[0, int(p), 0, :, d] = dev(rng.uniform(0.25, 1, 16) * rng.choice([-1, 1], 16) * 2.0 ** -122,
+                                              torch.bfloat16)
+    q = rnd(rng.standard_normal((rows, dh)), "f32")
+    q[:, 0], q[:, min(dh - 1, 70)] = F32_MAX, -F32_MAX * rng.uniform(0.998, 1, rows).astype(np.float32)
+    q = rnd(q, "f32")
+    assert np.isfinite(q).all() and np.isinf(rnd(q, "bf16")).any()
+    pages = i32(np.broadcast_to(np.arange(6, dtype=np.int32), (rows, 1, 6)).copy())
+    for pg in (None, pages):
+        got = attention(pool, dev(q, torch.float32), [rows], 1, "f32", pg).double().cpu().numpy()
+        assert np.isfinite(got).all()
+        assert attention_errors(pool, got, q, [rows], 1, "f32") <= 1
