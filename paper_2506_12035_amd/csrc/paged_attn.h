@@ -33,7 +33,8 @@
 // trails the true one by at most 2^8, which saves most rescales.  P is rounded
 // to bf16 (half a step, 2^-9 of each weight, as the products' other operand V
 // is exact in bf16 for every format).  float32 rows are split into three bf16
-// parts (24 bits, nothing lost) and so is P.
+// parts (24 bits, nothing lost) and so is P; infinite keys and values meet the
+// first parts only (a second pass, where there are any).
 //
 // Bound: single rows by the cache's bytes (16 int8 caches of 4000 .. 32768
 // tokens, 607 MB: 119 us, 118 at a copy's rate); many rows by the latency of
@@ -44,6 +45,7 @@
 #pragma once
 
 #include <algorithm>
+#include <type_traits>
 
 #include "paged_device.h"
 
@@ -280,6 +282,17 @@ __device__ __forceinline__ void split(float x, bf16 (&o)[T]) {
     o[1] = (bf16)x;
     o[2] = (bf16)(x - (float)o[1]);
   }
+}
+
+// Eight bf16 with zeros for infinities and NaN.
+__device__ __forceinline__ bf16x8 finite(bf16x8 x) {
+  u32x4 w = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((w[i] & 0x7F80u) == 0x7F80u) w[i] &= 0xFFFF0000u;
+    if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] &= 0xFFFFu;
+  }
+  return __builtin_bit_cast(bf16x8, w);
 }
 
 // Whether K goes through LDS (the text above).
@@ -551,7 +564,10 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   float m_run[RT], l_run[RT];
   bool seen[RT];
 
-  auto pass = [&]() {
+  // (again: the products with the lower parts of fp32 queries and weights leave
+  // out keys and values that are not finite, see below)
+  auto pass = [&](auto again) {
+    constexpr bool AGAIN = again.value;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       m_run[rt] = -INFINITY;
@@ -605,7 +621,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
           for (int n = 0; n < NC; ++n)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
-              s[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[n], qf[rt][e][n], s[rt][u], 0, 0, 0);
+              s[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(AGAIN && e > 0 ? finite(kf[n]) : kf[n], qf[rt][e][n], s[rt][u], 0, 0, 0);
       }
       if constexpr (FMT == I8) {
 #pragma unroll
@@ -692,7 +708,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
           for (int e = TERMS - 1; e >= 0; --e)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
-              acc[rt][m + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j], pb[rt][e], acc[rt][m + j], 0, 0, 0);
+              acc[rt][m + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(AGAIN && e > 0 ? finite(vf[j]) : vf[j], pb[rt][e], acc[rt][m + j], 0, 0, 0);
         }
       }
       if (!more) break;
@@ -789,13 +805,17 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
     }
   };
 
-  pass();
-  if constexpr (SEL) {
-    // A weight of zero times an infinite or NaN value of a page that only
-    // another row looks at is NaN: a block in which anything is not finite is
-    // computed again, row by row over each row's own pages.
+  // Two things make NaN of values that are not finite where none is due, and a
+  // block in which anything is not finite is computed again: a weight of zero
+  // times a value of a page that only another row looks at (row by row over each
+  // row's own pages), and an infinite bf16 key or value times a part of an fp32
+  // query or weight that is zero or of the other sign than the whole.
+  constexpr bool PARTS = FMT == BF && TERMS > 1;
+  pass(std::false_type());
+  if constexpr (SEL || PARTS) {
+    const bool foreign = SEL && i1 > i0;
     bool bad = false;
-    if (i1 > i0) {
+    if (PARTS || foreign) {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -804,9 +824,14 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
           for (int r = 0; r < 4; ++r) bad |= !(fabsf(acc[rt][m][r]) < INFINITY);
     }
     if (__syncthreads_or(bad)) {
-      one_by_one<FMT, DH, RowT>(a, tab, s_bits, s_list, words, p0, min(p0 + 16 * RT, packed), i0, row0, h, split_i,
-                                len, min(32 * t1, n_keys), wave, waves, lane);
-      return;
+      if constexpr (SEL) {
+        if (foreign) {
+          one_by_one<FMT, DH, RowT>(a, tab, s_bits, s_list, words, p0, min(p0 + 16 * RT, packed), i0, row0, h,
+                                    split_i, len, min(32 * t1, n_keys), wave, waves, lane);
+          return;
+        }
+      }
+      if constexpr (PARTS) pass(std::true_type());
     }
   }
   join();

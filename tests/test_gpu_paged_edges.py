@@ -6,7 +6,7 @@ import torch
 from paper_2506_12035_amd import binding
 
 from gpu_util import say
-from paged_util import DT, Pool, attention, attention_errors, dev, i32, rnd
+from paged_util import DT, TORCH, Pool, attention, attention_errors, dev, i32, offsets, rnd
 
 pytestmark = pytest.mark.gpu
 
@@ -87,3 +87,103 @@ def test_largest_fp32_queries(dh, rows):
         got = attention(pool, dev(q, torch.float32), [rows], 1, "f32", pg).double().cpu().numpy()
         assert np.isfinite(got).all()
         assert attention_errors(pool, got, q, [rows], 1, "f32") <= 1
+
+
+# ------------------------------------------------------------------ infinite keys and values
+
+# lens, rows, group, dh, every row lists: None, or pages of the cache
+INF_CASES = [
+    ([200], [1], 1, 64, None), ([200], [40], 1, 80, None), ([90, 130], [3, 5], 3, 128, None),
+    ([3000, 40], [1, 1], 2, 64, None),               # split
+    ([200], [1], 1, 80, 5), ([300], [9], 2, 64, 5),  # a block of one row, of several
+    ([2500], [1], 1, 128, 150), ([2500], [3], 1, 64, 150),
+]
+
+
+def _inf_pool(lens, dh):
+    """A bf16 cache in which every seventh key is -inf in one channel."""
+    pool = Pool("bf16", lens, 1, dh, 16, seed=41)
+    off = []
+    for b, n in enumerate(lens):
+        bad = np.arange(2, n, 7)
+        for j in bad:
+            pool.dk[0, int(pool.table[b, j // 16]), 0, j % 16, (5 * j) % dh] = float("-inf")
+        off.append(bad)
+    return pool, off
+
+
+def _lists(lens, rows, n_list, rng):
+    if n_list is None:
+        return None
+    out = [np.sort(rng.permutation(-(-n // 16))[:n_list]) for n, r in zip(lens, rows) for _ in range(r)]
+    return np.stack(out).astype(np.int32)[:, None]
+
+
+def _looked_at(pages, lens, rows):
+    if pages is None:
+        return [np.ones((r, 1, n), bool) for n, r in zip(lens, rows)]
+    off = offsets(rows)
+    out = []
+    for b, n in enumerate(lens):
+        look = np.zeros((rows[b], 1, n), bool)
+        for i in range(rows[b]):
+            look[i, 0] = np.isin(np.arange(n) // 16, pages[off[b] + i, 0])
+        out.append(look)
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", INF_CASES, ids=lambda c: "n{}r{}g{}d{}k{}".format(max(c[0]), sum(c[1]), *c[2:]))
+def test_keys_of_minus_infinity_count_nothing(case, dtype):
+    """Logits of -inf beside finite ones have weight zero (queries positive, so
+    that -inf keys give -inf; ones and halves, whose lower parts are zeros)."""
+    lens, rows, group, dh, n_list = case
+    say(f"paged attention, keys of -inf {case} {dtype}")
+    pool, bad = _inf_pool(lens, dh)
+    rng = np.random.default_rng(42)
+    q = rnd(np.abs(rng.standard_normal((sum(rows), group * dh))) * 0.3 + 0.01, dtype)
+    q[0] = 1.0
+    q[-1, ::2] = 0.5
+    pages = _lists(lens, rows, n_list, rng)
+    look = _looked_at(pages, lens, rows)
+    for b, j in enumerate(bad):
+        look[b][:, :, j] = False
+    got = attention(pool, dev(q, TORCH[dtype]), rows, group, dtype, None if pages is None else i32(pages))
+    got = got.double().cpu().numpy()
+    pool.dk[pool.dk == float("-inf")] = 0.0  # (of keys that are not looked at below)
+    assert np.isfinite(got).all()
+    assert attention_errors(pool, got, q, rows, group, dtype, look) <= 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", INF_CASES, ids=lambda c: "n{}r{}g{}d{}k{}".format(max(c[0]), sum(c[1]), *c[2:]))
+def test_infinite_values_reach_their_channel(case, dtype):
+    """An infinite value with a weight above zero makes its channel infinite
+    for the rows that look at it, and changes nothing else."""
+    lens, rows, group, dh, n_list = case
+    say(f"paged attention, infinite values {case} {dtype}")
+    pool = Pool("bf16", lens, 1, dh, 16, seed=43)
+    rng = np.random.default_rng(44)
+    places = [[(n // 2, 3, 1), (n - 1, dh - 1, -1), (1, 40, 1)] for n in lens]  # token, channel, sign
+    for b, some in enumerate(places):
+        for j, d, sign in some:
+            pool.dv[0, int(pool.table[b, j // 16]), 0, j % 16, d] = sign * float("inf")
+    q = rnd(0.5 * rng.standard_normal((sum(rows), group * dh)), dtype)
+    q[0] = 0.0  # weights that are all the same
+    pages = _lists(lens, rows, n_list, rng)
+    look = _looked_at(pages, lens, rows)
+    got = attention(pool, dev(q, TORCH[dtype]), rows, group, dtype, None if pages is None else i32(pages))
+    got = got.double().cpu().numpy().reshape(sum(rows), group, dh)
+    want = np.zeros_like(got)
+    off = offsets(rows)
+    for b, some in enumerate(places):
+        for j, d, sign in some:
+            for i in range(rows[b]):
+                if look[b][i, 0, j]:
+                    want[off[b] + i, :, d] = sign * np.inf
+    np.testing.assert_array_equal(np.where(np.isinf(got), got, 0.0), want)
+    # the other channels, whatever these hold
+    for d in (3, 40, dh - 1):
+        pool.dv[..., d] = 0.0
+        got[..., d] = 0.0
+    assert attention_errors(pool, got, q, rows, group, dtype, look) <= 1
