@@ -394,7 +394,8 @@ marche_status_t marche_diffusion_sample(const marche_head_t *head, const marche_
  * row and M = 448 or 127, e is the least integer >= -111 with A <= M * 2^e, code =
  * e + 127, and q = x * 2^-e rounded to the format, ties to even.  Powers of two
  * make this, and reading back, independent of the order of operations, and
- * q * 2^e is exact in bf16.  A row with an infinity or a NaN is stored as
+ * q * 2^e is exact in bf16.  (What would be rounded to 2^128, past bf16 and float32, becomes
+ * the number before it: 240 * 2^120 in E4M3, 63 * 2^122 in INT8.)  A row with an infinity or a NaN is stored as
  * q = NaN (E4M3) or 0 (INT8) with code 255 and reads back as NaN throughout. */
 typedef enum {
   MARCHE_CACHE_BF16 = 0,

@@ -12,6 +12,9 @@ import numpy as np
 
 LIMIT = {"e4m3": 448.0, "int8": 127.0}
 LEAST = -111
+# What stands in for a number that would be rounded to 2^128, which no float32
+# row holds: the next one towards zero, with the exponent that such rows have.
+TOP = {"e4m3": 240.0, "int8": 63.0}
 
 
 def round_e4m3(y):
@@ -24,8 +27,8 @@ def round_e4m3(y):
 
 
 def quantise(x, fmt):
-    """Rows (last axis) -> (q, codes); a row that is not finite: NaN (e4m3) or
-    0 (int8) with code 255."""
+    """Rows (last axis) of float32 values -> (q, codes); a row that is not finite:
+    NaN (e4m3) or 0 (int8) with code 255."""
     x = np.asarray(x, np.float64)
     amax = np.abs(x).max(-1)
     bad = ~np.isfinite(amax)
@@ -39,6 +42,7 @@ def quantise(x, fmt):
     with np.errstate(invalid="ignore"):
         y = x * np.exp2(-e * 1.0)[..., None]
         q = round_e4m3(np.where(bad[..., None], 0.0, y)) if fmt == "e4m3" else np.rint(y)
+    q = np.where(np.abs(q) * np.exp2(e * 1.0)[..., None] >= 2.0 ** 128, np.sign(q) * TOP[fmt], q)
     q = np.where(bad[..., None], np.nan if fmt == "e4m3" else 0.0, q)
     return q, np.where(bad, 255, e + 127).astype(np.int64)
 

@@ -76,8 +76,27 @@ __device__ __forceinline__ uint32_t largest(const u32x4 (&x)[NV]) {
 
 // Eight values of a row with exponent code `code` in the format.
 template <int FMT, typename InT, int NV>
-__device__ __forceinline__ u32x2 pack8(const u32x4 (&x)[NV], int code) {
+__device__ __forceinline__ u32x2 pack8(u32x4 (&x)[NV], int code) {
   u32x2 o;
+  // No magnitude above TOP_BITS in the largest rows (in e4m3 no other row reaches
+  // that), by a limit for either sign: as signed numbers the negative ones are
+  // below the positive limit, as unsigned ones the others below the negative.
+  const uint32_t top = FMT == E4 || code == TOP_CODE<FMT> ? TOP_BITS<FMT> : 0x7F7FFFFFu;
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(InT) == 4) {
+        x[v][i] = min((uint32_t)min((int)x[v][i], (int)top), top | 0x80000000u);
+      } else {
+        typedef short s16x2 __attribute__((ext_vector_type(2)));
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        const short high = (short)(top >> 16);
+        const unsigned short low = (unsigned short)(high | 0x8000);
+        const s16x2 w = __builtin_elementwise_min(__builtin_bit_cast(s16x2, +x[v][i]), s16x2{high, high});
+        x[v][i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, w), u16x2{low, low}));
+      }
+    }
   if (code == 255) {  // the whole row reads back as NaN
     o.x = o.y = FMT == E4 ? 0x7F7F7F7Fu : 0u;
     return o;
@@ -372,6 +391,14 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
   amax = __uint_as_float(wave_max_u32(lane < LPT ? __float_as_uint(amax) & 0x7FFFFFFFu : 0u));
   const int code = bad ? 255 : exp_code<I8>(amax);
   const size_t out = (size_t)page * a.n_heads + h;
+  if (code == TOP_CODE<I8>) {
+    const float top = int8_top(code);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      hi[i] = __builtin_amdgcn_fmed3f(hi[i], -top, top);
+      lo[i] = __builtin_amdgcn_fmed3f(lo[i], -top, top);
+    }
+  }
   if (lane < LPT) {
     uint32_t wh = 0, wl = 0;
     if (code != 255) {
@@ -484,6 +511,7 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
       am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
       const int qc = exp_code<I8>(__uint_as_float(am));
       const float inv = exp_inv(min(qc, 253));
+      const float top = int8_top(qc);
 #pragma unroll
       for (int s = 0; s < ST; ++s) {
         const int k0 = 64 * s + 16 * g;
@@ -495,7 +523,7 @@ __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float v = x[s % XN][4 * w + e];
-            y[e] = round_low(neg ? fminf(v, 0.f) : fmaxf(v, 0.f), inv);
+            y[e] = round_low(__builtin_amdgcn_fmed3f(v, neg ? -top : 0.f, neg ? 0.f : top), inv);
           }
           q[w] = k0 < 2 * DH ? pack_low(y[0], y[1], y[2], y[3]) : 0;
         }

@@ -29,7 +29,19 @@ __device__ __forceinline__ int exp_code(float amax) {
 }
 // 2^(code - 127); the code 255 gives infinity.
 __device__ __forceinline__ float exp_scale(uint32_t code) { return __uint_as_float(code << 23); }
-// 2^(127 - code), exact for every code a finite row has (16 .. 248).
+// The code of the largest finite rows, and, as float bits, the largest magnitude
+// in them: what would be rounded to 2^128 becomes the number before it, 240 2^120
+// or 63 2^122 (off by up to a step, not half a one), so that finite rows read back
+// finite.
+template <int FMT>
+constexpr int TOP_CODE = FMT == E4 ? 247 : 249;
+template <int FMT>
+constexpr uint32_t TOP_BITS = FMT == E4 ? 0x7F700000u : 0x7F7C0000u;
+// Of an int8 row with this code: the magnitude that its values are held to.
+__device__ __forceinline__ float int8_top(int code) {
+  return code == TOP_CODE<I8> ? __uint_as_float(TOP_BITS<I8>) : INFINITY;
+}
+// 2^(127 - code), exact for every code a finite row has (16 .. 249).
 __device__ __forceinline__ float exp_inv(int code) { return __uint_as_float((uint32_t)(254 - code) << 23); }
 
 // Four values of a dword of the format.

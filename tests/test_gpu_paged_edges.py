@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import paged as ref
 from paper_2506_12035_amd import binding
 
 from gpu_util import say
@@ -11,6 +12,7 @@ from paged_util import DT, TORCH, Pool, attention, attention_errors, dev, i32, o
 pytestmark = pytest.mark.gpu
 
 F32_MAX = float(np.finfo(np.float32).max)
+BF16_MAX = 255 * 2.0 ** 120
 
 
 # ------------------------------------------------------------------ select
@@ -187,3 +189,92 @@ def test_infinite_values_reach_their_channel(case, dtype):
         pool.dv[..., d] = 0.0
         got[..., d] = 0.0
     assert attention_errors(pool, got, q, rows, group, dtype, look) <= 1
+
+
+# ------------------------------------------------------------------ the largest finite rows
+
+def _top_rows(dh):
+    """Finite float32 rows whose values next to 2^128 must not be rounded to it."""
+    rng = np.random.default_rng(51)
+    top = [F32_MAX, BF16_MAX, 1.9375 * 2.0 ** 127, 1.984375 * 2.0 ** 127, 1.96875 * 2.0 ** 127, 1.875 * 2.0 ** 127,
+           1.75 * 2.0 ** 127, 1.9921875 * 2.0 ** 127]
+    x = rng.uniform(-1, 1, (2 * len(top), 1, dh)) * 2.0 ** 127
+    for i, t in enumerate(top):
+        x[i, 0, i], x[i + len(top), 0, -1 - i] = t, -t
+    x[:len(top), 0, 20:30] = np.linspace(-1, 1, 10) * BF16_MAX
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 80, 128])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_largest_finite_rows_stay_finite(fmt, dh, dtype):
+    say(f"paged write and read, largest rows {fmt} {dh} {dtype}")
+    x = rnd(np.clip(_top_rows(dh), -BF16_MAX, BF16_MAX) if dtype == "bf16" else _top_rows(dh), dtype)
+    assert np.isfinite(x).all()
+    n = len(x)
+    pool = Pool(fmt, [n], 1, dh, 16, seed=1)
+    d = dev(x.reshape(n, dh), TORCH[dtype])
+    binding.paged_write(pool.cache, 0, pool.dtable, pool.width, 1, i32(np.arange(n)), None, n, d, -d, dh, DT[dtype])
+    out = [torch.zeros(1, 1, n, dh, dtype=t, device="cuda") for t in (torch.float32, torch.bfloat16) for _ in range(2)]
+    for i, t in ((0, "f32"), (2, "bf16")):
+        binding.paged_read(pool.cache, 0, pool.dtable, pool.width, pool.dlens, 1, n, out[i], out[i + 1], DT[t])
+    torch.cuda.synchronize()
+    q, code = ref.quantise(x, fmt)
+    want = ref.value(q, code)
+    assert (np.abs(want) < 2.0 ** 128).all()
+    for name, sign in (("k", 1), ("v", -1)):
+        got = pool.layer_of(name)
+        np.testing.assert_array_equal(pool.seq(name, 0), sign * want)
+        assert np.array_equal(got[1][pool.table[0, 0], 0], code[:16, 0])
+    for i, t in enumerate(out):
+        np.testing.assert_array_equal(t[0, 0].double().cpu().numpy(), (-1) ** i * want[:, 0])
+
+
+def test_largest_keys_and_queries_in_bounds_and_scores():
+    """Bounds and the selection's queries are INT8 rows, the largest among them."""
+    say("paged bounds and select, largest values")
+    x = rnd(np.clip(_top_rows(64), -BF16_MAX, BF16_MAX), "bf16")
+    pool = Pool("bf16", [16 * 9], 1, 64, 16, seed=2, with_bounds=True)
+    for p in range(9):
+        pool.dk[0, int(pool.table[0, p]), 0, 3] = dev(x[p, 0] * 2.0 ** -(p % 3), torch.bfloat16)
+    binding.paged_bounds(pool.cache, 0, pool.dtable, pool.width, pool.dlens, None, pool.width, 1)
+    torch.cuda.synchronize()
+    k = pool.seq("k", 0)
+    at = pool.table[0, :9]
+    for p in range(9):
+        want, code = ref.bounds(k[16 * p:16 * p + 16])
+        np.testing.assert_array_equal(pool.db[0, int(at[p])].cpu().numpy(), want)
+        np.testing.assert_array_equal(pool.dbe[0, int(at[p])].cpu().numpy(), code)
+    assert pool.dbe.max() == 249
+    # scores within float32: queries at the top over small bounds
+    rng = np.random.default_rng(3)
+    pool.db[:] = dev(rng.integers(-127, 128, pool.db.shape).astype(np.int8))
+    pool.dbe[:] = 30
+    bound, code = pool.db[0].cpu().numpy().astype(float), pool.dbe[0].cpu().numpy().astype(int)
+    for dtype in ("bf16", "f32"):
+        q = x[:, 0] if dtype == "bf16" else rnd(_top_rows(64)[:, 0], "f32")
+        n = len(q)
+        pages = torch.zeros(n, 1, 4, dtype=torch.int32, device="cuda")
+        binding.paged_select(pool.cache, 0, pool.dtable, pool.width, pool.dlens, 1, dev(q, TORCH[dtype]), 64, None, n, 1,
+                             DT[dtype], 4, pages)
+        want = [ref.select(ref.scores(q[r][None], bound[at, 0], code[at, 0]), 4) for r in range(n)]
+        assert pages[:, 0].tolist() == want
+
+
+def test_largest_query_beside_the_largest_of_the_exponent_below():
+    """Rows that share a call are quantised each by itself: 127 * 2^121 is 127
+    beside a row that reaches past it."""
+    say("paged select, two largest queries")
+    pool = Pool("int8", [32], 1, 64, 16, with_bounds=True)
+    pool.dbe[:] = 30
+    a, b = (int(p) for p in pool.table[0, :2])
+    pool.db[0, a, 0, 0, 0], pool.db[0, b, 0, 0, 1] = 100, 125  # 100 * 127 against 125 * 101
+    q = np.zeros((2, 64))
+    q[0, 5] = BF16_MAX
+    q[1, :2] = 127 * 2.0 ** 121, 101 * 2.0 ** 121
+    for dtype in ("bf16", "f32"):
+        pages = torch.full((2, 1, 1), -5, dtype=torch.int32, device="cuda")
+        binding.paged_select(pool.cache, 0, pool.dtable, pool.width, pool.dlens, 1, dev(q, TORCH[dtype]), 64, None, 2, 1,
+                             DT[dtype], 1, pages)
+        assert pages[1, 0].tolist() == [0]
