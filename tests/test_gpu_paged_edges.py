@@ -158,6 +158,23 @@ def test_keys_of_minus_infinity_count_nothing(case, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_whose_logits_are_all_minus_infinity(dtype):
+    """0 / 0, beside rows with a finite logit and rows without a key."""
+    say(f"paged attention, all logits -inf {dtype}")
+    pool = Pool("bf16", [1024, 64, 0], 1, 64, 64, seed=6)
+    for b, n in ((0, 992), (1, 64)):
+        for p in range(-(-n // 64)):
+            pool.dk[0, int(pool.table[b, p]), 0, :min(64, n - 64 * p)] = float("-inf")
+    q = np.ones((3, 64))
+    got = attention(pool, dev(q, TORCH[dtype]), [1, 1, 1], 1, dtype).double().cpu().numpy()
+    assert np.isnan(got[1]).all() and (got[2] == 0).all()
+    pool.dk[pool.dk == float("-inf")] = 0.0
+    look = [np.arange(1024)[None, None] >= 992, np.zeros((1, 1, 64), bool), np.zeros((1, 1, 0), bool)]
+    got[1] = 0.0
+    assert attention_errors(pool, got, q, [1, 1, 1], 1, dtype, look) <= 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("case", INF_CASES, ids=lambda c: "n{}r{}g{}d{}k{}".format(max(c[0]), sum(c[1]), *c[2:]))
 def test_infinite_values_reach_their_channel(case, dtype):
     """An infinite value with a weight above zero makes its channel infinite
