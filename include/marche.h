@@ -457,7 +457,10 @@ marche_status_t marche_paged_cache_init(marche_paged_cache_t *cache, int32_t n_l
  * row and output pointers are 16-byte aligned.
  * Device lists are preconditions, as for marche_step; MARCHE_VALIDATE copies them to the
  * host and checks them there before anything is launched (host sync; not under
- * stream capture), returning INVALID_ARG with the sequence named. */
+ * stream capture), returning INVALID_ARG with the sequence named.  It refuses
+ * also what the calls would leave out: lengths and tokens past the page table,
+ * pages outside the pool (of the sequence's tokens), listed pages that the sequence
+ * does not have. */
 
 /* Writes new keys and values into the cache: row r of sequence b becomes token
  * a_idx[r] (>= 0; distinct within a sequence) of it, quantised as above (bf16
@@ -527,12 +530,17 @@ marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t l
  * parts joined, so a row's rounding may depend on the sizes of its call.
  * q_max is the largest number of rows of a sequence and len_max the largest
  * length (host copies, for launch geometry, and preconditions as the lists
- * are; q_total * n_q_heads < 2^30, with the same exception).  The weighted sum is float32 and divided by
- * the weights' sum last: values near 2^128 / (256 * tokens) may overflow in it.  o: [q_total][n_q_heads * head_dim].
+ * are; q_total * n_q_heads < 2^30, with the same exception).  Logits, the
+ * softmax's maximum and sum and the weighted sum are float32.  For bf16 rows each
+ * weight enters the weighted sum rounded to bf16 (off by up to 2^-8 of it;
+ * unrounded in the weights' sum), for float32 rows with 24 bits.  The weights' sum
+ * divides last: values near 2^128 / (256 * tokens) may overflow before.  INT8
+ * keys meet the query before their exponent does: logits may overflow from
+ * |q| = 2^128 / (127 * head_dim) on.  o: [q_total][n_q_heads * head_dim].
  * pages NULL: n_select is 0.  With pages: max_pages <= 4096.  workspace:
- * marche_paged_attention_workspace_bytes, 256-byte aligned (may be 0 bytes;
- * for these sizes: a smaller len_max can need more; 0 for sizes that the call
- * refuses; the cache's pointers are not looked at). */
+ * marche_paged_attention_workspace_bytes, 256-byte aligned, for no other call in
+ * flight (may be 0 bytes; for these sizes: a smaller len_max can need more; 0 for
+ * sizes that the call refuses; the cache's pointers are not looked at). */
 size_t marche_paged_attention_workspace_bytes(const marche_paged_cache_t *cache, int32_t n_seqs,
                                               int32_t q_total, int32_t q_max, int32_t n_q_heads,
                                               int32_t len_max, int32_t n_select);

@@ -135,8 +135,11 @@ __device__ __forceinline__ u32x2 pack8(u32x4 (&x)[NV], int code) {
 // rounding, one 8-byte (16 for bf16) store.  Bound by bytes: each new row is
 // read once and its slot written once.  (Two or four pairs a thread, to find
 // the rows' sequences less often: 59.0 and 64.6 us for 56.4 on 40960 rows of 16
-// heads of 64, bf16 to int8; with STREAM 51.3, 4.9 TB/s.)  STREAM: the rows
-// are loaded past the caches, for calls whose rows do not fit them anyway.
+// heads of 64, bf16 to int8, without STREAM; now, with it, 52.5, 4.8 TB/s.)
+// STREAM: the rows are loaded past the caches, for calls whose rows do not fit
+// them anyway.  The loads wait for the range of the rows that have a sequence
+// (a clamped row instead of a branch, behind which they were waited for at once:
+// 53.2 us for 55.3).
 template <int FMT, int DH, typename InT, bool STREAM>
 __global__ __launch_bounds__(256) void paged_write_kernel(PagedWriteArgs a) {
   constexpr int PER = paged_write_pairs(DH), GROUP = 256 / PER;
@@ -439,8 +442,8 @@ __device__ __forceinline__ uint32_t score_key(float f) {
 // ascending order.
 //
 // Bound by latency: row offsets, length, page ids and bounds are loaded one after
-// the other.  8 rows of 32 heads over 512 pages (64 workgroups) 12.1 us, 36 .. 100
-// rows of 16 heads over 34 pages of 32 sequences 17.9 us (the workgroups fill the
+// the other.  8 rows of 32 heads over 512 pages (64 workgroups) 12.0 us, 36 .. 100
+// rows of 16 heads over 34 pages of 32 sequences 18.8 us (the workgroups fill the
 // chip twice); the bounds and queries alone are 1.8 and 1.3 us of bytes.
 template <int DH, typename InT, int KPL>
 __global__ __launch_bounds__(1024) void paged_select_kernel(PagedSelectArgs a) {
@@ -821,7 +824,8 @@ hipError_t launch_paged_select(DType dt, int32_t head_dim, const PagedSelectArgs
       if (dt == DType::BF16) launch_kernel(paged_select_kernel<dh.value, bf16, K>, g, b, lds, s, a);
       else launch_kernel(paged_select_kernel<dh.value, float, K>, g, b, lds, s, a);
     };
-    // keys per lane of a row's wavefront: the fewest that hold max_pages
+    // keys per lane of a row's wavefront: the fewest that hold max_pages (64, beyond
+    // 1024 pages, spill two registers)
     const int kpl = a.p_cap / 64;
     if (kpl <= 1) go(std::integral_constant<int, 1>());
     else if (kpl <= 4) go(std::integral_constant<int, 4>());

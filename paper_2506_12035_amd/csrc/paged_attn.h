@@ -31,8 +31,8 @@
 //
 // Softmax statistics and O are float32; the maximum that P is taken against
 // trails the true one by at most 2^8, which saves most rescales.  P is rounded
-// to bf16 (half a step, 2^-9 of each weight, as the products' other operand V
-// is exact in bf16 for every format).  float32 rows are split into three bf16
+// to bf16 (half a step, 2^-8 of each weight; the products' other operand V
+// is exact in bf16 for every format, int8 with its exponent in P).  float32 rows are split into three bf16
 // parts (24 bits, nothing lost) and so is P; infinite keys and values meet the
 // first parts only (a second pass, where there are any).
 //
@@ -191,8 +191,7 @@ struct KvRaw {
       }
   }
   // K of half u as operands: product n covers the eight channels from chan(n, g)
-  // on (the tail's: four, and zeros.  Its own 16-deep instruction is no faster,
-  // and following a 32-deep one on the same accumulators gave wrong sums).
+  // on (the tail's: four, and zeros; a 16-deep instruction of its own is no faster).
   __device__ __forceinline__ void keys(int u, const char *s_k, int c, int g, bf16x8 (&f)[NC]) const {
     u32x4 k[KQ];
     u32x2 kt = {this->kt[u][0], this->kt[u][1]};
@@ -301,7 +300,9 @@ constexpr bool paged_stage = DH * (FMT == BF ? 2 : 1) > 64 && (RT == 2 || sizeof
 
 // Attention of a block's packed rows [p0, p1) over the pages that each of them
 // looks at, a wavefront per row, 16 keys at a time (lanes 0 .. 15 a key each):
-// the plain loop, for blocks that hold values that are not finite.
+// the plain loop, for blocks that hold values that are not finite.  Slow: one
+// NaN query among 36 .. 100 rows over 8 of 34 bf16 pages makes the call take 4.1 ms for
+// 72 us.
 template <int FMT, int DH, typename RowT>
 __device__ __forceinline__ void one_by_one(const PagedAttnArgs &a, const int32_t *tab, const uint32_t *s_bits,
                                            const uint16_t *s_list, int words, int p0, int p1, int i0, int row0, int h,
