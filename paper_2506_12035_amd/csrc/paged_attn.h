@@ -300,9 +300,8 @@ constexpr bool paged_stage = DH * (FMT == BF ? 2 : 1) > 64 && (RT == 2 || sizeof
 
 // Attention of a block's packed rows [p0, p1) over the pages that each of them
 // looks at, a wavefront per row, 16 keys at a time (lanes 0 .. 15 a key each):
-// the plain loop, for blocks that hold values that are not finite.  Slow: one
-// NaN query among 36 .. 100 rows over 8 of 34 bf16 pages makes the call take 4.1 ms for
-// 72 us.
+// the plain loop, for blocks that list values that are not finite.  Slow: one of
+// them among 36 .. 100 rows over 8 of 34 bf16 pages makes the call take 4.0 ms for 72 us.
 template <int FMT, int DH, typename RowT>
 __device__ __forceinline__ void one_by_one(const PagedAttnArgs &a, const int32_t *tab, const uint32_t *s_bits,
                                            const uint16_t *s_list, int words, int p0, int p1, int i0, int row0, int h,
@@ -806,33 +805,37 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
     }
   };
 
-  // Two things make NaN of values that are not finite where none is due, and a
-  // block in which anything is not finite is computed again: a weight of zero
-  // times a value of a page that only another row looks at (row by row over each
-  // row's own pages), and an infinite bf16 key or value times a part of an fp32
-  // query or weight that is zero or of the other sign than the whole.
-  constexpr bool PARTS = FMT == BF && TERMS > 1;
-  pass(std::false_type());
-  if constexpr (SEL || PARTS) {
-    const bool foreign = SEL && i1 > i0;
+  // Whether anything is not finite; with `own`, apart from rows whose weights' sum is
+  // NaN: their own logits make all of them NaN.
+  auto spoiled = [&](bool own) {
     bool bad = false;
-    if (PARTS || foreign) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+    for (int rt = 0; rt < RT; ++rt) {
+      float l = l_run[rt] + __shfl_xor(l_run[rt], 16, 64);
+      l += __shfl_xor(l, 32, 64);
+      bool x = false;
 #pragma unroll
-        for (int m = 0; m < M; ++m)
+      for (int m = 0; m < M; ++m)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) bad |= !(fabsf(acc[rt][m][r]) < INFINITY);
+        for (int r = 0; r < 4; ++r) x |= !(fabsf(acc[rt][m][r]) < INFINITY);
+      bad |= x && !(own && l != l);
     }
-    if (__syncthreads_or(bad)) {
-      if constexpr (SEL) {
-        if (foreign) {
-          one_by_one<FMT, DH, RowT>(a, tab, s_bits, s_list, words, p0, min(p0 + 16 * RT, packed), i0, row0, h,
-                                    split_i, len, min(32 * t1, n_keys), wave, waves, lane);
-          return;
-        }
-      }
-      if constexpr (PARTS) pass(std::true_type());
+    return __syncthreads_or(bad);
+  };
+
+  pass(std::false_type());
+  // An infinite bf16 key or value times a part of an fp32 query or weight that is
+  // zero, or of the other sign than the whole, is NaN where none is due.
+  if constexpr (FMT == BF && TERMS > 1)
+    if (spoiled(false)) pass(std::true_type());
+  // A weight of zero times an infinite or NaN value of a page that only another row
+  // looks at is NaN: such a block is computed again, row by row over each row's own
+  // pages.
+  if constexpr (SEL) {
+    if (i1 > i0 && spoiled(true)) {
+      one_by_one<FMT, DH, RowT>(a, tab, s_bits, s_list, words, p0, min(p0 + 16 * RT, packed), i0, row0, h, split_i,
+                                len, min(32 * t1, n_keys), wave, waves, lane);
+      return;
     }
   }
   join();

@@ -208,6 +208,49 @@ def test_infinite_values_reach_their_channel(case, dtype):
     assert attention_errors(pool, got, q, rows, group, dtype, look) <= 1
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8"])
+def test_queries_that_are_not_finite_stay_among_themselves(fmt, dtype):
+    """NaN and infinite queries in blocks whose rows list pages of their own, one
+    of which holds a value that is not finite."""
+    say(f"paged attention, queries that are not finite {fmt} {dtype}")
+    for lens, rows, group, k in (([300], [9], 2, 5), ([2500, 70], [3, 4], 1, 4), ([2500], [3], 1, 150)):
+        pool = Pool(fmt, lens, 1, 64, 16, seed=61)
+        rng = np.random.default_rng(62)
+        pages = _lists(lens, rows, k, rng)
+        look = _looked_at(pages, lens, rows)
+        q = rnd(rng.standard_normal((sum(rows), group * 64)), dtype)
+        q[0, 5], q[2, 64 * group - 1] = np.nan, np.inf
+        bad = np.zeros((sum(rows), group), bool)
+        bad[0, 0] = bad[2, group - 1] = True
+        for poisoned in (False, True):
+            if poisoned:  # token 1 of the first sequence: rows that list page 0 are NaN whole
+                at = int(pool.table[0, 0])
+                if fmt == "bf16":
+                    pool.dv[0, at, 0, 1] = float("nan")
+                else:
+                    pool.dv[0, at, 0, 1] = 0x7F if fmt == "e4m3" else 0
+                    pool.dve[0, at, 0, 1] = 255
+                bad[:rows[0]] |= look[0][:, 0, 1][:, None]
+            got = attention(pool, dev(q, TORCH[dtype]), rows, group, dtype, i32(pages)).double().cpu().numpy()
+            got = got.reshape(sum(rows), group, 64)
+            assert np.array_equal(np.isnan(got).all(-1), bad) and np.array_equal(np.isnan(got).any(-1), bad)
+            if poisoned:  # (the oracle's own zero weights times NaN)
+                pool.dv[0, at, 0, 1] = 0
+                if fmt != "bf16":
+                    pool.dve[0, at, 0, 1] = 127
+            fine = np.where(bad.repeat(64, 1), 0.0, q)  # queries of zero in place of those that are not finite
+            want = np.where(bad[..., None], 0.0, got)
+            for b, off in enumerate(offsets(rows)[:-1]):
+                for i in range(rows[b]):
+                    for g in range(group):
+                        if bad[off + i, g]:
+                            o, _, _ = ref.attention(fine[off + i, 64 * g:64 * g + 64][None], pool.seq("k", b)[:, 0],
+                                                    pool.seq("v", b)[:, 0], look[b][i])
+                            want[off + i, g] = o[0]
+            assert attention_errors(pool, want, fine, rows, group, dtype, look) <= 1
+
+
 # ------------------------------------------------------------------ the largest finite rows
 
 def _top_rows(dh):
