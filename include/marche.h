@@ -504,14 +504,15 @@ marche_status_t marche_paged_bounds(const marche_paged_cache_t *cache, int32_t l
  * rows, and
  *   score = max over the query heads of the key head of
  *           2^(eq + eb) * sum_d (q_d > 0 ? q_d * hi_d : q_d * lo_d),
- * a whole number times a power of two: exact, whatever the order (magnitudes
- * below the float32 range: 0, above it: infinity).  Equal scores go to the lower page; NaN
- * (queries or keys that are not finite) ranks below every number, -infinity among them, and
- * counts in the maximum only where every query head's score is NaN.  Logical pages are written in ascending
- * order to pages[r][head][0 .. n_select), then -1 where the sequence has fewer.
- * q: rows of [n_q_heads][head_dim], q_stride apart.  1 <= n_select,
- * max_pages <= 4096; q_total * n_q_heads < 2^30, less where a launch of 2^32 threads would
- * not do (UNSUPPORTED).  Needs cache->bounds, up to date for every page below lens. */
+ * a whole number times a power of two: exact, whatever the order, within
+ * float32's normal range (magnitudes below it are rounded, down to 0, those above it are
+ * infinite).  Equal scores go to the lower page; NaN (queries or keys that are not
+ * finite; also a page outside the pool) ranks below every number, -infinity among
+ * them, and counts in the maximum only where every query head's score is NaN.
+ * Logical pages are written in ascending order to pages[r][head][0 .. n_select),
+ * then -1 where the sequence has fewer.  q: rows of [n_q_heads][head_dim], q_stride
+ * apart.  1 <= n_select, max_pages <= 4096; q_total * n_q_heads < 2^30, less where
+ * a launch of 2^32 threads would not do (UNSUPPORTED).  Needs cache->bounds, up to date for every page below lens. */
 marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t layer,
                                     const int32_t *page_table, int32_t max_pages,
                                     const int32_t *lens, int32_t n_seqs, const void *q,

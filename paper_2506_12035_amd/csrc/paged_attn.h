@@ -31,10 +31,10 @@
 //
 // Softmax statistics and O are float32; the maximum that P is taken against
 // trails the true one by at most 2^8, which saves most rescales.  P is rounded
-// to bf16 (half a step, 2^-8 of each weight; the products' other operand V
-// is exact in bf16 for every format, int8 with its exponent in P).  float32 rows are split into three bf16
-// parts (24 bits, nothing lost) and so is P; infinite keys and values meet the
-// first parts only (a second pass, where there are any).
+// to bf16 (half a step, 2^-8 of each weight; the products' other operand V is
+// exact in bf16 for every format, int8 with its exponent in P).  float32 rows are
+// split into three bf16 parts (24 bits, nothing lost) and so is P; infinite keys
+// and values meet the first parts only (a second pass, where there are any).
 //
 // Bound: single rows by the cache's bytes (16 int8 caches of 4000 .. 32768
 // tokens, 607 MB: 119 us, 118 at a copy's rate); many rows by the latency of
