@@ -554,6 +554,96 @@ marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_
                                        int32_t n_select, void *workspace, size_t workspace_bytes,
                                        marche_stream_t stream);
 
+/* ---- Positions, windows and drafted trees on the paged cache ---- */
+
+/* Rotation by positions (host struct).  Pair i < n_pairs of a head's channels, x and
+ * y, becomes  (x cos t - y sin t, y cos t + x sin t),  t = position on axis[i] *
+ * freq[i] radians; channels of no pair stay as they are.  HALVES: pair i is channels i
+ * and i + n_pairs (n_pairs a multiple of 4); NEIGHBOURS: 2 i and 2 i + 1.
+ * 0 <= n_pairs <= head_dim / 2; 1 <= n_axes <= 4, axis[i] < n_axes; |freq[i]| <= 2^16.
+ * The struct may be filled directly or by marche_rotary_init: axis a has axis_pairs[a]
+ * pairs (>= 0, their sum n_pairs), those of axis 0 first, and freq[i] = base^(-i /
+ * n_pairs), or with per_axis base^(-j / axis_pairs[a]) for the axis's pair j, so that
+ * every axis has all frequencies.  base > 0, finite. */
+typedef enum { MARCHE_ROTARY_HALVES = 0, MARCHE_ROTARY_NEIGHBOURS = 1 } marche_rotary_layout_t;
+typedef struct {
+  double freq[64];
+  uint8_t axis[64];
+  int32_t n_pairs, n_axes;
+  int32_t layout; /* marche_rotary_layout_t */
+} marche_rotary_t;
+marche_status_t marche_rotary_init(marche_rotary_t *rotary, int32_t head_dim, int32_t layout,
+                                   int32_t n_axes, const int32_t *axis_pairs, int32_t per_axis,
+                                   double base);
+
+/* marche_paged_write with the rotation on the way: row r's keys, turned by its
+ * positions pos[axis][r] (pos [rotary->n_axes][a_total] int32, device, any sign; NULL: a_idx[r] on
+ * every axis), and its values become token a_idx[r] of its sequence, and its queries,
+ * turned likewise, go to row r of q_out (rows q_out_stride apart).  Angles are formed in 64
+ * bits, the rotation in float32; keys are rounded once, to the cache's format, queries to
+ * `dtype`.  Keys whose turned values pass float32's range are stored as a row that is
+ * not finite.  q, k_new and v_new: rows of [n_q_heads][head_dim] and [n_heads][head_dim]
+ * elements of `dtype` at distance row_stride.  q_out may be q where q_out_stride is
+ * row_stride; no other output may overlap an input.  Queries are turned whatever becomes of
+ * their row's token (one that is negative, at or past max_pages * page_size or of a
+ * page outside the pool is not written).  q and q_out NULL, n_q_heads 0: keys and
+ * values alone.  a_total * (n_q_heads + 2 n_heads) < 2^28, for head_dim 80 and 128 <= 2^28 -
+ * 16.  Bounds of the pages (marche_paged_bounds) are of the turned keys. */
+marche_status_t marche_paged_append(const marche_paged_cache_t *cache, int32_t layer,
+                                    const int32_t *page_table, int32_t max_pages, int32_t n_seqs,
+                                    const int32_t *a_idx, const int32_t *a_off, int32_t a_total,
+                                    const marche_rotary_t *rotary, const int32_t *pos,
+                                    const void *q, int32_t n_q_heads, const void *k_new,
+                                    const void *v_new, int64_t row_stride, int32_t dtype,
+                                    void *q_out, int64_t q_out_stride, marche_stream_t stream);
+
+/* marche_paged_attention for rows that stand at tokens: row r, at token t = q_idx[r] of its
+ * sequence ([q_total] int32, device), sees the cached tokens j with
+ *   j < lens[b],  j <= t,  and  j > t - window or j < sinks,
+ * so the last `window` tokens up to its own and the sequence's first `sinks` ones (window
+ * INT32_MAX: every token up to its own, for t < INT32_MAX).  window >= 1, sinks >= 0.  t may lie past lens[b]
+ * (its keys not yet written) or be negative (the row sees nothing); a row that sees nothing
+ * gets zeros.  Rows may stand in any order, and run fastest where those of a sequence follow
+ * each other.  Pages whose tokens no row sees are not looked at: their table entries may be -1
+ * (MARCHE_VALIDATE checks no page here).  Masked keys and values count nothing, whatever
+ * they are.  Everything else as in marche_paged_attention, the limits too; the workspace
+ * query likewise (for these sizes; 0 for sizes that the call refuses). */
+size_t marche_paged_attention_window_workspace_bytes(const marche_paged_cache_t *cache,
+                                                     int32_t n_seqs, int32_t q_total,
+                                                     int32_t q_max, int32_t n_q_heads,
+                                                     int32_t len_max, int32_t window,
+                                                     int32_t sinks);
+marche_status_t marche_paged_attention_window(const marche_paged_cache_t *cache, int32_t layer,
+                                              const int32_t *page_table, int32_t max_pages,
+                                              const int32_t *lens, int32_t len_max, int32_t n_seqs,
+                                              const void *q, int64_t q_stride,
+                                              const int32_t *q_idx, const int32_t *q_off,
+                                              int32_t q_total, int32_t q_max, int32_t n_q_heads,
+                                              int32_t dtype, int32_t window, int32_t sinks, void *o,
+                                              void *workspace, size_t workspace_bytes,
+                                              marche_stream_t stream);
+
+/* marche_paged_attention for a tree of drafted tokens that lie in the cache behind the
+ * context they continue: of sequence b's tokens, row r sees
+ *   j < min(ctx[b], lens[b]),  and  ctx[b] <= j < lens[b]  where bit i % 32 of
+ *   mask[r][i / 32] is set,  i = j - ctx[b]
+ * (a drafted token: itself and its ancestors; any other mask will do too).  ctx [n_seqs]
+ * int32 (device; a negative one counts as 0); mask [q_total][mask_words] uint32 (device),
+ * 1 <= mask_words <= 64; drafted tokens past 32 * mask_words are not seen.  A row that
+ * sees nothing gets zeros.  Masked keys and values count nothing, whatever they are.
+ * Everything else as in marche_paged_attention; the workspace query likewise. */
+size_t marche_paged_attention_tree_workspace_bytes(const marche_paged_cache_t *cache,
+                                                   int32_t n_seqs, int32_t q_total, int32_t q_max,
+                                                   int32_t n_q_heads, int32_t len_max);
+marche_status_t marche_paged_attention_tree(const marche_paged_cache_t *cache, int32_t layer,
+                                            const int32_t *page_table, int32_t max_pages,
+                                            const int32_t *lens, int32_t len_max, int32_t n_seqs,
+                                            const void *q, int64_t q_stride, const int32_t *q_off,
+                                            int32_t q_total, int32_t q_max, int32_t n_q_heads,
+                                            int32_t dtype, const int32_t *ctx, const uint32_t *mask,
+                                            int32_t mask_words, void *o, void *workspace,
+                                            size_t workspace_bytes, marche_stream_t stream);
+
 /* Name of a status code (static string). */
 const char *marche_status_string(marche_status_t s);
 

@@ -108,3 +108,34 @@ def attention(q, k, v, look=None):
         o[i], a[i] = w @ v[at], w @ np.abs(v[at])
         d[i] = (np.abs(k[at]) @ np.abs(q[i])).max() / np.sqrt(q.shape[1])
     return o, a, d
+
+
+def rotate(x, pos, freq, axis, layout):
+    """Rows [rows][heads][head_dim] turned by positions [axes][rows]: pair i (frequency
+    freq[i], axis axis[i]) is channels i and i + pairs ("halves") or 2 i and 2 i + 1."""
+    y = np.array(x, np.float64)
+    n = len(freq)
+    for i in range(n):
+        one, two = (i, i + n) if layout == "halves" else (2 * i, 2 * i + 1)
+        t = (np.asarray(pos, np.float64)[axis[i]] * freq[i])[:, None]
+        a, b = np.array(x, np.float64)[..., one], np.array(x, np.float64)[..., two]
+        y[..., one], y[..., two] = a * np.cos(t) - b * np.sin(t), b * np.cos(t) + a * np.sin(t)
+    return y
+
+
+def window(t, n, size, sinks):
+    """Which of n tokens rows at tokens t see: [rows][n]."""
+    t, j = np.asarray(t, np.int64)[:, None], np.arange(n)[None]
+    return (j <= t) & ((j > t - size) | (j < sinks))
+
+
+def tree(mask, n, ctx):
+    """Which of n tokens rows with masks [rows][words] (uint32) see behind `ctx` tokens."""
+    mask = np.asarray(mask).view(np.uint32)
+    look = np.zeros((len(mask), n), bool)
+    ctx = max(int(ctx), 0)
+    look[:, :ctx] = True
+    bits = (mask[:, :, None] >> np.arange(32, dtype=np.uint32) & 1).reshape(len(mask), 32 * mask.shape[1]) == 1
+    m = max(0, min(n - ctx, bits.shape[1]))
+    look[:, ctx:ctx + m] = bits[:, :m]
+    return look

@@ -23,6 +23,7 @@ MARCHE_F32, MARCHE_BF16 = 0, 1
 MARCHE_SELECT_HIGHEST, MARCHE_SELECT_LOWEST = 0, 1
 MARCHE_ATTN_TWO_SEGMENT, MARCHE_ATTN_CONCAT = 0, 1
 MARCHE_CACHE_BF16, MARCHE_CACHE_E4M3, MARCHE_CACHE_INT8 = 0, 1, 2
+MARCHE_ROTARY_HALVES, MARCHE_ROTARY_NEIGHBOURS = 0, 1
 
 EXPORTED = (
     "kv_cache_init", "marche_step_workspace_bytes", "marche_step", "marche_step_images",
@@ -34,6 +35,9 @@ EXPORTED = (
     "marche_paged_cache_bytes", "marche_paged_cache_init", "marche_paged_write",
     "marche_paged_read", "marche_paged_bounds", "marche_paged_select",
     "marche_paged_attention_workspace_bytes", "marche_paged_attention",
+    "marche_rotary_init", "marche_paged_append",
+    "marche_paged_attention_window_workspace_bytes", "marche_paged_attention_window",
+    "marche_paged_attention_tree_workspace_bytes", "marche_paged_attention_tree",
     "marche_status_string", "marche_last_error",
     "marche_profile_enable", "marche_profile_collect", "marche_profile_entry",
     "marche_profile_reset",
@@ -73,6 +77,11 @@ class PagedCache(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_exp", "v_exp", "bounds", "bounds_exp")] + [
         (n, C.c_int32) for n in ("n_layers", "n_pages", "n_heads", "page_size", "head_dim",
                                  "format")]
+
+
+class Rotary(C.Structure):
+    _fields_ = [("freq", C.c_double * 64), ("axis", C.c_uint8 * 64), ("n_pairs", C.c_int32),
+                ("n_axes", C.c_int32), ("layout", C.c_int32)]
 
 
 class MarcheError(RuntimeError):
@@ -133,6 +142,18 @@ def lib() -> C.CDLL:
         L.marche_paged_attention_workspace_bytes.restype = sz
         L.marche_paged_attention.argtypes = [pc, i32, vp, i32, vp, i32, i32, vp, i64, vp, i32, i32,
                                              i32, i32, vp, vp, i32, vp, sz, vp]
+        pr, f64 = C.POINTER(Rotary), C.c_double
+        L.marche_rotary_init.argtypes = [pr, i32, i32, i32, C.POINTER(i32), i32, f64]
+        L.marche_paged_append.argtypes = [pc, i32, vp, i32, i32, vp, vp, i32, pr, vp, vp, i32, vp,
+                                          vp, i64, i32, vp, i64, vp]
+        L.marche_paged_attention_window_workspace_bytes.argtypes = [pc] + [i32] * 7
+        L.marche_paged_attention_window_workspace_bytes.restype = sz
+        L.marche_paged_attention_window.argtypes = [pc, i32, vp, i32, vp, i32, i32, vp, i64, vp, vp,
+                                                    i32, i32, i32, i32, i32, i32, vp, vp, sz, vp]
+        L.marche_paged_attention_tree_workspace_bytes.argtypes = [pc] + [i32] * 5
+        L.marche_paged_attention_tree_workspace_bytes.restype = sz
+        L.marche_paged_attention_tree.argtypes = [pc, i32, vp, i32, vp, i32, i32, vp, i64, vp, i32,
+                                                  i32, i32, i32, vp, vp, i32, vp, vp, sz, vp]
         L.marche_status_string.argtypes = [C.c_int]
         L.marche_status_string.restype = C.c_char_p
         L.marche_last_error.argtypes = []
@@ -152,7 +173,9 @@ def lib() -> C.CDLL:
                      "marche_encoder_input", "marche_encoder_to_decoder",
                      "marche_diffusion_sample", "marche_paged_cache_init", "marche_paged_write",
                      "marche_paged_read", "marche_paged_bounds", "marche_paged_select",
-                     "marche_paged_attention", "marche_profile_enable", "marche_profile_entry"):
+                     "marche_paged_attention", "marche_rotary_init", "marche_paged_append",
+                     "marche_paged_attention_window", "marche_paged_attention_tree",
+                     "marche_profile_enable", "marche_profile_entry"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -401,6 +424,58 @@ def paged_attention(cache: PagedCache, layer: int, page_table, max_pages: int, l
                                         _ptr(q_off), q_total, q_max, n_q_heads, dtype, _ptr(o),
                                         _ptr(pages), n_select, _ptr(workspace), workspace_bytes,
                                         _stream(stream)))
+
+
+def rotary(head_dim: int, layout: int, axis_pairs: Sequence[int], per_axis: bool = False,
+           base: float = 10000.0) -> Rotary:
+    """Rotation by positions whose axes have these numbers of channel pairs, one after another."""
+    r = Rotary()
+    _check(lib().marche_rotary_init(C.byref(r), head_dim, layout, len(axis_pairs),
+                                    (C.c_int32 * max(1, len(axis_pairs)))(*axis_pairs),
+                                    1 if per_axis else 0, base))
+    return r
+
+
+def paged_append(cache: PagedCache, layer: int, page_table, max_pages: int, n_seqs: int, a_idx,
+                 a_off, a_total: int, rotary: Rotary, pos, q, n_q_heads: int, k_new, v_new,
+                 row_stride: int, dtype: int, q_out, q_out_stride: int, stream=None) -> None:
+    _check(lib().marche_paged_append(C.byref(cache), layer, _ptr(page_table), max_pages, n_seqs,
+                                     _ptr(a_idx), _ptr(a_off), a_total, C.byref(rotary), _ptr(pos),
+                                     _ptr(q), n_q_heads, _ptr(k_new), _ptr(v_new), row_stride,
+                                     dtype, _ptr(q_out), q_out_stride, _stream(stream)))
+
+
+def paged_attention_window_workspace_bytes(cache: PagedCache, n_seqs: int, q_total: int,
+                                           q_max: int, n_q_heads: int, len_max: int, window: int,
+                                           sinks: int) -> int:
+    return lib().marche_paged_attention_window_workspace_bytes(
+        C.byref(cache), n_seqs, q_total, q_max, n_q_heads, len_max, window, sinks)
+
+
+def paged_attention_window(cache: PagedCache, layer: int, page_table, max_pages: int, lens,
+                           len_max: int, n_seqs: int, q, q_stride: int, q_idx, q_off, q_total: int,
+                           q_max: int, n_q_heads: int, dtype: int, window: int, sinks: int, o,
+                           workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().marche_paged_attention_window(
+        C.byref(cache), layer, _ptr(page_table), max_pages, _ptr(lens), len_max, n_seqs, _ptr(q),
+        q_stride, _ptr(q_idx), _ptr(q_off), q_total, q_max, n_q_heads, dtype, window, sinks,
+        _ptr(o), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def paged_attention_tree_workspace_bytes(cache: PagedCache, n_seqs: int, q_total: int, q_max: int,
+                                         n_q_heads: int, len_max: int) -> int:
+    return lib().marche_paged_attention_tree_workspace_bytes(C.byref(cache), n_seqs, q_total,
+                                                             q_max, n_q_heads, len_max)
+
+
+def paged_attention_tree(cache: PagedCache, layer: int, page_table, max_pages: int, lens,
+                         len_max: int, n_seqs: int, q, q_stride: int, q_off, q_total: int,
+                         q_max: int, n_q_heads: int, dtype: int, ctx, mask, mask_words: int, o,
+                         workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().marche_paged_attention_tree(
+        C.byref(cache), layer, _ptr(page_table), max_pages, _ptr(lens), len_max, n_seqs, _ptr(q),
+        q_stride, _ptr(q_off), q_total, q_max, n_q_heads, dtype, _ptr(ctx), _ptr(mask), mask_words,
+        _ptr(o), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def profile_enable(on: bool) -> None:

@@ -4,7 +4,7 @@
 namespace marche {
 
 hipError_t launch_paged_attention_bf16(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s) {
-  return launch_paged_fmt<BF>(dt, head_dim, a, s);
+  return launch_paged_fmt<BF, false>(dt, head_dim, a, s);
 }
 
 }  // namespace marche

@@ -114,7 +114,7 @@ enum KClass {
   K_FILL, K_ATTN2_W1, K_ATTN2_W2, K_ATTN2_W4, K_CONCAT, K_ATTN_RES, K_ENC_INPUT, K_MASK_FILL,
   K_LN_ROWS, K_TIME_SINUS, K_HEAD_SILU_COND, K_HEAD_MOD, K_HEAD_STEP, K_TRANSPOSE, K_ATTN_RES_SC,
   K_ATTN_W8, K_ATTN_SC, K_PAGED_WRITE, K_PAGED_READ, K_PAGED_BOUNDS, K_PAGED_SELECT, K_PAGED_ATTN,
-  K_PAGED_JOIN,
+  K_PAGED_JOIN, K_PAGED_APPEND, K_PAGED_WINDOW, K_PAGED_TREE,
   K_GEMM_FIRST  // then, per projection, one class per tile and the few-row kernel
 };
 const char *const kClassNames[K_GEMM_FIRST] = {
@@ -124,7 +124,7 @@ const char *const kClassNames[K_GEMM_FIRST] = {
     "mask_fill",      "ln_rows",        "time_sinus",     "head_silu_cond",      "head_mod",
     "head_step",      "transpose",      "attention_res_scores", "attention_q256", "attention_scores",
     "paged_write",    "paged_read",     "paged_bounds",   "paged_select",        "paged_attention",
-    "paged_join"};
+    "paged_join",     "paged_append",   "paged_window",   "paged_tree"};
 static_assert(sizeof(kClassNames) / sizeof(kClassNames[0]) == K_GEMM_FIRST, "one name per class");
 
 enum GemmProj { P_QKV, P_O, P_FC1, P_FC2, P_EMBED, P_HEAD, P_HEAD_SILU, P_COUNT };
@@ -1131,7 +1131,8 @@ bool misaligned(const void *p) { return reinterpret_cast<uintptr_t>(p) & 15; }
 // MARCHE_VALIDATE: the device lists of a call, copied to the host.
 struct PagedLists {
   const int32_t *page_table = nullptr, *lens = nullptr, *off = nullptr, *idx = nullptr,
-                *first = nullptr, *pages = nullptr;
+                *first = nullptr, *pages = nullptr, *ctx = nullptr;
+  bool any_page = false;  // pages of tokens below lens may lie outside the pool
   int32_t n_seqs = 0, max_pages = 0, total = 0, row_max = 0, len_max = INT32_MAX, n_select = 0;
   int32_t rows = 0;  // of idx and pages on the host: none behind the last sequence's
 };
@@ -1153,9 +1154,10 @@ const char *check_lists(const PagedLists &l, const marche_paged_cache_t *c, int3
     if (r0 < 0 || r1 < r0 || r1 > l.rows || r1 - r0 > l.row_max) return say("row offsets inconsistent", b);
     if (l.lens) {
       if (l.lens[b] < 0 || l.lens[b] > cap || l.lens[b] > l.len_max) return say("length out of range", b);
-      for (int64_t t = 0; t < l.lens[b]; t += c->page_size)
+      for (int64_t t = 0; t < l.lens[b] && !l.any_page; t += c->page_size)
         if (!page_ok(b, t)) return say("page outside the pool", b);
     }
+    if (l.ctx && (l.ctx[b] < 0 || l.ctx[b] > l.lens[b])) return say("context out of range", b);
     if (l.first && l.first[b] > l.lens[b]) return say("first token out of range", b);
     if (l.idx) {
       std::vector<int32_t> seen(l.idx + r0, l.idx + r1);
@@ -1185,11 +1187,12 @@ marche_status_t validate_paged(PagedLists l, const marche_paged_cache_t *c, hipS
     if (n) e = hipMemcpyAsync(kept.back().data(), p, n * 4, hipMemcpyDeviceToHost, stream);
     p = kept.back().data();
   };
-  kept.reserve(6);
+  kept.reserve(7);
   fetch(l.page_table, (size_t)l.n_seqs * l.max_pages);
   fetch(l.lens, l.n_seqs);
   fetch(l.off, (size_t)l.n_seqs + 1);
   fetch(l.first, l.n_seqs);
+  fetch(l.ctx, l.n_seqs);
   l.rows = l.total;
   if (l.off && e == hipSuccess && (e = hipStreamSynchronize(stream)) == hipSuccess)
     l.rows = std::min(std::max(l.off[l.n_seqs], 0), l.total);
@@ -1207,6 +1210,7 @@ marche_status_t validate_paged(PagedLists l, const marche_paged_cache_t *c, hipS
 // The kernel arguments that the workspace query and the call share.
 void paged_attn_sizes(PagedAttnArgs &p, const marche_paged_cache_t *c, int32_t n_seqs, int32_t q_total,
                       int32_t q_max, int32_t n_q_heads, int32_t len_max, int32_t n_select, DType dt) {
+  if (p.look == PAGED_ALL && n_select > 0) p.look = PAGED_LISTED;
   p.n_pages = c->n_pages;
   p.n_heads = c->n_heads;
   p.page_log2 = __builtin_ctz((unsigned)c->page_size);
@@ -1448,9 +1452,11 @@ marche_status_t marche_paged_select(const marche_paged_cache_t *cache, int32_t l
   return MARCHE_OK;
 }
 
-size_t marche_paged_attention_workspace_bytes(const marche_paged_cache_t *cache, int32_t n_seqs,
-                                              int32_t q_total, int32_t q_max, int32_t n_q_heads,
-                                              int32_t len_max, int32_t n_select) {
+namespace {
+
+// Bytes of workspace for either type of rows; `look` has the mask's sizes.
+size_t attention_workspace(const PagedAttnArgs &look, const marche_paged_cache_t *cache, int32_t n_seqs,
+                           int32_t q_total, int32_t q_max, int32_t n_q_heads, int32_t len_max, int32_t n_select) {
   marche_status_t st;
   if (!cache || !paged_shape(cache->n_layers, cache->n_pages, cache->n_heads, cache->page_size,
                              cache->head_dim, raw_enum(cache->format), &st) ||
@@ -1459,8 +1465,8 @@ size_t marche_paged_attention_workspace_bytes(const marche_paged_cache_t *cache,
       (int64_t)q_total * n_q_heads >= PAGED_MAX_ROWS)
     return 0;
   size_t need = 0;
-  for (DType dt : {DType::BF16, DType::F32}) {  // either type of rows
-    PagedAttnArgs p{};
+  for (DType dt : {DType::BF16, DType::F32}) {
+    PagedAttnArgs p = look;
     paged_attn_sizes(p, cache, n_seqs, q_total, q_max, n_q_heads, len_max, n_select, dt);
     if (!paged_launchable(p)) continue;
     const size_t rows = paged_part_rows(p);
@@ -1469,14 +1475,14 @@ size_t marche_paged_attention_workspace_bytes(const marche_paged_cache_t *cache,
   return need;
 }
 
-marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_t layer,
-                                       const int32_t *page_table, int32_t max_pages,
-                                       const int32_t *lens, int32_t len_max, int32_t n_seqs,
-                                       const void *q, int64_t q_stride, const int32_t *q_off,
-                                       int32_t q_total, int32_t q_max, int32_t n_q_heads,
-                                       int32_t dtype, void *o, const int32_t *pages,
-                                       int32_t n_select, void *workspace, size_t workspace_bytes,
-                                       marche_stream_t stream_) {
+// The three attention calls, which differ in what `a` says of the keys that a row sees.
+// `ready`: whether the call's own arrays are there; `l`: its lists.
+marche_status_t run_attention(const char *name, int cls, PagedAttnArgs a, PagedLists lists, bool ready,
+                              const marche_paged_cache_t *cache, int32_t layer, const int32_t *page_table,
+                              int32_t max_pages, const int32_t *lens, int32_t len_max, int32_t n_seqs,
+                              const void *q, int64_t q_stride, const int32_t *q_off, int32_t q_total,
+                              int32_t q_max, int32_t n_q_heads, int32_t dtype, void *o, int32_t n_select,
+                              void *workspace, size_t workspace_bytes, hipStream_t stream) {
   PagedLayer l;
   marche_status_t st = check_paged(cache, layer, max_pages, n_seqs, &l);
   if (st != MARCHE_OK) return st;
@@ -1488,24 +1494,22 @@ marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_
   if (q_max < 0 || q_max > q_total || (q_total > 0 && q_max == 0) ||
       (!q_off && n_seqs > 0 && q_max != q_total / n_seqs))
     return fail(MARCHE_ERR_INVALID_ARG, "q_max=%d inconsistent with q_total=%d", q_max, q_total);
-  if (!pages && n_select != 0) return fail(MARCHE_ERR_INVALID_ARG, "n_select=%d without pages", n_select);
-  if (pages && (n_select < 1 || n_select > PAGED_MAX_PAGES))
+  if (!a.pages && n_select != 0) return fail(MARCHE_ERR_INVALID_ARG, "n_select=%d without pages", n_select);
+  if (a.pages && (n_select < 1 || n_select > PAGED_MAX_PAGES))
     return fail(MARCHE_ERR_INVALID_ARG, "n_select=%d outside [1, %d]", n_select, PAGED_MAX_PAGES);
-  if (pages && max_pages > PAGED_MAX_PAGES)
+  if (a.pages && max_pages > PAGED_MAX_PAGES)
     return fail(MARCHE_ERR_UNSUPPORTED, "max_pages=%d > %d with selected pages", max_pages, PAGED_MAX_PAGES);
   const int32_t dh = cache->head_dim;
   if ((int64_t)q_total * n_q_heads >= PAGED_MAX_ROWS)
     return fail(MARCHE_ERR_UNSUPPORTED, "q_total*n_q_heads reaches 2^30");
   if (q_total == 0) return MARCHE_OK;
   const DType dt = dtype == MARCHE_BF16 ? DType::BF16 : DType::F32;
-  PagedAttnArgs a{};
   a.max_pages = max_pages;
   paged_attn_sizes(a, cache, n_seqs, q_total, q_max, n_q_heads, len_max, n_select, dt);
   if (!paged_launchable(a))
     return fail(MARCHE_ERR_UNSUPPORTED, "n_seqs=%d sequences of up to q_max=%d rows, q_total=%d, are too many for one call",
                 n_seqs, q_max, q_total);
-  if (!page_table || !lens || !q || !o)
-    return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_attention");
+  if (!page_table || !lens || !q || !o || !ready) return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to %s", name);
   if (misaligned(q) || misaligned(o)) return fail(MARCHE_ERR_INVALID_ARG, "q and o must be 16-byte aligned");
   const size_t rows = paged_part_rows(a);
   const size_t need = align256(rows * dh * 4) + align256(rows * 8);
@@ -1514,12 +1518,10 @@ marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_
                 workspace ? "too small" : "is NULL", workspace_bytes, need);
   if (reinterpret_cast<uintptr_t>(workspace) & 255)
     return fail(MARCHE_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-  hipStream_t stream = static_cast<hipStream_t>(stream_);
-  PagedLists lists;
   lists.page_table = page_table;
   lists.lens = lens;
   lists.off = q_off;
-  lists.pages = pages;
+  lists.pages = a.pages;
   lists.n_seqs = n_seqs;
   lists.max_pages = max_pages;
   lists.total = q_total;
@@ -1536,20 +1538,240 @@ marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_
   a.q_off = q_off;
   a.q = q;
   a.o = o;
-  a.pages = pages;
   a.part_o = static_cast<float *>(workspace);
   a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + align256(rows * dh * 4));
   a.q_stride = q_stride;
   a.rows_each = q_total / n_seqs;
   a.sl2 = (float)(1.4426950408889634 / std::sqrt((double)dh));
   // Algorithmic work and traffic as if every sequence had len_max tokens.
-  const double keys = pages ? std::min<double>(len_max, (double)n_select * cache->page_size) : len_max;
-  LAUNCH(K_PAGED_ATTN, 4.0 * q_total * (double)n_q_heads * dh * keys,
+  const double keys = a.pages ? std::min<double>(len_max, (double)n_select * cache->page_size)
+                      : a.look == PAGED_WINDOW ? std::min<double>(len_max, (double)a.window + a.sinks)
+                                               : len_max;
+  LAUNCH(cls, 4.0 * q_total * (double)n_q_heads * dh * keys,
          2.0 * n_seqs * keys * (double)l.row_bytes + 2.0 * q_total * (double)n_q_heads * dh * elem_size(dtype),
          launch_paged_attention(dt, raw_enum(cache->format), dh, a, stream));
   if (a.splits > 1)
     LAUNCH(K_PAGED_JOIN, 0, (double)rows * (dh + 2) * 4 + (double)q_total * n_q_heads * dh * elem_size(dtype),
            launch_paged_join(dt, dh, a, stream));
+  return MARCHE_OK;
+}
+
+}  // namespace
+
+size_t marche_paged_attention_workspace_bytes(const marche_paged_cache_t *cache, int32_t n_seqs,
+                                              int32_t q_total, int32_t q_max, int32_t n_q_heads,
+                                              int32_t len_max, int32_t n_select) {
+  return attention_workspace(PagedAttnArgs{}, cache, n_seqs, q_total, q_max, n_q_heads, len_max, n_select);
+}
+
+marche_status_t marche_paged_attention(const marche_paged_cache_t *cache, int32_t layer,
+                                       const int32_t *page_table, int32_t max_pages,
+                                       const int32_t *lens, int32_t len_max, int32_t n_seqs,
+                                       const void *q, int64_t q_stride, const int32_t *q_off,
+                                       int32_t q_total, int32_t q_max, int32_t n_q_heads,
+                                       int32_t dtype, void *o, const int32_t *pages,
+                                       int32_t n_select, void *workspace, size_t workspace_bytes,
+                                       marche_stream_t stream) {
+  PagedAttnArgs a{};
+  a.pages = pages;
+  return run_attention("marche_paged_attention", K_PAGED_ATTN, a, PagedLists(), true, cache, layer, page_table,
+                       max_pages, lens, len_max, n_seqs, q, q_stride, q_off, q_total, q_max, n_q_heads, dtype, o,
+                       n_select, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+size_t marche_paged_attention_window_workspace_bytes(const marche_paged_cache_t *cache,
+                                                     int32_t n_seqs, int32_t q_total,
+                                                     int32_t q_max, int32_t n_q_heads,
+                                                     int32_t len_max, int32_t window,
+                                                     int32_t sinks) {
+  if (window < 1 || sinks < 0) return 0;
+  PagedAttnArgs a{};
+  a.look = PAGED_WINDOW;
+  a.window = window;
+  a.sinks = sinks;
+  return attention_workspace(a, cache, n_seqs, q_total, q_max, n_q_heads, len_max, 0);
+}
+
+marche_status_t marche_paged_attention_window(const marche_paged_cache_t *cache, int32_t layer,
+                                              const int32_t *page_table, int32_t max_pages,
+                                              const int32_t *lens, int32_t len_max, int32_t n_seqs,
+                                              const void *q, int64_t q_stride,
+                                              const int32_t *q_idx, const int32_t *q_off,
+                                              int32_t q_total, int32_t q_max, int32_t n_q_heads,
+                                              int32_t dtype, int32_t window, int32_t sinks, void *o,
+                                              void *workspace, size_t workspace_bytes,
+                                              marche_stream_t stream) {
+  if (window < 1) return fail(MARCHE_ERR_INVALID_ARG, "window=%d < 1", window);
+  if (sinks < 0) return fail(MARCHE_ERR_INVALID_ARG, "sinks=%d < 0", sinks);
+  PagedAttnArgs a{};
+  a.look = PAGED_WINDOW;
+  a.q_idx = q_idx;
+  a.window = window;
+  a.sinks = sinks;
+  PagedLists lists;
+  lists.any_page = true;
+  return run_attention("marche_paged_attention_window", K_PAGED_WINDOW, a, lists, q_idx != nullptr, cache, layer,
+                       page_table, max_pages, lens, len_max, n_seqs, q, q_stride, q_off, q_total, q_max, n_q_heads,
+                       dtype, o, 0, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+size_t marche_paged_attention_tree_workspace_bytes(const marche_paged_cache_t *cache,
+                                                   int32_t n_seqs, int32_t q_total, int32_t q_max,
+                                                   int32_t n_q_heads, int32_t len_max) {
+  PagedAttnArgs a{};
+  a.look = PAGED_TREE;
+  return attention_workspace(a, cache, n_seqs, q_total, q_max, n_q_heads, len_max, 0);
+}
+
+marche_status_t marche_paged_attention_tree(const marche_paged_cache_t *cache, int32_t layer,
+                                            const int32_t *page_table, int32_t max_pages,
+                                            const int32_t *lens, int32_t len_max, int32_t n_seqs,
+                                            const void *q, int64_t q_stride, const int32_t *q_off,
+                                            int32_t q_total, int32_t q_max, int32_t n_q_heads,
+                                            int32_t dtype, const int32_t *ctx, const uint32_t *mask,
+                                            int32_t mask_words, void *o, void *workspace,
+                                            size_t workspace_bytes, marche_stream_t stream) {
+  if (mask_words < 1 || mask_words > PAGED_MAX_MASK_WORDS)
+    return fail(MARCHE_ERR_INVALID_ARG, "mask_words=%d outside [1, %d]", mask_words, PAGED_MAX_MASK_WORDS);
+  PagedAttnArgs a{};
+  a.look = PAGED_TREE;
+  a.ctx = ctx;
+  a.mask = mask;
+  a.mask_words = mask_words;
+  PagedLists lists;
+  lists.ctx = ctx;
+  return run_attention("marche_paged_attention_tree", K_PAGED_TREE, a, lists, ctx && mask, cache, layer, page_table,
+                       max_pages, lens, len_max, n_seqs, q, q_stride, q_off, q_total, q_max, n_q_heads, dtype, o, 0,
+                       workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+namespace {
+
+marche_status_t check_rotary(const marche_rotary_t *r, int32_t head_dim) {
+  if (!r) return fail(MARCHE_ERR_INVALID_ARG, "rotary is NULL");
+  const int32_t layout = raw_enum(r->layout);
+  if (layout != MARCHE_ROTARY_HALVES && layout != MARCHE_ROTARY_NEIGHBOURS)
+    return fail(MARCHE_ERR_INVALID_ARG, "rotary.layout=%d is not supported", layout);
+  if (r->n_pairs < 0 || r->n_pairs > head_dim / 2 || (layout == MARCHE_ROTARY_HALVES && r->n_pairs % 4))
+    return fail(MARCHE_ERR_INVALID_ARG, "rotary.n_pairs=%d: must be in [0, head_dim/2=%d]%s", r->n_pairs,
+                head_dim / 2, layout == MARCHE_ROTARY_HALVES ? " and a multiple of 4" : "");
+  if (r->n_axes < 1 || r->n_axes > 4)
+    return fail(MARCHE_ERR_INVALID_ARG, "rotary.n_axes=%d outside [1, 4]", r->n_axes);
+  for (int32_t i = 0; i < r->n_pairs; ++i) {
+    if (r->axis[i] >= r->n_axes)
+      return fail(MARCHE_ERR_INVALID_ARG, "rotary.axis[%d]=%d with n_axes=%d", i, (int)r->axis[i], r->n_axes);
+    if (!(std::fabs(r->freq[i]) <= 65536.0))
+      return fail(MARCHE_ERR_INVALID_ARG, "rotary.freq[%d]=%g past 2^16", i, r->freq[i]);
+  }
+  return MARCHE_OK;
+}
+
+}  // namespace
+
+marche_status_t marche_rotary_init(marche_rotary_t *rotary, int32_t head_dim, int32_t layout,
+                                   int32_t n_axes, const int32_t *axis_pairs, int32_t per_axis,
+                                   double base) {
+  if (!rotary || !axis_pairs) return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_rotary_init");
+  if (head_dim != 64 && head_dim != 80 && head_dim != 128)
+    return fail(MARCHE_ERR_UNSUPPORTED, "head_dim=%d is not supported", head_dim);
+  if (n_axes < 1 || n_axes > 4) return fail(MARCHE_ERR_INVALID_ARG, "n_axes=%d outside [1, 4]", n_axes);
+  if (!(base > 0.0) || !std::isfinite(base)) return fail(MARCHE_ERR_INVALID_ARG, "base=%g must be > 0", base);
+  int32_t total = 0;
+  for (int32_t a = 0; a < n_axes; ++a) {
+    if (axis_pairs[a] < 0 || axis_pairs[a] > head_dim / 2 - total)
+      return fail(MARCHE_ERR_INVALID_ARG, "axis_pairs[%d]=%d: must be >= 0, of at most head_dim/2=%d in all", a,
+                  axis_pairs[a], head_dim / 2);
+    total += axis_pairs[a];
+  }
+  marche_rotary_t r{};
+  r.n_pairs = total;
+  r.n_axes = n_axes;
+  r.layout = layout;
+  for (int32_t a = 0, i = 0; a < n_axes; ++a)
+    for (int32_t j = 0; j < axis_pairs[a]; ++j, ++i) {
+      r.axis[i] = (uint8_t)a;
+      r.freq[i] = std::pow(base, per_axis ? -(double)j / axis_pairs[a] : -(double)i / total);
+    }
+  const marche_status_t st = check_rotary(&r, head_dim);
+  if (st == MARCHE_OK) *rotary = r;
+  return st;
+}
+
+marche_status_t marche_paged_append(const marche_paged_cache_t *cache, int32_t layer,
+                                    const int32_t *page_table, int32_t max_pages, int32_t n_seqs,
+                                    const int32_t *a_idx, const int32_t *a_off, int32_t a_total,
+                                    const marche_rotary_t *rotary, const int32_t *pos,
+                                    const void *q, int32_t n_q_heads, const void *k_new,
+                                    const void *v_new, int64_t row_stride, int32_t dtype,
+                                    void *q_out, int64_t q_out_stride, marche_stream_t stream_) {
+  PagedLayer l;
+  marche_status_t st = check_paged(cache, layer, max_pages, n_seqs, &l);
+  if (st != MARCHE_OK || (st = check_row_dtype(dtype)) != MARCHE_OK) return st;
+  const int32_t H = cache->n_heads, dh = cache->head_dim;
+  if ((st = check_rotary(rotary, dh)) != MARCHE_OK) return st;
+  if (n_q_heads < 0 || n_q_heads % H)
+    return fail(MARCHE_ERR_INVALID_ARG, "n_q_heads=%d is no multiple of the cache's n_heads=%d", n_q_heads, H);
+  if (n_q_heads == 0 && (q || q_out)) return fail(MARCHE_ERR_INVALID_ARG, "q or q_out without query heads");
+  if ((st = check_rows("a", a_total, a_off, n_seqs, row_stride, (int64_t)std::max(n_q_heads, H) * dh)) != MARCHE_OK)
+    return st;
+  if (n_q_heads > 0 && (q_out_stride < (int64_t)n_q_heads * dh || q_out_stride % 8))
+    return fail(MARCHE_ERR_INVALID_ARG, "q_out_stride %lld: must be a multiple of 8, >= %lld", (long long)q_out_stride,
+                (long long)n_q_heads * dh);
+  const int64_t heads = (int64_t)n_q_heads + 2 * H;
+  if (heads >= (1LL << 28) || a_total * heads >= (1LL << 28) || too_many_threads(a_total * heads, paged_write_pairs(dh)))
+    return fail(MARCHE_ERR_UNSUPPORTED, "a_total*(n_q_heads+2*n_heads) reaches 2^28, or all but");
+  if (a_total == 0) return MARCHE_OK;
+  if (!page_table || !a_idx || !k_new || !v_new || (n_q_heads > 0 && (!q || !q_out)))
+    return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_append");
+  if (misaligned(q) || misaligned(k_new) || misaligned(v_new) || misaligned(q_out))
+    return fail(MARCHE_ERR_INVALID_ARG, "q, k_new, v_new and q_out must be 16-byte aligned");
+  if (q_out == q && q && q_out_stride != row_stride)
+    return fail(MARCHE_ERR_INVALID_ARG, "q_out is q, but q_out_stride=%lld differs from row_stride=%lld",
+                (long long)q_out_stride, (long long)row_stride);
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  PagedLists lists;
+  lists.page_table = page_table;
+  lists.off = a_off;
+  lists.idx = a_idx;
+  lists.n_seqs = n_seqs;
+  lists.max_pages = max_pages;
+  lists.total = lists.row_max = a_total;
+  if ((st = validate_paged(lists, cache, stream)) != MARCHE_OK) return st;
+  PagedTurns turns{};
+  for (int32_t i = 0; i < rotary->n_pairs; ++i) {
+    turns.turn[i] = rotary->freq[i] / 6.283185307179586476925;
+    turns.axis[i] = rotary->axis[i];
+  }
+  PagedAppendArgs a{};
+  a.k = l.k;
+  a.v = l.v;
+  a.k_exp = l.k_exp;
+  a.v_exp = l.v_exp;
+  a.table = page_table;
+  a.a_idx = a_idx;
+  a.a_off = a_off;
+  a.pos = pos;
+  a.q = q;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.q_out = q_out;
+  a.row_stride = row_stride;
+  a.q_out_stride = q_out_stride;
+  a.n_pages = cache->n_pages;
+  a.n_heads = H;
+  a.q_heads = n_q_heads;
+  a.page_log2 = l.page_log2;
+  a.max_pages = max_pages;
+  a.n_seqs = n_seqs;
+  a.a_total = a_total;
+  a.rows_each = a_total / n_seqs;
+  a.n_pairs = rotary->n_pairs;
+  // Algorithmic traffic: every new row read once, its slot and its queries written once.
+  LAUNCH(K_PAGED_APPEND, 6.0 * a_total * (n_q_heads + H) * rotary->n_pairs,
+         2.0 * a_total * ((double)(H + n_q_heads) * dh * elem_size(dtype) + l.row_bytes) +
+             4.0 * a_total * (1 + (pos ? rotary->n_axes : 0)),
+         launch_paged_append(dtype == MARCHE_BF16 ? DType::BF16 : DType::F32, raw_enum(cache->format), dh,
+                             raw_enum(rotary->layout) == MARCHE_ROTARY_HALVES, turns, a, stream));
   return MARCHE_OK;
 }
 

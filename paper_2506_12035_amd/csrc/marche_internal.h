@@ -277,6 +277,26 @@ struct PagedWriteArgs {
 constexpr int paged_write_pairs(int32_t head_dim) { return head_dim == 64 ? 32 : 16; }
 hipError_t launch_paged_write(DType dt, int32_t format, int32_t head_dim, PagedWriteArgs a,
                               hipStream_t s);
+// The rotation of an append: of pair i the turns (2 pi) per position, and its axis.
+struct PagedTurns {
+  double turn[64];
+  uint8_t axis[64];
+};
+struct PagedAppendArgs {
+  void *k, *v;
+  uint8_t *k_exp, *v_exp;
+  const int32_t *table, *a_idx, *a_off, *pos;  // pos NULL: a_idx on every axis
+  const void *q, *k_new, *v_new;
+  void *q_out;
+  int64_t row_stride, q_out_stride;
+  int32_t n_pages, n_heads, q_heads, page_log2, max_pages, n_seqs, a_total, rows_each, n_pairs;
+  int32_t slots;              // paged_append_plan: lane groups per row
+  FastDiv d_slots, d_rows;    // set by the launch
+};
+// Heads of one row that a lane group of the append kernel takes, one after another.
+int paged_append_heads(int32_t head_dim, int64_t rows, int32_t heads);
+hipError_t launch_paged_append(DType dt, int32_t format, int32_t head_dim, bool halves, const PagedTurns &turns,
+                               PagedAppendArgs a, hipStream_t s);
 constexpr int PAGED_READ_TOKENS = 128;  // tokens per workgroup of the read kernel
 struct PagedReadArgs {
   const void *k, *v;
@@ -315,6 +335,11 @@ struct PagedSelectArgs {
 int64_t paged_select_grid(PagedSelectArgs &a);
 hipError_t launch_paged_select(DType dt, int32_t head_dim, const PagedSelectArgs &a, int64_t grid,
                                hipStream_t s);
+// Which keys a row of the attention sees: every token; those of listed pages; those
+// of a window up to its own token, and the sequence's first ones; a context and the
+// drafted tokens that its mask names.
+enum PagedLook : int32_t { PAGED_ALL = 0, PAGED_LISTED = 1, PAGED_WINDOW = 2, PAGED_TREE = 3 };
+constexpr int PAGED_MAX_MASK_WORDS = 64;  // of 32 drafted tokens each
 constexpr int PAGED_JOIN_THREADS = 256;  // of the join's workgroup, one per (row, query head)
 constexpr int PAGED_MAX_SHARED = 256;  // sequences of a call whose ranges are shared out on the device
 struct PagedAttnArgs {
@@ -324,10 +349,14 @@ struct PagedAttnArgs {
   const void *q;
   void *o;
   const int32_t *pages;  // [q_total][n_heads][n_select], or NULL: every token
+  const int32_t *q_idx;  // [q_total]: the rows' tokens (windows)
+  const int32_t *ctx;    // [n_seqs]: tokens before the drafted ones (trees)
+  const uint32_t *mask;  // [q_total][mask_words]: drafted tokens that a row sees
   float *part_o, *part_ml;
   int64_t q_stride;
   int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, q_total, q_max, rows_each, group, len_max,
       n_select;
+  int32_t look, window, sinks, mask_words;  // PagedLook
   float sl2;  // log2(e) / sqrt(head_dim)
   // the plan (paged_plan): 16-row tiles and wavefronts per workgroup, row
   // blocks per sequence, key ranges, 32-key tiles per range, rows of a block
@@ -347,5 +376,9 @@ hipError_t launch_paged_join(DType dt, int32_t head_dim, const PagedAttnArgs &a,
 hipError_t launch_paged_attention_bf16(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
 hipError_t launch_paged_attention_e4m3(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
 hipError_t launch_paged_attention_int8(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
+// windows and trees
+hipError_t launch_paged_masked_bf16(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
+hipError_t launch_paged_masked_e4m3(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
+hipError_t launch_paged_masked_int8(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
 
 }  // namespace marche

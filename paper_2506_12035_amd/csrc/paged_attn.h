@@ -294,18 +294,63 @@ __device__ __forceinline__ bf16x8 finite(bf16x8 x) {
   return __builtin_bit_cast(bf16x8, w);
 }
 
+// Tokens that a row at token t sees of `len`: those of [lo, hi), and of [0, hi) those
+// below the number of sinks (hi = 0: none).
+__device__ __forceinline__ void window_of(const PagedAttnArgs &a, int len, int t, int &lo, int &hi) {
+  hi = t < 0 ? 0 : min(t, len - 1) + 1;
+  lo = t < 0 ? 0 : max(t - (a.window - 1), 0);
+}
+// Which of the 16 keys from `key` on these are, as bits.
+__device__ __forceinline__ uint32_t below16(int n) { return n <= 0 ? 0u : n >= 16 ? 0xFFFFu : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t window_bits(int lo, int hi, int sinks, int key) {
+  return below16(hi - key) & (~below16(lo - key) | below16(sinks - key));
+}
+// Of a block's rows: the smallest and largest lo and hi (rows that see nothing
+// count in hi_min and lo_max, so that no tile is taken to be whole for them).
+struct Span {
+  int lo_min, lo_max, hi_min, hi_max;
+};
+__device__ __forceinline__ Span span_of(const PagedAttnArgs &a, int len, int row, int rows, int lane) {
+  int lo = 0, hi = 0;
+  window_of(a, len, a.q_idx[row + min(lane, rows - 1)], lo, hi);
+  Span s{hi > 0 ? lo : INT32_MAX, lo, hi, hi};
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    s.lo_min = min(s.lo_min, __shfl_xor(s.lo_min, o, 64));
+    s.lo_max = max(s.lo_max, __shfl_xor(s.lo_max, o, 64));
+    s.hi_min = min(s.hi_min, __shfl_xor(s.hi_min, o, 64));
+    s.hi_max = max(s.hi_max, __shfl_xor(s.hi_max, o, 64));
+  }
+  s.lo_min = __builtin_amdgcn_readfirstlane(s.lo_min);
+  s.lo_max = __builtin_amdgcn_readfirstlane(s.lo_max);
+  s.hi_min = __builtin_amdgcn_readfirstlane(s.hi_min);
+  s.hi_max = __builtin_amdgcn_readfirstlane(s.hi_max);
+  return s;
+}
+// Bits `at` .. at + 15 of a row's mask; those before bit 0 (the context) are set, those
+// behind the last word are not.
+__device__ __forceinline__ uint32_t tree_bits(const uint32_t *mask, int words, int at) {
+  const int w = at >> 5;  // (-1 for the context's last tokens)
+  if (w < -1) return 0xFFFFu;
+  const uint32_t lo = w < 0 ? 0xFFFFFFFFu : w < words ? mask[w] : 0u;
+  const uint32_t hi = w + 1 < words ? mask[w + 1] : 0u;
+  return (uint32_t)((((uint64_t)hi << 32) | lo) >> (at & 31)) & 0xFFFFu;
+}
+
 // Whether K goes through LDS (the text above).
 template <int FMT, int DH, int RT, typename RowT>
 constexpr bool paged_stage = DH * (FMT == BF ? 2 : 1) > 64 && (RT == 2 || sizeof(RowT) == 4);
 
-// Attention of a block's packed rows [p0, p1) over the pages that each of them
+// Attention of a block's packed rows [p0, p1) over the tokens that each of them
 // looks at, a wavefront per row, 16 keys at a time (lanes 0 .. 15 a key each):
-// the plain loop, for blocks that list values that are not finite.  Slow: one of
-// them among 36 .. 100 rows over 8 of 34 bf16 pages makes the call take 4.0 ms for 72 us.
-template <int FMT, int DH, typename RowT>
-__device__ __forceinline__ void one_by_one(const PagedAttnArgs &a, const int32_t *tab, const uint32_t *s_bits,
-                                           const uint16_t *s_list, int words, int p0, int p1, int i0, int row0, int h,
-                                           int split_i, int len, int end, int wave, int waves, int lane) {
+// the plain loop, for blocks in which a row's masked keys have values that are not
+// finite.  first(pos): the key at the block's position pos (a multiple of 16); look(i, key):
+// whether row i sees it.  Slow: one such value among 36 .. 100 rows over 8 of 34 bf16
+// pages makes the call take 4.0 ms for 72 us.
+template <int FMT, int DH, typename RowT, typename First, typename Look>
+__device__ __forceinline__ void one_by_one(const PagedAttnArgs &a, const int32_t *tab, First first, Look look, int p0,
+                                           int p1, int row0, int h, int split_i, int len, int pos0, int end, int wave,
+                                           int waves, int lane) {
   const int page = 1 << a.page_log2;
   auto at = [&](const void *x, const uint8_t *ex, size_t slot, int d) {
     if constexpr (FMT == BF) return (float)static_cast<const bf16 *>(x)[slot * DH + d];
@@ -319,29 +364,33 @@ __device__ __forceinline__ void one_by_one(const PagedAttnArgs &a, const int32_t
     float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};
     bool seen = false;
 #pragma unroll 1
-    for (int pos = 32 * split_i * a.chunk; pos < end; pos += 16) {
-      const int lp = s_list[pos >> a.page_log2];
-      if (!((s_bits[(i - i0) * words + (lp >> 5)] >> (lp & 31)) & 1u)) continue;
-      const int phys = tab[lp];
-      const int n = min(len - (lp << a.page_log2) - (pos & (page - 1)), 16);
-      if ((unsigned)phys >= (unsigned)a.n_pages || n <= 0) continue;
-      const size_t slot = (((size_t)phys * a.n_heads + h) << a.page_log2) + (pos & (page - 1));
+    for (int pos = pos0; pos < end; pos += 16) {
+      const int key = first(pos);
+      const int n = min(len - key, 16);
+      if (n <= 0) continue;
+      const unsigned long long sees = __ballot(lane < n && look(i, key + lane));
+      if (!sees) continue;
+      const int phys = tab[key >> a.page_log2];
+      if ((unsigned)phys >= (unsigned)a.n_pages) continue;
+      const size_t slot = (((size_t)phys * a.n_heads + h) << a.page_log2) + (key & (page - 1));
+      const bool mine = (sees >> lane) & 1u;
       seen = true;
       float s = 0.f;
-      if (lane < n) {
+      if (mine) {
 #pragma unroll 1
         for (int d = 0; d < DH; ++d) s = fmaf(to_f32(q[d]), at(a.k, a.k_exp, slot + lane, d), s);
         s *= a.sl2;
       }
-      const float m_new = fmaxf(m, wave_max(lane < n ? s : -INFINITY));
+      const float m_new = fmaxf(m, wave_max(mine ? s : -INFINITY));
       const float al = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-      const float p = lane < n ? __builtin_amdgcn_exp2f(s - (m_new == -INFINITY ? 0.f : m_new)) : 0.f;
+      const float p = mine ? __builtin_amdgcn_exp2f(s - (m_new == -INFINITY ? 0.f : m_new)) : 0.f;
       m = m_new;
       l = l * al + wave_sum(p);
       acc[0] *= al;
       acc[1] *= al;
 #pragma unroll 1
       for (int r = 0; r < n; ++r) {
+        if (!((sees >> r) & 1u)) continue;
         const float w = __shfl(p, r, 64);
         acc[0] = fmaf(w, at(a.v, a.v_exp, slot + r, lane), acc[0]);
         if (lane + 64 < DH) acc[1] = fmaf(w, at(a.v, a.v_exp, slot + r, lane + 64), acc[1]);
@@ -364,9 +413,11 @@ __device__ __forceinline__ void one_by_one(const PagedAttnArgs &a, const int32_t
   }
 }
 
-template <int FMT, int DH, int RT, typename RowT, bool SEL>
+// MODE: which keys a row sees (PagedLook).
+template <int FMT, int DH, int RT, typename RowT, int MODE>
 __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAttnArgs a,
                                                                          const int32_t *__restrict__ table) {
+  constexpr bool SEL = MODE == PAGED_LISTED, WIN = MODE == PAGED_WINDOW, TREE = MODE == PAGED_TREE;
   constexpr bool STAGE = paged_stage<FMT, DH, RT, RowT>;
   using Raw = KvRaw<FMT, DH, STAGE>;
   constexpr int TERMS = sizeof(RowT) == 4 ? 3 : 1;
@@ -389,7 +440,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   int split_i = at0 - at1 * a.splits, chunk = a.chunk;
   int b = a.d_heads.div(pair);
   const int h = pair - b * a.n_heads;
-  if (!SEL && a.budget > 0) {
+  if (!SEL && !WIN && a.budget > 0) {
     if (b >= a.budget) return;
     const Shares sh(a, lane);
     chunk = sh.chunk;
@@ -404,8 +455,8 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   // sequence is long enough).
   const int page = 1 << a.page_log2;
   const int32_t *tab = table + (size_t)b * a.max_pages;
-  const int first = split_i * chunk + wave;
-  const int ahead = SEL ? 0 : tab[min((32 * first) >> a.page_log2, a.max_pages - 1)];
+  int first = split_i * chunk + wave;
+  const int ahead = SEL || WIN ? 0 : tab[min((32 * first) >> a.page_log2, a.max_pages - 1)];
   const int len = min(paged_len(a.lens[b], a.max_pages, a.page_log2), a.len_max);
   int row0 = b * a.rows_each, row1 = row0 + a.rows_each;  // the sequence's rows
   if (a.q_off) {
@@ -427,7 +478,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   float *s_l = s_m + (waves > 1 ? waves * RT * 16 : 0);       // [waves][RT*16]
   int *s_row = reinterpret_cast<int *>(s_l + (waves > 1 ? waves * RT * 16 : 0));  // [RT*16]
   uint32_t *s_bits = reinterpret_cast<uint32_t *>(s_row + (waves > 1 ? RT * 16 : 0));
-  const int words = (a.max_pages + 31) >> 5;
+  const int words = TREE ? a.mask_words : (a.max_pages + 31) >> 5;
   auto row_of = [&](int p) { return (int)a.d_group.div(p); };  // a packed row's row
   const int i0 = row_of(p0), i1 = row_of(min(p0 + 16 * RT, packed) - 1);  // the block's rows
   uint32_t *s_any = s_bits + (SEL ? a.bit_rows * words : 0);
@@ -469,12 +520,35 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
     __syncthreads();
   }
   n_list = __builtin_amdgcn_readfirstlane(n_list);
-  const int n_keys = SEL ? n_list << a.page_log2 : len;  // positions the block walks through
+  int n_keys = SEL ? n_list << a.page_log2 : len;  // positions the block walks through
+  // drafted tokens: the rows' bits for those behind the context
+  const int ctx = TREE ? max(a.ctx[b], 0) : 0;
+  if constexpr (TREE) {
+    const int n = (i1 - i0 + 1) * words;
+    for (int x = tid; x < n; x += blockDim.x) s_bits[x] = a.mask[(size_t)(row0 + i0) * words + x];
+    __syncthreads();
+  }
+  // windows: what any row of the block sees is the sinks' tiles and, from tile `jump`
+  // positions further on, those from the first row's window to the last row's token
+  Span sp;
+  int sink_tiles = 0, jump = 0;
+  if constexpr (WIN) {
+    sp = span_of(a, len, row0 + i0, i1 - i0 + 1, lane);
+    const int end = (sp.hi_max + 31) >> 5;
+    sink_tiles = (min(a.sinks, sp.hi_max) + 31) >> 5;
+    const int from = max(sp.lo_min >> 5, sink_tiles);
+    jump = from - sink_tiles;
+    const int tiles = sink_tiles + max(end - from, 0);
+    n_keys = 32 * tiles;
+    chunk = ((int)a.d_splits.div(tiles + a.splits - 1) + waves - 1) / waves * waves;
+    first = split_i * chunk + wave;
+  }
   const int t1 = min((split_i + 1) * chunk, (n_keys + 31) >> 5);  // the range's last tile
 
   // queries: lane (c, g) holds row c of each tile (columns behind the last row
   // repeat the block's first: computed and never stored)
   bf16x8 qf[RT][TERMS][NC];
+  int w_lo[RT], w_hi[RT];  // windows: the row's first token and the one behind its last
   int loc[RT];  // the row within the block
   int out[RT];  // and its (row, query head) in the output, or -1
 #pragma unroll
@@ -483,6 +557,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
     const bool on = pr < packed;
     const int i = on ? row_of(pr) : i0, hg = on ? pr - i * a.group : 0;
     loc[rt] = i - i0;
+    if constexpr (WIN) window_of(a, len, a.q_idx[row0 + i], w_lo[rt], w_hi[rt]);
     out[rt] = on ? (row0 + i) * (a.n_heads * a.group) + h * a.group + hg : -1;
     const RowT *q = static_cast<const RowT *>(a.q) + (size_t)(row0 + i) * a.q_stride +
                     (size_t)(h * a.group + hg) * DH;
@@ -510,26 +585,27 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   // the 16 tokens exist, and (selected pages) the logical pages.  All uniform.
   struct Tile {
     size_t slot[2];
-    int n[2], lp[2];
+    int n[2], lp[2], key[2];
   };
   auto place = [&](int t, bool start) {
     Tile x;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int pos = 32 * t + 16 * u;
+      const int pos = 32 * (WIN && t >= sink_tiles ? t + jump : t) + 16 * u;
+      x.key[u] = pos;
       if (u == 1 && a.page_log2 > 4) {  // the same page
         x.lp[1] = x.lp[0];
         x.slot[1] = x.slot[0] + 16;
         x.n[1] = x.n[0] < 16 ? 0 : min(max(len - (SEL ? (x.lp[0] << a.page_log2) + (pos & (page - 1)) : pos), 0), 16);
         break;
       }
-      bool ok = pos < n_keys;
+      bool ok = pos < (WIN ? len : n_keys);
       int lp = ok ? pos >> a.page_log2 : 0, key = pos;
       if constexpr (SEL) {
         lp = __builtin_amdgcn_readfirstlane((int)s_list[lp]);
         key = (lp << a.page_log2) + (pos & (page - 1));
       }
-      const int phys = !ok ? 0 : !SEL && start && u == 0 ? ahead : tab[lp];
+      const int phys = !ok ? 0 : !SEL && !WIN && start && u == 0 ? ahead : tab[lp];
       ok = ok && (unsigned)phys < (unsigned)a.n_pages;
       x.n[u] = ok ? min(max(len - key, 0), 16) : 0;
       x.slot[u] = (((size_t)(ok ? phys : 0) * a.n_heads + h) << a.page_log2) + (pos & (page - 1));
@@ -651,6 +727,19 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           bool look = true;
+          uint32_t bits16 = 0xFFFFu;  // which of the half's keys the row sees
+          if constexpr (WIN) {
+            if (!(x.key[u] + 16 <= sp.hi_min && (x.key[u] >= sp.lo_max || x.key[u] + 16 <= a.sinks))) {
+              bits16 = window_bits(w_lo[rt], w_hi[rt], a.sinks, x.key[u]);
+              look = (bits16 & ((1u << x.n[u]) - 1u)) != 0;
+            }
+          }
+          if constexpr (TREE) {
+            if (x.key[u] + 16 > ctx) {
+              bits16 = tree_bits(s_bits + loc[rt] * words, words, x.key[u] - ctx);
+              look = (bits16 & ((1u << x.n[u]) - 1u)) != 0;
+            }
+          }
           if constexpr (SEL) {
             const uint32_t w = AHEAD ? bits.w[rt][u] : s_bits[loc[rt] * words + (x.lp[u] >> 5)];
             look = (w >> (x.lp[u] & 31)) & 1u;
@@ -659,6 +748,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             if (SEL && !look) s[rt][u][r] = -INFINITY;
+            if ((WIN || TREE) && !((bits16 >> (4 * g + r)) & 1u)) s[rt][u][r] = -INFINITY;
             mx[rt] = fmaxf(mx[rt], s[rt][u][r]);
           }
         }
@@ -828,27 +918,46 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   // zero, or of the other sign than the whole, is NaN where none is due.
   if constexpr (FMT == BF && TERMS > 1)
     if (spoiled(false)) pass(std::true_type());
-  // A weight of zero times an infinite or NaN value of a page that only another row
-  // looks at is NaN: such a block is computed again, row by row over each row's own
-  // pages.
-  if constexpr (SEL) {
-    if (i1 > i0 && spoiled(true)) {
-      one_by_one<FMT, DH, RowT>(a, tab, s_bits, s_list, words, p0, min(p0 + 16 * RT, packed), i0, row0, h, split_i,
-                                len, min(32 * t1, n_keys), wave, waves, lane);
+  // A weight of zero times an infinite or NaN value that only another row looks at (or
+  // none, in a tile that some row sees a part of) is NaN: such a block is computed
+  // again, row by row over each row's own keys.
+  if constexpr (MODE != PAGED_ALL) {
+    if ((!SEL || i1 > i0) && spoiled(true)) {
+      one_by_one<FMT, DH, RowT>(
+          a, tab,
+          [&](int pos) {
+            if constexpr (SEL) return ((int)s_list[pos >> a.page_log2] << a.page_log2) + (pos & (page - 1));
+            else return WIN && pos >= 32 * sink_tiles ? pos + 32 * jump : pos;
+          },
+          [&](int i, int key) {
+            if constexpr (SEL) {
+              const int lp = key >> a.page_log2;
+              return ((s_bits[(i - i0) * words + (lp >> 5)] >> (lp & 31)) & 1u) != 0;
+            } else if constexpr (WIN) {
+              int lo, hi;
+              window_of(a, len, a.q_idx[row0 + i], lo, hi);
+              return key < hi && (key >= lo || key < a.sinks);
+            } else {
+              return (tree_bits(s_bits + (i - i0) * words, words, key - ctx) & 1u) != 0;
+            }
+          },
+          p0, min(p0 + 16 * RT, packed), row0, h, split_i, len, 32 * split_i * chunk, min(32 * t1, n_keys), wave,
+          waves, lane);
       return;
     }
   }
   join();
 }
 
-template <int FMT, int DH, int RT, typename RowT, bool SEL>
+template <int FMT, int DH, int RT, typename RowT, int MODE>
 hipError_t launch_paged_attn(const PagedAttnArgs &a, hipStream_t s) {
   constexpr int OS = DH + 4;
   const int words = (a.max_pages + 31) / 32;
   size_t lds = paged_stage<FMT, DH, RT, RowT> ? 32 * DH * (FMT == BF ? 2 : 1) : 0;
   if (a.waves > 1) lds = ((size_t)a.waves * (RT * 16 * OS + 2 * RT * 16) + RT * 16) * 4;
-  if (SEL) lds += ((size_t)(a.bit_rows + 1) * words) * 4 + (size_t)words * 64;
-  auto kernel = paged_attn_kernel<FMT, DH, RT, RowT, SEL>;
+  if (MODE == PAGED_LISTED) lds += ((size_t)(a.bit_rows + 1) * words) * 4 + (size_t)words * 64;
+  if (MODE == PAGED_TREE) lds += (size_t)a.bit_rows * a.mask_words * 4;
+  auto kernel = paged_attn_kernel<FMT, DH, RT, RowT, MODE>;
   if (lds > 65536) {
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -859,27 +968,34 @@ hipError_t launch_paged_attn(const PagedAttnArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int FMT, int DH, typename RowT, bool SEL>
+template <int FMT, int DH, typename RowT, int MODE>
 hipError_t launch_paged_rt(const PagedAttnArgs &a, hipStream_t s) {
-  if (a.row_tiles == 1) return launch_paged_attn<FMT, DH, 1, RowT, SEL>(a, s);
+  if (a.row_tiles == 1) return launch_paged_attn<FMT, DH, 1, RowT, MODE>(a, s);
   if constexpr (sizeof(RowT) == 2)
-    if (a.row_tiles == 2) return launch_paged_attn<FMT, DH, 2, RowT, SEL>(a, s);
+    if (a.row_tiles == 2) return launch_paged_attn<FMT, DH, 2, RowT, MODE>(a, s);
   return hipErrorInvalidValue;
 }
 
-template <int FMT, int DH>
-hipError_t launch_paged_dh(DType dt, const PagedAttnArgs &a, hipStream_t s) {
-  if (dt == DType::BF16)
-    return a.pages ? launch_paged_rt<FMT, DH, bf16, true>(a, s) : launch_paged_rt<FMT, DH, bf16, false>(a, s);
-  return a.pages ? launch_paged_rt<FMT, DH, float, true>(a, s) : launch_paged_rt<FMT, DH, float, false>(a, s);
+// MASKED: windows and trees; otherwise every token, or listed pages.
+template <int FMT, int DH, bool MASKED, typename RowT>
+hipError_t launch_paged_mode(const PagedAttnArgs &a, hipStream_t s) {
+  if constexpr (MASKED)
+    return a.look == PAGED_TREE ? launch_paged_rt<FMT, DH, RowT, PAGED_TREE>(a, s)
+                                : launch_paged_rt<FMT, DH, RowT, PAGED_WINDOW>(a, s);
+  else
+    return a.pages ? launch_paged_rt<FMT, DH, RowT, PAGED_LISTED>(a, s) : launch_paged_rt<FMT, DH, RowT, PAGED_ALL>(a, s);
 }
 
-template <int FMT>
+template <int FMT, bool MASKED>
 hipError_t launch_paged_fmt(DType dt, int head_dim, const PagedAttnArgs &a, hipStream_t s) {
+  auto go = [&](auto dh) {
+    return dt == DType::BF16 ? launch_paged_mode<FMT, dh.value, MASKED, bf16>(a, s)
+                             : launch_paged_mode<FMT, dh.value, MASKED, float>(a, s);
+  };
   switch (head_dim) {
-    case 64: return launch_paged_dh<FMT, 64>(dt, a, s);
-    case 80: return launch_paged_dh<FMT, 80>(dt, a, s);
-    case 128: return launch_paged_dh<FMT, 128>(dt, a, s);
+    case 64: return go(std::integral_constant<int, 64>());
+    case 80: return go(std::integral_constant<int, 80>());
+    case 128: return go(std::integral_constant<int, 128>());
   }
   return hipErrorInvalidValue;
 }

@@ -1,6 +1,8 @@
 // Device-side helpers of the paged cache's kernels.
 #pragma once
 
+#include <type_traits>
+
 #include "device_common.h"
 
 namespace marche {
@@ -60,6 +62,116 @@ __device__ __forceinline__ void unpack4(uint32_t w, float scale, float *o) {
     o[2] = (float)(int8_t)(w >> 16) * scale;
     o[3] = (float)(int8_t)(w >> 24) * scale;
   }
+}
+
+// ------------------------------------------------------------------ rows in 8 bits
+
+// Largest over a group of 8 or 16 neighbouring lanes.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true));
+}
+template <int GROUP>
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  v = dpp_max<0xB1>(v);                           // quad_perm [1,0,3,2]
+  v = dpp_max<0x4E>(v);                           // quad_perm [2,3,0,1]
+  v = dpp_max<0x141>(v);                          // row_half_mirror: 8 lanes
+  if constexpr (GROUP == 16) v = dpp_max<0x140>(v);  // row_mirror
+  return v;
+}
+
+// Largest over the wavefront, uniform (no LDS crossbar).
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = group_max<16>(v);
+  auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(p[0], p[1]);
+  auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __builtin_amdgcn_readfirstlane(max(q[0], q[1]));
+}
+
+// Four int8 numbers from floats whose low bytes hold them.
+__device__ __forceinline__ int pack_low(float a, float b, float c, float d) {
+  const uint32_t x = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x0C0C0400u);
+  const uint32_t y = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x04000C0Cu);
+  return (int)(x | y);
+}
+// x 2^-e, exact, rounded to a whole number (ties to even) in the low byte: the
+// sum with 1.5 2^23 has no bits below 1, and its low bits are two's complement.
+__device__ __forceinline__ float round_low(float x, float inv) { return fmaf(x, inv, 12582912.f); }
+
+// Largest magnitude of eight values as float bits, which order like the
+// magnitudes and place NaN above infinity (bf16: in pairs of 16-bit halves).
+template <typename InT, int NV>
+__device__ __forceinline__ uint32_t largest(const u32x4 (&x)[NV]) {
+  if constexpr (sizeof(InT) == 2) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x[0][i] & 0x7FFF7FFFu));
+    return (uint32_t)max(m[0], m[1]) << 16;
+  } else {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, x[i / 4][i % 4] & 0x7FFFFFFFu);
+    return m;
+  }
+}
+
+// Eight values of a row with exponent code `code` in the format.
+template <int FMT, typename InT, int NV>
+__device__ __forceinline__ u32x2 pack8(u32x4 (&x)[NV], int code) {
+  u32x2 o;
+  // No magnitude above TOP_BITS in the largest rows (in e4m3 no other row reaches
+  // that), by a limit for either sign: as signed numbers the negative ones are
+  // below the positive limit, as unsigned ones the others below the negative.
+  const uint32_t top = FMT == E4 || code == TOP_CODE<FMT> ? TOP_BITS<FMT> : 0x7F7FFFFFu;
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(InT) == 4) {
+        x[v][i] = min((uint32_t)min((int)x[v][i], (int)top), top | 0x80000000u);
+      } else {
+        typedef short s16x2 __attribute__((ext_vector_type(2)));
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        const short high = (short)(top >> 16);
+        const unsigned short low = (unsigned short)(high | 0x8000);
+        const s16x2 w = __builtin_elementwise_min(__builtin_bit_cast(s16x2, +x[v][i]), s16x2{high, high});
+        x[v][i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, w), u16x2{low, low}));
+      }
+    }
+  if (code == 255) {  // the whole row reads back as NaN
+    o.x = o.y = FMT == E4 ? 0x7F7F7F7Fu : 0u;
+    return o;
+  }
+  const float inv = exp_inv(code);
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    if constexpr (FMT == E4 && sizeof(InT) == 2) {
+      // the conversion divides by the scale's power of two
+      typedef short s16x2 __attribute__((ext_vector_type(2)));
+      s16x2 q = {0, 0};
+      q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(bf16x2, +x[0][2 * w]), exp_scale(code), false);
+      q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(bf16x2, +x[0][2 * w + 1]), exp_scale(code), true);
+      o[w] = __builtin_bit_cast(uint32_t, q);
+      continue;
+    }
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(InT) == 4) f[i] = __uint_as_float(x[w % NV][i]);
+      else f[i] = __uint_as_float(i % 2 ? x[0][2 * w + i / 2] & 0xFFFF0000u : x[0][2 * w + i / 2] << 16);
+    }
+    if constexpr (FMT == E4) {
+      int q = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] * inv, f[1] * inv, 0, false);
+      q = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] * inv, f[3] * inv, q, true);
+      o[w] = (uint32_t)q;
+    } else {
+      o[w] = (uint32_t)pack_low(round_low(f[0], inv), round_low(f[1], inv), round_low(f[2], inv), round_low(f[3], inv));
+    }
+  }
+  return o;
 }
 
 // ------------------------------------------------------------------ sequences
@@ -175,5 +287,27 @@ struct Shares {
     return -1;
   }
 };
+
+// ------------------------------------------------------------------ launches
+
+// f(std::integral_constant<int, FMT>, std::integral_constant<int, DH>)
+template <typename F>
+static hipError_t by_shape(int32_t format, int32_t head_dim, F f) {
+  auto dh = [&](auto fmt) {
+    switch (head_dim) {
+      case 64: f(fmt, std::integral_constant<int, 64>()); break;
+      case 80: f(fmt, std::integral_constant<int, 80>()); break;
+      case 128: f(fmt, std::integral_constant<int, 128>()); break;
+      default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+  };
+  switch (format) {
+    case BF: return dh(std::integral_constant<int, BF>());
+    case E4: return dh(std::integral_constant<int, E4>());
+    case I8: return dh(std::integral_constant<int, I8>());
+  }
+  return hipErrorInvalidValue;
+}
 
 }  // namespace marche
