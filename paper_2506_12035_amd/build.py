@@ -22,7 +22,8 @@ LIB = os.path.join(PKG, "libmarche.so")
 SOURCES = ("marche_api.cpp", "marche_noalloc.hip", "k_elementwise.hip", "k_gemm.hip",
            "k_attn.hip", "k_select.hip", "k_mar.hip", "k_paged.hip", "k_paged_attn_bf16.hip",
            "k_paged_attn_e4m3.hip", "k_paged_attn_int8.hip", "k_paged_append.hip", "k_paged_masked_bf16.hip",
-           "k_paged_masked_e4m3.hip", "k_paged_masked_int8.hip")
+           "k_paged_masked_e4m3.hip", "k_paged_masked_int8.hip", "k_paged_rows_bf16.hip",
+           "k_paged_rows_e4m3.hip", "k_paged_rows_int8.hip")
 ARCH = "gfx950"
 
 # -packed-fp32-ops: keep the compiler from forming packed fp32 VALU ops.
@@ -46,7 +47,8 @@ def hipcc() -> str:
 EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"]
          for src in ("k_attn.hip", "k_paged_attn_bf16.hip", "k_paged_attn_e4m3.hip",
                      "k_paged_attn_int8.hip", "k_paged_masked_bf16.hip", "k_paged_masked_e4m3.hip",
-                     "k_paged_masked_int8.hip")}
+                     "k_paged_masked_int8.hip", "k_paged_rows_bf16.hip", "k_paged_rows_e4m3.hip",
+                     "k_paged_rows_int8.hip")}
 
 
 def _compile(src: str) -> str:

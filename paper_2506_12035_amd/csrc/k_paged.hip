@@ -621,6 +621,90 @@ __global__ __launch_bounds__(PAGED_JOIN_THREADS) void paged_join_kernel(PagedAtt
   static_cast<RowT *>(a.o)[row * DH + d] = (RowT)(seen ? total / l : 0.f);
 }
 
+// The same for many rows, whose sequences of one range have been written already: a lane
+// group per (row, head), four channels a lane, ROWS_JOIN of them in turn; the
+// group's lanes hold the parts' maxima and sums.
+constexpr int ROWS_JOIN = 4;
+template <int DH, typename RowT>
+__global__ __launch_bounds__(256) void paged_rows_join_kernel(PagedAttnArgs a) {
+  constexpr int LANES = DH == 64 ? 16 : 32, PER = 256 / LANES, K = 64 / LANES;
+  const int tid = threadIdx.x, lane = tid & 63, c = tid % LANES;
+  const int heads = a.n_heads * a.group;
+  const int64_t n = (int64_t)a.q_total * heads;
+  int chunk = 0;
+  if (a.budget > 0) chunk = Shares(a, lane).chunk;
+  const int first = a.q_off ? a.q_off[0] : 0, last = a.q_off ? a.q_off[a.n_seqs] : a.q_total;
+#pragma unroll 1
+  for (int i = 0; i < ROWS_JOIN; ++i) {
+    const int64_t x0 = ((int64_t)blockIdx.x * ROWS_JOIN + i) * PER + (tid & ~63) / LANES;  // of the wavefront
+    if (x0 >= n) return;
+    const int64_t x = min(x0 + lane / LANES, n - 1);
+    const int r = (int)(x / heads);
+    int b = a.q_off ? wave_find_seq(a.q_off, a.n_seqs, __builtin_amdgcn_readfirstlane((int)(x0 / heads)), lane) : r / a.rows_each;
+    if (a.q_off)
+      while (b < a.n_seqs && a.q_off[b + 1] <= r) ++b;
+    int splits = a.splits;
+    if (a.budget > 0) {
+      const int len = min(paged_len(a.lens[min(b, a.n_seqs - 1)], a.max_pages, a.page_log2), a.len_max);
+      splits = (((len + 31) >> 5) + chunk - 1) / chunk;
+    }
+    if (r < first || r >= last || splits == 1 || x0 + lane / LANES >= n) continue;  // (whole groups)
+    float ms[K], ls[K], m = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int s = LANES * k + c;
+      ms[k] = -INFINITY;
+      ls[k] = -1.f;
+      if (s < splits) {
+        ms[k] = a.part_ml[2 * (s * n + x)];
+        ls[k] = a.part_ml[2 * (s * n + x) + 1];
+        if (ls[k] == -1.f) ms[k] = -INFINITY;
+      }
+      m = fmaxf(m, ms[k]);
+    }
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    float l = 0.f;
+    bool seen = false;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const bool has = ls[k] != -1.f;  // a part that saw keys
+      const float w = !has ? 0.f : ms[k] == -INFINITY ? (m == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(ms[k] - m);
+      l += has ? ls[k] * w : 0.f;
+      seen |= has;
+      ms[k] = has ? w : -1.f;
+    }
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) {
+      l += __shfl_xor(l, o, 64);
+      seen |= __shfl_xor((int)seen, o, 64) != 0;
+    }
+    const int d = 4 * c < DH ? 4 * c : 0;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      for (int s0 = LANES * k; s0 < min(splits, LANES * (k + 1)); s0 += 4) {
+        f32x4 y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y[u] = *reinterpret_cast<const f32x4 *>(a.part_o + (min(s0 + u, splits - 1) * n + x) * DH + d);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float w = __shfl(ms[k], (lane & ~(LANES - 1)) + (s0 + u) % LANES, 64);
+          if (s0 + u < splits && w != -1.f) {  // (a part without keys adds nothing, whatever it holds)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] = fmaf(y[u][e], w, sum[e]);
+          }
+        }
+      }
+    }
+    if (4 * c >= DH) continue;
+    const float inv = seen ? 1.f / l : 0.f;
+    RowT *o = static_cast<RowT *>(a.o) + x * DH + d;
+    if constexpr (sizeof(RowT) == 4) *reinterpret_cast<f32x4 *>(o) = sum * inv;
+    else *reinterpret_cast<bf16x4 *>(o) = bf16x4{(bf16)(sum[0] * inv), (bf16)(sum[1] * inv), (bf16)(sum[2] * inv), (bf16)(sum[3] * inv)};
+  }
+}
+
 // ------------------------------------------------------------------ launches
 
 hipError_t launch_paged_write(DType dt, int32_t format, int32_t head_dim, PagedWriteArgs a, hipStream_t s) {
@@ -707,13 +791,52 @@ hipError_t launch_paged_select(DType dt, int32_t head_dim, const PagedSelectArgs
   });
 }
 
+static int64_t paged_pairs(const PagedAttnArgs &a) { return (int64_t)(a.budget > 0 ? a.budget : a.n_seqs) * a.n_heads; }
+
 int64_t paged_grid(const PagedAttnArgs &a) {
-  const int64_t pairs = (int64_t)(a.budget > 0 ? a.budget : a.n_seqs) * a.n_heads;  // dealt to 8 XCDs
+  const int64_t pairs = paged_pairs(a);  // dealt to 8 XCDs
+  if (a.look == PAGED_WINDOW || a.row_waves > 0) return pairs * a.row_blocks * (a.budget > 0 ? 1 : a.splits);
   return (pairs + 7) / 8 * 8 * a.row_blocks * (a.budget > 0 ? 1 : a.splits);
+}
+
+// The plan of windows and trees with many rows (paged_rows.h).
+static void rows_plan(PagedAttnArgs &a) {
+  const int rows = a.q_max * a.group;
+  a.row_waves = PAGED_ROW_WAVES;
+  a.waves = a.row_waves;
+  a.row_tiles = 2 * a.row_waves;
+  a.row_blocks = (rows - 1) / (32 * a.row_waves) + 1;
+  const int64_t units = (int64_t)a.n_seqs * a.n_heads * a.row_blocks;
+  int64_t keys = a.len_max;
+  if (a.look == PAGED_WINDOW)
+    keys = std::min<int64_t>(keys, (int64_t)a.sinks + a.window + 32 * a.row_waves / a.group + 126);
+  const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32);
+  // two workgroups for each compute unit, eight 32-key tiles each at least
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({64, (512 + units - 1) / units, tiles / 8}));
+  a.chunk = (int32_t)((tiles + splits - 1) / splits);
+  a.chunk += a.chunk & 1;
+  a.splits = (int32_t)((tiles + a.chunk - 1) / a.chunk);
+  const int64_t per = (int64_t)a.n_heads * a.row_blocks;
+  if (a.look == PAGED_TREE && units < 2048 && a.n_seqs <= PAGED_MAX_SHARED && tiles * a.n_seqs < (1LL << 30) && tiles > 8) {
+    a.budget = (int32_t)(a.n_seqs + (512 + per - 1) / per);
+    a.chunk = 8;  // at least
+    a.splits = (int32_t)std::min<int64_t>({64, a.budget, (tiles + a.chunk - 1) / a.chunk});
+  }
 }
 
 void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
   const int rows = a.q_max * a.group;  // packed rows of a sequence and key head
+  a.row_waves = a.budget = 0;
+  a.d_heads = FastDiv::of(a.n_heads);
+  a.d_group = FastDiv::of(a.group);
+  if (dt == DType::BF16 && rows > PAGED_FEW_ROWS && (a.look == PAGED_WINDOW || a.look == PAGED_TREE)) {
+    rows_plan(a);
+    a.d_splits = FastDiv::of(a.budget > 0 ? 1 : a.splits);
+    a.d_blocks = FastDiv::of(a.row_blocks);
+    const int64_t pairs = a.budget > 0 ? (int64_t)a.n_heads * a.row_blocks : paged_pairs(a);
+    a.d_pairs = FastDiv::of((uint32_t)std::min<int64_t>(pairs, INT32_MAX));
+    return;
+  }
   // Two 16-row tiles a wavefront share what is loaded (36 .. 100 rows over 32
   // caches of 1088 bf16 tokens: 46 us, 69 with one); float32 rows have no registers
   // for them.  Where rows list fewer pages than there are, one tile's rows list
@@ -765,12 +888,16 @@ void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
   }
   a.d_splits = FastDiv::of(a.budget > 0 ? 1 : a.splits);
   a.d_blocks = FastDiv::of(a.row_blocks);
-  a.d_heads = FastDiv::of(a.n_heads);
-  a.d_group = FastDiv::of(a.group);
+  a.d_pairs = FastDiv::of((uint32_t)std::min<int64_t>(paged_pairs(a), INT32_MAX));
 }
 
 hipError_t launch_paged_attention(DType dt, int32_t format, int32_t head_dim, const PagedAttnArgs &a,
                                   hipStream_t s) {
+  if (a.row_waves > 0) switch (format) {
+      case BF: return launch_paged_rows_bf16(head_dim, a, s);
+      case E4: return launch_paged_rows_e4m3(head_dim, a, s);
+      case I8: return launch_paged_rows_int8(head_dim, a, s);
+    }
   if (a.look == PAGED_WINDOW || a.look == PAGED_TREE) switch (format) {
       case BF: return launch_paged_masked_bf16(dt, head_dim, a, s);
       case E4: return launch_paged_masked_e4m3(dt, head_dim, a, s);
@@ -786,6 +913,12 @@ hipError_t launch_paged_attention(DType dt, int32_t format, int32_t head_dim, co
 
 hipError_t launch_paged_join(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)a.q_total * a.n_heads * a.group);
+  if (a.row_waves > 0) {
+    const int64_t per = ROWS_JOIN * (head_dim == 64 ? 16 : 8);
+    return by_shape(BF, head_dim, [&](auto, auto dh) {
+      launch_kernel(paged_rows_join_kernel<dh.value, bf16>, (unsigned)((grid + per - 1) / per), 256, 0, s, a);
+    });
+  }
   return by_shape(BF, head_dim, [&](auto, auto dh) {
     if (dt == DType::BF16) launch_kernel(paged_join_kernel<dh.value, bf16>, grid, PAGED_JOIN_THREADS, 0, s, a);
     else launch_kernel(paged_join_kernel<dh.value, float>, grid, PAGED_JOIN_THREADS, 0, s, a);

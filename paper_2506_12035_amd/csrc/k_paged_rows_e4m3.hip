@@ -1,0 +1,10 @@
+// Attention of many rows over a paged cache of e4m3 (kernel in paged_rows.h).
+#include "paged_rows.h"
+
+namespace marche {
+
+hipError_t launch_paged_rows_e4m3(int32_t head_dim, const PagedAttnArgs &a, hipStream_t s) {
+  return launch_paged_rows<E4>(head_dim, a, s);
+}
+
+}  // namespace marche

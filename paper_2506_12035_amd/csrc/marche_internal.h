@@ -339,6 +339,8 @@ hipError_t launch_paged_select(DType dt, int32_t head_dim, const PagedSelectArgs
 // of a window up to its own token, and the sequence's first ones; a context and the
 // drafted tokens that its mask names.
 enum PagedLook : int32_t { PAGED_ALL = 0, PAGED_LISTED = 1, PAGED_WINDOW = 2, PAGED_TREE = 3 };
+constexpr int PAGED_FEW_ROWS = 64;  // packed rows up to which windows and trees go the way of the others
+constexpr int PAGED_ROW_WAVES = 4;  // wavefronts of 32 rows of a workgroup otherwise
 constexpr int PAGED_MAX_MASK_WORDS = 64;  // of 32 drafted tokens each
 constexpr int PAGED_JOIN_THREADS = 256;  // of the join's workgroup, one per (row, query head)
 constexpr int PAGED_MAX_SHARED = 256;  // sequences of a call whose ranges are shared out on the device
@@ -364,6 +366,9 @@ struct PagedAttnArgs {
   // the device (Shares), at most `splits` each and `budget` in all, of `chunk`
   // tiles at least.
   int32_t row_tiles, waves, row_blocks, splits, chunk, bit_rows, budget;
+  // row_waves > 0: blocks of 32 row_waves rows (paged_rows.h), otherwise of 16 row_tiles
+  int32_t row_waves;
+  FastDiv d_pairs;  // (sequence, head) pairs (PagedUnit)
   FastDiv d_splits, d_blocks, d_heads, d_group;
 };
 // Workgroups of the attention launch.
@@ -380,5 +385,8 @@ hipError_t launch_paged_attention_int8(DType dt, int32_t head_dim, const PagedAt
 hipError_t launch_paged_masked_bf16(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
 hipError_t launch_paged_masked_e4m3(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
 hipError_t launch_paged_masked_int8(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
+hipError_t launch_paged_rows_bf16(int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
+hipError_t launch_paged_rows_e4m3(int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
+hipError_t launch_paged_rows_int8(int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
 
 }  // namespace marche

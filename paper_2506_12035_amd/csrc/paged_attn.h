@@ -433,13 +433,23 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
   // and the blocks and ranges of a pair follow each other on its XCD, whose L2
   // they share.  (Contiguous sequences per XCD leave most XCDs idle at the end
   // where sequences differ.)
-  const int at0 = blockIdx.x >> 3;
-  const int at1 = a.d_splits.div(at0);
-  const int at2 = a.d_blocks.div(at1), rb = at1 - at2 * a.row_blocks;
-  const int pair = 8 * at2 + (blockIdx.x & 7);
-  int split_i = at0 - at1 * a.splits, chunk = a.chunk;
-  int b = a.d_heads.div(pair);
-  const int h = pair - b * a.n_heads;
+  int split_i, chunk = a.chunk, rb, b, h;
+  if constexpr (WIN) {
+    const PagedUnit u(a, blockIdx.x, a.n_seqs * a.n_heads);
+    rb = u.block;
+    split_i = u.split;
+    b = (int)a.d_heads.div(u.pair);
+    h = u.pair - b * a.n_heads;
+  } else {
+    const int at0 = blockIdx.x >> 3;
+    const int at1 = a.d_splits.div(at0);
+    const int at2 = a.d_blocks.div(at1);
+    rb = at1 - at2 * a.row_blocks;
+    const int pair = 8 * at2 + (blockIdx.x & 7);
+    split_i = at0 - at1 * a.splits;
+    b = a.d_heads.div(pair);
+    h = pair - b * a.n_heads;
+  }
   if (!SEL && !WIN && a.budget > 0) {
     if (b >= a.budget) return;
     const Shares sh(a, lane);

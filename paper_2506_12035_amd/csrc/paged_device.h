@@ -233,6 +233,20 @@ __device__ __forceinline__ int wave_find_seq(const int32_t *off, int n_seqs, int
   return lo;
 }
 
+// Workgroup `id` of windows and of blocks of many rows: the (sequence or range, head)
+// pairs go round first, so that they go round the 8 XCDs too and a pair of a multiple of 8
+// keeps to one, whose L2 its blocks share; the last row blocks, which see most and which
+// short sequences do not have, begin.
+struct PagedUnit {
+  int pair, split, block;
+  __device__ __forceinline__ PagedUnit(const PagedAttnArgs &a, int id, int pairs) {
+    const int u = (int)a.d_pairs.div(id), v = (int)a.d_splits.div(u);
+    pair = id - u * pairs;
+    split = u - v * (a.budget > 0 ? 1 : a.splits);
+    block = a.row_blocks - 1 - v;
+  }
+};
+
 // ------------------------------------------------------------------ shares of long caches
 
 // Sequences of different lengths are cut into ranges of one length, `chunk`
@@ -283,6 +297,34 @@ struct Shares {
         return 64 * k + l;
       }
       before = __shfl(end, 63, 64);
+    }
+    return -1;
+  }
+  // The same, longest ranges first: those of a whole chunk, then the sequences' last ones
+  // from half a chunk on, then the shorter ones.
+  __device__ __forceinline__ int find_long_first(int x, int lane, int &part) const {
+    int before = 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+#pragma unroll
+      for (int k = 0; k < PAGED_MAX_SHARED / 64; ++k) {
+        const int whole = (int)((uint32_t)tiles[k] / (uint32_t)chunk), rest = tiles[k] - whole * chunk;
+        const int n = pass == 0 ? whole : rest > 0 && (2 * rest >= chunk) == (pass == 1) ? 1 : 0;
+        int end = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const int y = __shfl_up(end, o, 64);
+          if (lane >= o) end += y;
+        }
+        end += before;
+        const unsigned long long past = __ballot(end > x);
+        if (past) {
+          const int l = __ffsll((long long)past) - 1;
+          part = __builtin_amdgcn_readfirstlane(pass == 0 ? x - __shfl(end - n, l, 64) : __shfl(whole, l, 64));
+          return 64 * k + l;
+        }
+        before = __shfl(end, 63, 64);
+      }
     }
     return -1;
   }
