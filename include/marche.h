@@ -587,8 +587,7 @@ marche_status_t marche_rotary_init(marche_rotary_t *rotary, int32_t head_dim, in
  * row_stride; no other output may overlap an input.  Queries are turned whatever becomes of
  * their row's token (one that is negative, at or past max_pages * page_size or of a
  * page outside the pool is not written).  q and q_out NULL, n_q_heads 0: keys and
- * values alone.  a_total * (n_q_heads + 2 n_heads) < 2^28, for head_dim 80 and 128 <= 2^28 -
- * 16.  Bounds of the pages (marche_paged_bounds) are of the turned keys. */
+ * values alone.  a_total * (n_q_heads + 2 n_heads) <= 2^28 - 64.  Bounds of the pages (marche_paged_bounds) are of the turned keys. */
 marche_status_t marche_paged_append(const marche_paged_cache_t *cache, int32_t layer,
                                     const int32_t *page_table, int32_t max_pages, int32_t n_seqs,
                                     const int32_t *a_idx, const int32_t *a_off, int32_t a_total,

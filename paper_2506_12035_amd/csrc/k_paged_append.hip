@@ -36,142 +36,157 @@ __device__ __forceinline__ void turn(int pos, double per, float &sn, float &cs) 
   cs = (q + 1) & 2 ? -b : b;
 }
 
-// A lane holds four pairs of a head: eight channels, in two pieces of four (HALVES: the
-// pairs' first and second channels, or, behind the turned ones, any eight; otherwise
-// eight neighbours).  A group of lanes takes N heads of one row, queries' before
-// keys' before values', so that the angles are formed once for them.
-template <int FMT, int DH, typename InT, bool HALVES, int N>
+// Workgroups of the queries come first, then the keys', then the values', so that a
+// wavefront does one thing.  A lane holds eight channels of a head in two pieces of four: of
+// queries and keys four pairs (HALVES: their first and their second channels, or, behind the
+// turned ones, any eight; otherwise eight neighbours), of values neighbours.  A group of
+// lanes takes N heads of one row, so that angles, row and page are found once for them.
+// STREAM: rows past the caches, for calls whose rows do not fit them anyway.
+template <int FMT, int DH, typename InT, bool HALVES, int N, bool STREAM>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedTurns turns, PagedAppendArgs a) {
   constexpr int PER = paged_write_pairs(DH), GROUP = 256 / PER;
   using Piece = std::conditional_t<sizeof(InT) == 4, u32x4, u32x2>;
   __shared__ int s_b0;
   const int tid = threadIdx.x, lane = tid & 63, c = tid % GROUP;
-  const uint32_t u0 = blockIdx.x * PER, unit = u0 + tid / GROUP;  // below 2^31
-  const int r = (int)a.d_slots.div(unit), slot = (int)(unit - (uint32_t)r * a.slots);
   const RowRange own(a.a_off, a.n_seqs, a.a_total);
   if (own.none()) return;
-  const int rr = own.nearest(r);  // (what is loaded for others is not used)
-  const bool on = r == rr && c < DH / 8;
 
-  // the pieces' channels
-  const int P = a.n_pairs, cc = c < DH / 8 ? c : 0;
-  const bool split = HALVES && 4 * cc < P;
-  const int first = split ? 4 * cc : 8 * cc, second = split ? P + 4 * cc : 8 * cc + 4;
+  auto run = [&](auto kind, uint32_t block) {
+    constexpr int KIND = kind.value;  // 0 queries, 1 keys, 2 values
+    const int heads = KIND == 0 ? a.q_heads : a.n_heads, slots = KIND == 0 ? a.q_slots : a.kv_slots;
+    const FastDiv d_slots = KIND == 0 ? a.d_q_slots : a.d_kv_slots;
+    const uint32_t u0 = block * PER, unit = u0 + tid / GROUP;  // below 2^31
+    const int r = (int)d_slots.div(unit), h0 = (int)(unit - (uint32_t)r * slots) * N;
+    const int rr = own.nearest(r);  // (what is loaded for others is not used)
+    const int cc = c < DH / 8 ? c : 0;
+    const bool on = r == rr && c < DH / 8;
 
-  const int heads = a.q_heads + 2 * a.n_heads;
-  Piece in[N][2];
+    const int P = a.n_pairs;
+    const bool split = KIND < 2 && HALVES && 4 * cc < P;
+    const int first = split ? 4 * cc : 8 * cc, second = split ? P + 4 * cc : 8 * cc + 4;
+    const InT *from = static_cast<const InT *>(KIND == 0 ? a.q : KIND == 1 ? a.k_new : a.v_new) + (size_t)rr * a.row_stride;
+    Piece in[N][2];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int x = min(slot + i * a.slots, heads - 1);
-    const int h = x < a.q_heads ? x : x < a.q_heads + a.n_heads ? x - a.q_heads : x - a.q_heads - a.n_heads;
-    const void *base = x < a.q_heads ? a.q : x < a.q_heads + a.n_heads ? a.k_new : a.v_new;
-    const InT *p = static_cast<const InT *>(base) + (size_t)rr * a.row_stride + (size_t)h * DH;
-    in[i][0] = *reinterpret_cast<const Piece *>(p + first);
-    in[i][1] = *reinterpret_cast<const Piece *>(p + second);
-  }
-
-  const int tok = a.a_idx[rr];
-  float sn[4], cs[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int pair = min(4 * cc + e, 63);
-    const int pos = a.pos ? a.pos[(size_t)turns.axis[pair] * a.a_total + rr] : tok;
-    turn(pos, turns.turn[pair], sn[e], cs[e]);
-  }
-
-  int b;
-  if (a.a_off) {
-    if (tid < 64) {
-      const int f = wave_find_seq(a.a_off, a.n_seqs, own.nearest((int)a.d_slots.div(u0)), lane);
-      if (tid == 0) s_b0 = f;
+    for (int i = 0; i < N; ++i) {
+      const InT *p = from + min(h0 + i, heads - 1) * DH;
+      const Piece *x = reinterpret_cast<const Piece *>(p + first), *y = reinterpret_cast<const Piece *>(p + second);
+      in[i][0] = STREAM ? __builtin_nontemporal_load(x) : *x;
+      in[i][1] = STREAM ? __builtin_nontemporal_load(y) : *y;
     }
-    __syncthreads();
-    b = s_b0;  // of the workgroup's first row; on from there
-    while (b < a.n_seqs && a.a_off[b + 1] <= rr) ++b;
-  } else {
-    b = (int)a.d_rows.div((uint32_t)rr);
-  }
-  const bool ok = on && b < a.n_seqs && tok >= 0 && (tok >> a.page_log2) < a.max_pages;
-  const int page = ok ? a.table[(size_t)b * a.max_pages + (tok >> a.page_log2)] : -1;
 
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int x = slot + i * a.slots;
-    if (x >= heads) break;
-    float f[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if constexpr (sizeof(InT) == 4) f[e] = __uint_as_float(in[i][e / 4][e % 4]);
-      else f[e] = __uint_as_float(e % 2 ? in[i][e / 4][e % 4 / 2] & 0xFFFF0000u : in[i][e / 4][e % 4 / 2] << 16);
-    }
-    if (x < a.q_heads + a.n_heads) {
+    const int tok = a.a_idx[rr];
+    float sn[4], cs[4];
+    if constexpr (KIND < 2) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (4 * cc + e >= P) break;
-        const int u = HALVES ? e : 2 * e, v = HALVES ? 4 + e : 2 * e + 1;
-        const float p = f[u], q = f[v];
-        f[u] = fmaf(-q, sn[e], p * cs[e]);
-        f[v] = fmaf(p, sn[e], q * cs[e]);
+        const int pair = min(4 * cc + e, 63);
+        const int pos = a.pos ? a.pos[(size_t)turns.axis[pair] * a.a_total + rr] : tok;
+        turn(pos, turns.turn[pair], sn[e], cs[e]);
       }
     }
-    auto bf = [&](int e) { return __builtin_bit_cast(uint32_t, bf16x2{(bf16)f[e], (bf16)f[e + 1]}); };
-    auto raw = [&](int e) { return __float_as_uint(f[e]); };
-    if (x < a.q_heads) {
-      InT *o = static_cast<InT *>(a.q_out) + (size_t)rr * a.q_out_stride + (size_t)x * DH;
-      if (!on) continue;
-      if constexpr (sizeof(InT) == 4) {
-        *reinterpret_cast<u32x4 *>(o + first) = u32x4{raw(0), raw(1), raw(2), raw(3)};
-        *reinterpret_cast<u32x4 *>(o + second) = u32x4{raw(4), raw(5), raw(6), raw(7)};
+    size_t at = 0;
+    bool fits = on;
+    if constexpr (KIND > 0) {
+      int b;
+      if (a.a_off) {
+        if (tid < 64) {
+          const int f = wave_find_seq(a.a_off, a.n_seqs, own.nearest((int)d_slots.div(u0)), lane);
+          if (tid == 0) s_b0 = f;
+        }
+        __syncthreads();
+        b = s_b0;  // of the workgroup's first row; on from there
+        while (b < a.n_seqs && a.a_off[b + 1] <= rr) ++b;
       } else {
-        *reinterpret_cast<u32x2 *>(o + first) = u32x2{bf(0), bf(2)};
-        *reinterpret_cast<u32x2 *>(o + second) = u32x2{bf(4), bf(6)};
+        b = (int)a.d_rows.div((uint32_t)rr);
       }
-      continue;
+      const bool ok = on && b < a.n_seqs && tok >= 0 && (tok >> a.page_log2) < a.max_pages;
+      const int page = ok ? a.table[(size_t)b * a.max_pages + (tok >> a.page_log2)] : -1;
+      fits = (unsigned)page < (unsigned)a.n_pages;
+      at = (((size_t)max(page, 0) * a.n_heads + h0) << a.page_log2) + (tok & ((1 << a.page_log2) - 1));
     }
-    const bool is_v = x >= a.q_heads + a.n_heads;
-    const int h = x - a.q_heads - (is_v ? a.n_heads : 0);
-    const size_t at = (((size_t)max(page, 0) * a.n_heads + h) << a.page_log2) + (tok & ((1 << a.page_log2) - 1));
-    const bool fits = (unsigned)page < (unsigned)a.n_pages;
-    if constexpr (FMT == BF) {
-      if (!fits) continue;
-      bf16 *o = static_cast<bf16 *>(is_v ? a.v : a.k) + at * DH;
-      *reinterpret_cast<u32x2 *>(o + first) = u32x2{bf(0), bf(2)};
-      *reinterpret_cast<u32x2 *>(o + second) = u32x2{bf(4), bf(6)};
-    } else {
-      u32x4 y[2] = {{raw(0), raw(1), raw(2), raw(3)}, {raw(4), raw(5), raw(6), raw(7)}};
-      const int code = exp_code<FMT>(__uint_as_float(group_max<GROUP>(on ? largest<float>(y) : 0u)));
-      const u32x2 o = pack8<FMT, float>(y, code);
-      if (!fits) continue;
-      char *to = static_cast<char *>(is_v ? a.v : a.k) + at * DH;
-      *reinterpret_cast<uint32_t *>(to + first) = o.x;
-      *reinterpret_cast<uint32_t *>(to + second) = o.y;
-      if (c == 0) (is_v ? a.v_exp : a.k_exp)[at] = (uint8_t)code;
-    }
-  }
-}
 
-int paged_append_heads(int32_t head_dim, int64_t rows, int32_t heads) {
-  return rows * heads >= 4096 ? 4 : 1;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (h0 + i >= heads) break;
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (sizeof(InT) == 4) f[e] = __uint_as_float(in[i][e / 4][e % 4]);
+        else f[e] = __uint_as_float(e % 2 ? in[i][e / 4][e % 4 / 2] & 0xFFFF0000u : in[i][e / 4][e % 4 / 2] << 16);
+      }
+      if constexpr (KIND < 2) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int u = HALVES ? e : 2 * e, v = HALVES ? 4 + e : 2 * e + 1;
+          const float x = fmaf(-f[v], sn[e], f[u] * cs[e]), y = fmaf(f[u], sn[e], f[v] * cs[e]);
+          const bool turned = HALVES ? 4 * cc < P : 4 * cc + e < P;
+          f[u] = turned ? x : f[u];
+          f[v] = turned ? y : f[v];
+        }
+      }
+      auto bf = [&](int e) { return __builtin_bit_cast(uint32_t, bf16x2{(bf16)f[e], (bf16)f[e + 1]}); };
+      auto raw = [&](int e) { return __float_as_uint(f[e]); };
+      auto put = [&](auto *to, auto x, auto y) {
+        using V = decltype(x);
+        if (STREAM && KIND == 0) {
+          __builtin_nontemporal_store(x, reinterpret_cast<V *>(to + first));
+          __builtin_nontemporal_store(y, reinterpret_cast<V *>(to + second));
+        } else {
+          *reinterpret_cast<V *>(to + first) = x;
+          *reinterpret_cast<V *>(to + second) = y;
+        }
+      };
+      if constexpr (KIND == 0) {
+        InT *o = static_cast<InT *>(a.q_out) + (size_t)rr * a.q_out_stride + (h0 + i) * DH;
+        if (!fits) continue;
+        if constexpr (sizeof(InT) == 4) put(o, u32x4{raw(0), raw(1), raw(2), raw(3)}, u32x4{raw(4), raw(5), raw(6), raw(7)});
+        else put(o, u32x2{bf(0), bf(2)}, u32x2{bf(4), bf(6)});
+      } else if constexpr (FMT == BF) {
+        if (!fits) continue;
+        put(static_cast<bf16 *>(KIND == 2 ? a.v : a.k) + (at + ((size_t)i << a.page_log2)) * DH, u32x2{bf(0), bf(2)}, u32x2{bf(4), bf(6)});
+      } else {
+        u32x4 y[2] = {{raw(0), raw(1), raw(2), raw(3)}, {raw(4), raw(5), raw(6), raw(7)}};
+        const int code = exp_code<FMT>(__uint_as_float(group_max<GROUP>(on ? largest<float>(y) : 0u)));
+        const u32x2 o = pack8<FMT, float>(y, code);
+        if (!fits) continue;
+        const size_t x = at + ((size_t)i << a.page_log2);
+        put(static_cast<uint8_t *>(KIND == 2 ? a.v : a.k) + x * DH, o.x, o.y);
+        if (c == 0) (KIND == 2 ? a.v_exp : a.k_exp)[x] = (uint8_t)code;
+      }
+    }
+  };
+  const uint32_t id = blockIdx.x;
+  if (id < a.q_blocks) run(std::integral_constant<int, 0>(), id);
+  else if (id < a.q_blocks + a.kv_blocks) run(std::integral_constant<int, 1>(), id - a.q_blocks);
+  else run(std::integral_constant<int, 2>(), id - a.q_blocks - a.kv_blocks);
 }
 
 hipError_t launch_paged_append(DType dt, int32_t format, int32_t head_dim, bool halves, const PagedTurns &turns,
                                PagedAppendArgs a, hipStream_t s) {
-  const int heads = a.q_heads + 2 * a.n_heads, n = paged_append_heads(head_dim, a.a_total, heads);
-  a.slots = (heads + n - 1) / n;
-  a.d_slots = FastDiv::of(a.slots);
-  a.d_rows = FastDiv::of(std::max(1, a.rows_each));
+  // Four heads a lane group share the angles where there are enough of them to fill the chip.
+  const int64_t pairs = (int64_t)a.a_total * (a.q_heads + 2 * a.n_heads);
+  const int n = pairs >= 32768 && a.n_heads >= 4 ? 4 : 1;
   const int per = paged_write_pairs(head_dim);
-  const unsigned grid = (unsigned)(((int64_t)a.a_total * a.slots + per - 1) / per);
+  a.q_slots = std::max(1, (a.q_heads + n - 1) / n);
+  a.kv_slots = (a.n_heads + n - 1) / n;
+  a.d_q_slots = FastDiv::of(a.q_slots);
+  a.d_kv_slots = FastDiv::of(a.kv_slots);
+  a.d_rows = FastDiv::of(std::max(1, a.rows_each));
+  a.q_blocks = a.q_heads ? (uint32_t)(((int64_t)a.a_total * a.q_slots + per - 1) / per) : 0;
+  a.kv_blocks = (uint32_t)(((int64_t)a.a_total * a.kv_slots + per - 1) / per);
+  const unsigned grid = a.q_blocks + 2 * a.kv_blocks;
+  const bool stream = (double)pairs * head_dim * (dt == DType::BF16 ? 2 : 4) >= 64e6;
   return by_shape(format, head_dim, [&](auto fmt, auto dh) {
-    auto go = [&](auto half, auto several) {
-      constexpr bool H = half.value;
+    auto go = [&](auto half, auto several, auto st) {
+      constexpr bool H = half.value, S = st.value;
       constexpr int N = several.value ? 4 : 1;
-      if (dt == DType::BF16) launch_kernel(paged_append_kernel<fmt.value, dh.value, bf16, H, N>, grid, 256, 0, s, turns, a);
-      else launch_kernel(paged_append_kernel<fmt.value, dh.value, float, H, N>, grid, 256, 0, s, turns, a);
+      if (dt == DType::BF16) launch_kernel(paged_append_kernel<fmt.value, dh.value, bf16, H, N, S>, grid, 256, 0, s, turns, a);
+      else launch_kernel(paged_append_kernel<fmt.value, dh.value, float, H, N, S>, grid, 256, 0, s, turns, a);
     };
     auto by_n = [&](auto half) {
-      if (n > 1) go(half, std::true_type());
-      else go(half, std::false_type());
+      if (n > 1 && stream) go(half, std::true_type(), std::true_type());
+      else if (n > 1) go(half, std::true_type(), std::false_type());
+      else go(half, std::false_type(), std::false_type());
     };
     if (halves) by_n(std::true_type());
     else by_n(std::false_type());

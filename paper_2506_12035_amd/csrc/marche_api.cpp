@@ -1718,8 +1718,9 @@ marche_status_t marche_paged_append(const marche_paged_cache_t *cache, int32_t l
     return fail(MARCHE_ERR_INVALID_ARG, "q_out_stride %lld: must be a multiple of 8, >= %lld", (long long)q_out_stride,
                 (long long)n_q_heads * dh);
   const int64_t heads = (int64_t)n_q_heads + 2 * H;
-  if (heads >= (1LL << 28) || a_total * heads >= (1LL << 28) || too_many_threads(a_total * heads, paged_write_pairs(dh)))
-    return fail(MARCHE_ERR_UNSUPPORTED, "a_total*(n_q_heads+2*n_heads) reaches 2^28, or all but");
+  // (queries, keys and values are launched by whole workgroups each)
+  if (heads > (1LL << 28) - 64 || a_total * heads > (1LL << 28) - 64)
+    return fail(MARCHE_ERR_UNSUPPORTED, "a_total*(n_q_heads+2*n_heads) exceeds 2^28 - 64");
   if (a_total == 0) return MARCHE_OK;
   if (!page_table || !a_idx || !k_new || !v_new || (n_q_heads > 0 && (!q || !q_out)))
     return fail(MARCHE_ERR_INVALID_ARG, "NULL argument to marche_paged_append");

@@ -290,11 +290,11 @@ struct PagedAppendArgs {
   void *q_out;
   int64_t row_stride, q_out_stride;
   int32_t n_pages, n_heads, q_heads, page_log2, max_pages, n_seqs, a_total, rows_each, n_pairs;
-  int32_t slots;              // paged_append_plan: lane groups per row
-  FastDiv d_slots, d_rows;    // set by the launch
+  // set by the launch: lane groups per row and workgroups of the queries, and of the keys
+  int32_t q_slots, kv_slots;
+  uint32_t q_blocks, kv_blocks;
+  FastDiv d_q_slots, d_kv_slots, d_rows;
 };
-// Heads of one row that a lane group of the append kernel takes, one after another.
-int paged_append_heads(int32_t head_dim, int64_t rows, int32_t heads);
 hipError_t launch_paged_append(DType dt, int32_t format, int32_t head_dim, bool halves, const PagedTurns &turns,
                                PagedAppendArgs a, hipStream_t s);
 constexpr int PAGED_READ_TOKENS = 128;  // tokens per workgroup of the read kernel

@@ -144,16 +144,16 @@ def test_rotary_refusals(args, status):
     assert e.value.status == status
 
 
-@pytest.mark.parametrize("dh,most", [(64, 2 ** 28 - 1), (80, 2 ** 28 - 16), (128, 2 ** 28 - 16)])
-def test_append_fills_the_largest_launch(dh, most):
-    """Heads of all rows by whole workgroups of 32 (64 channels) or 16: one query, key and
-    value head a row each."""
+@pytest.mark.parametrize("dh", [64, 80, 128])
+def test_append_fills_the_largest_launch(dh):
+    """Whole workgroups of the queries', the keys' and the values' heads: one of each a row."""
     c = _cache(n_heads=1, head_dim=dh)
     rot = binding.rotary(dh, HALVES, [4])
     call = dict(heads=1, rot=rot, stride=dh, q_out_stride=dh, k=FAKE + 8)
-    assert _append(c, total=most // 3, **call) == INVALID and "aligned" in binding.last_error()
-    assert _append(c, total=2 ** 28 // 3 + 1, **call) == UNSUPPORTED and "2^28" in binding.last_error()
-    assert _append(c, total=BIG, **call) == UNSUPPORTED
+    most = (2 ** 28 - 64) // 3
+    assert _append(c, total=most, **call) == INVALID and "aligned" in binding.last_error()
+    for total in (most + 1, 2 ** 28, BIG):
+        assert _append(c, total=total, **call) == UNSUPPORTED and "2^28" in binding.last_error()
 
 
 @pytest.mark.parametrize("call", [_window, _tree], ids=lambda c: c.__name__[1:])
