@@ -799,6 +799,19 @@ int64_t paged_grid(const PagedAttnArgs &a) {
   return (pairs + 7) / 8 * 8 * a.row_blocks * (a.budget > 0 ? 1 : a.splits);
 }
 
+// Sequences of a tree call cut into equal ranges on the device, of 2 `waves` tiles at
+// least, such that those of a whole chunk fill `slots` workgroups and the sequences'
+// last ones, which begin later, the gaps.  (16 int8 caches of 900 .. 32768 tokens, 16 heads of 64, 12 ..
+// 25 rows: 245 us with 512 workgroups for all ranges, in the sequences' order.)
+static void share_out(PagedAttnArgs &a, int64_t tiles, int waves, int64_t slots) {
+  const int64_t per = (int64_t)a.n_heads * a.row_blocks, most = (tiles + 8 * waves - 1) / (8 * waves);
+  if (a.n_seqs > PAGED_MAX_SHARED || tiles * a.n_seqs >= (1LL << 30) || most < 4) return;
+  a.waves = waves;
+  a.chunk = 8 * waves;
+  a.budget = (int32_t)std::min<int64_t>(a.n_seqs + (slots + per - 1) / per, a.n_seqs * most);
+  a.splits = (int32_t)std::min<int64_t>({64, a.budget, most});
+}
+
 // The plan of windows and trees with many rows (paged_rows.h).
 static void rows_plan(PagedAttnArgs &a) {
   const int rows = a.q_max * a.group;
@@ -811,17 +824,12 @@ static void rows_plan(PagedAttnArgs &a) {
   if (a.look == PAGED_WINDOW)
     keys = std::min<int64_t>(keys, (int64_t)a.sinks + a.window + 32 * a.row_waves / a.group + 126);
   const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32);
-  // two workgroups for each compute unit, eight 32-key tiles each at least
-  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({64, (512 + units - 1) / units, tiles / 8}));
+  // two workgroups for each compute unit, twelve 32-key tiles each at least
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({64, (512 + units - 1) / units, tiles / 12}));
   a.chunk = (int32_t)((tiles + splits - 1) / splits);
   a.chunk += a.chunk & 1;
   a.splits = (int32_t)((tiles + a.chunk - 1) / a.chunk);
-  const int64_t per = (int64_t)a.n_heads * a.row_blocks;
-  if (a.look == PAGED_TREE && units < 2048 && a.n_seqs <= PAGED_MAX_SHARED && tiles * a.n_seqs < (1LL << 30) && tiles > 8) {
-    a.budget = (int32_t)(a.n_seqs + (512 + per - 1) / per);
-    a.chunk = 8;  // at least
-    a.splits = (int32_t)std::min<int64_t>({64, a.budget, (tiles + a.chunk - 1) / a.chunk});
-  }
+  if (a.look == PAGED_TREE && units < 2048) share_out(a, tiles, PAGED_ROW_WAVES, 512);
 }
 
 void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
@@ -879,8 +887,10 @@ void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
   // equal ranges, shared out on the device, over 512 workgroups (two of 4
   // wavefronts per compute unit; measured against 256 to 1024 of 2 to 8).
   const int64_t per = (int64_t)a.n_heads * a.row_blocks;
-  if (a.n_select == 0 && a.look != PAGED_WINDOW && a.n_seqs <= PAGED_MAX_SHARED && tiles * a.n_seqs < (1LL << 30) &&
-      a.splits > 1) {
+  if (a.look == PAGED_TREE) {
+    if (units < 2048) share_out(a, tiles, 4, 768);
+  } else if (a.n_select == 0 && a.look != PAGED_WINDOW && a.n_seqs <= PAGED_MAX_SHARED && tiles * a.n_seqs < (1LL << 30) &&
+             a.splits > 1) {
     a.waves = std::min(a.waves, 4);
     a.budget = (int32_t)std::max<int64_t>(2 * a.n_seqs, (512 + per - 1) / per);
     a.chunk = 2 * a.waves;  // at least

@@ -454,7 +454,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256) void paged_attn_kernel(PagedAt
     if (b >= a.budget) return;
     const Shares sh(a, lane);
     chunk = sh.chunk;
-    b = __builtin_amdgcn_readfirstlane(sh.find(b, lane, split_i));
+    b = __builtin_amdgcn_readfirstlane(TREE ? sh.find_long_first(b, lane, split_i) : sh.find(b, lane, split_i));
     if (b < 0) return;
   } else if (b >= a.n_seqs) {
     return;

@@ -164,19 +164,23 @@ __global__ __launch_bounds__(QB * 64, 2) void paged_rows_kernel(PagedAttnArgs a,
   }
   auto key_of = [&](int t) { return WIN ? ROWS_TK * (t >= sink_tiles ? t + jump : t) : base + ROWS_TK * t; };
 
-  // Page ids of a tile's four 16-key parts, -1 where there are no tokens.  Uniform.
+  // Page ids of a tile's four 16-key parts, -1 where there are no tokens.  Uniform, from a
+  // register that holds those of 16 tiles, asked for in order (scalar loads in the loop
+  // would make the waits for LDS reads waits for them).
   struct Pages {
     int id[4];
   };
+  int ids = -1, ids_at = t0 - 16;
   auto pages_of = [&](int t) {
-    Pages p;
-    const int key = key_of(t);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int k = key + 16 * j;
-      const int x = tab[min(k >> a.page_log2, a.max_pages - 1)];
-      p.id[j] = k < end && (unsigned)x < (unsigned)a.n_pages ? x : -1;
+    if (t - ids_at >= 16) {
+      ids_at = t;
+      const int key = key_of(t + (lane >> 2)) + 16 * (lane & 3);
+      const int x = key < end ? tab[key >> a.page_log2] : -1;
+      ids = (unsigned)x < (unsigned)a.n_pages ? x : -1;
     }
+    Pages p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p.id[j] = __builtin_amdgcn_readlane(ids, 4 * (t - ids_at) + j);
     return p;
   };
   auto slot_of = [&](int id, int key) {
