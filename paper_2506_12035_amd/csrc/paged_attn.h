@@ -313,19 +313,9 @@ struct Span {
 __device__ __forceinline__ Span span_of(const PagedAttnArgs &a, int len, int row, int rows, int lane) {
   int lo = 0, hi = 0;
   window_of(a, len, a.q_idx[row + min(lane, rows - 1)], lo, hi);
-  Span s{hi > 0 ? lo : INT32_MAX, lo, hi, hi};
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    s.lo_min = min(s.lo_min, __shfl_xor(s.lo_min, o, 64));
-    s.lo_max = max(s.lo_max, __shfl_xor(s.lo_max, o, 64));
-    s.hi_min = min(s.hi_min, __shfl_xor(s.hi_min, o, 64));
-    s.hi_max = max(s.hi_max, __shfl_xor(s.hi_max, o, 64));
-  }
-  s.lo_min = __builtin_amdgcn_readfirstlane(s.lo_min);
-  s.lo_max = __builtin_amdgcn_readfirstlane(s.lo_max);
-  s.hi_min = __builtin_amdgcn_readfirstlane(s.hi_min);
-  s.hi_max = __builtin_amdgcn_readfirstlane(s.hi_max);
-  return s;
+  // (none of them is negative)
+  auto least = [](int v) { return (int)~wave_max_u32(~(uint32_t)v); };
+  return Span{least(hi > 0 ? lo : INT32_MAX), (int)wave_max_u32((uint32_t)lo), least(hi), (int)wave_max_u32((uint32_t)hi)};
 }
 // Bits `at` .. at + 15 of a row's mask; those before bit 0 (the context) are set, those
 // behind the last word are not.

@@ -221,14 +221,24 @@ __global__ __launch_bounds__(QB * 64, 2) void paged_rows_kernel(PagedAttnArgs a,
     const int key = key_of(t);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int row = min((64 * (n * QB + wave) + lane) / PPR, ROWS_TK - 1), j = row >> 4;
+      const int op = min(n * QB + wave, OPS - 1), row = (64 * op + (DH == 80 ? lane : 0)) / PPR, j = row >> 4;
       const int id = j == 0 ? p.id[0] : j == 1 ? p.id[1] : j == 2 ? p.id[2] : p.id[3];
-      o.c[n] = exps[slot_of(id, key + row)];
+      if constexpr (DH == 80) o.c[n] = exps[slot_of(id, key + row)];
+      else o.c[n] = at<uint8_t>(scalar(exps + slot_of(id, key + row)), (uint32_t)(lane / PPR), 0);
     }
     return o;
   };
   // The pieces that this lane fetched, in bf16 to their places (rows without a token: zeros).
-  auto convert = [&](const char *raw, const Codes &codes, int t, const Pages &p, char *to) {
+  struct Raw {
+    u32x4 w[N];
+  };
+  auto read_raw = [&](const char *raw) {
+    Raw o;
+#pragma unroll
+    for (int n = 0; n < N; ++n) o.w[n] = *reinterpret_cast<const u32x4 *>(raw + 16 * min(64 * (n * QB + wave) + lane, PIECES - 1));
+    return o;
+  };
+  auto convert = [&](const Raw &raw, const Codes &codes, int t, const Pages &p, char *to) {
     const bool whole = full(key_of(t), p);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -236,7 +246,7 @@ __global__ __launch_bounds__(QB * 64, 2) void paged_rows_kernel(PagedAttnArgs a,
       const int op = n * QB + wave;
       if (OPS % QB != 0 && op >= OPS) break;
       const int x = 64 * op + lane, row = x / PPR, part = x - row * PPR;
-      u32x4 w = *reinterpret_cast<const u32x4 *>(raw + 16 * x);
+      u32x4 w = raw.w[n];
       float s = exp_scale(codes.c[n]);
       if (!whole) {
         const int j = row >> 4, id = j == 0 ? p.id[0] : j == 1 ? p.id[1] : j == 2 ? p.id[2] : p.id[3];
@@ -357,6 +367,9 @@ __global__ __launch_bounds__(QB * 64, 2) void paged_rows_kernel(PagedAttnArgs a,
     read_k(0);
     read_v(0);
     __builtin_amdgcn_sched_barrier(0);
+    // (products first: the other workgroup's wavefront fills what they leave; 580 us without
+    // for 8192 rows over windows of 8192, 561 with)
+    __builtin_amdgcn_s_setprio(1);
     const float mm = m_run == -INFINITY ? 0.f : -m_run;
     float x[8];
     auto weight = [&](int y, int i) {
@@ -396,6 +409,7 @@ __global__ __launch_bounds__(QB * 64, 2) void paged_rows_kernel(PagedAttnArgs a,
       }
     }
     __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(0);
   };
   // Tile t's logits are formed during tile t - 1's softmax and product: K runs a tile ahead of
   // V.  Slot x of K and of V holds tiles of parity x; behind them lie the 8-bit rows.
@@ -422,9 +436,10 @@ __global__ __launch_bounds__(QB * 64, 2) void paged_rows_kernel(PagedAttnArgs a,
       fetch(a.k, second, p1, v_slot(1));
       const Codes c0 = fetch_codes(a.k_exp, t0, p0), c1 = fetch_codes(a.v_exp, t0, p0), c2 = fetch_codes(a.k_exp, second, p1);
       rows_arrive();
-      convert(k_raw, c0, t0, p0, k_slot(0));
-      convert(v_raw, c1, t0, p0, v_slot(0));
-      convert(v_slot(1), c2, second, p1, k_slot(1));
+      const Raw r0 = read_raw(k_raw), r1 = read_raw(v_raw), r2 = read_raw(v_slot(1));
+      convert(r0, c0, t0, p0, k_slot(0));
+      convert(r1, c1, t0, p0, v_slot(0));
+      convert(r2, c2, second, p1, k_slot(1));
       __syncthreads();
     }
     f32x16 sa[2], sb[2];
@@ -456,8 +471,9 @@ __global__ __launch_bounds__(QB * 64, 2) void paged_rows_kernel(PagedAttnArgs a,
       }
       rows_arrive();
       if constexpr (FMT != BF) {
-        if (third) convert(k_raw, kc, t + 2, p2, k_slot(X));
-        if (second) convert(v_raw, vc, t + 1, p1, v_slot(1 - X));
+        const Raw kr = read_raw(k_raw), vr = read_raw(v_raw);
+        if (third) convert(kr, kc, t + 2, p2, k_slot(X));
+        if (second) convert(vr, vc, t + 1, p1, v_slot(1 - X));
       }
       __syncthreads();
       if constexpr (FMT == BF) {
