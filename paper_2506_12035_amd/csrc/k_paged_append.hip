@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedTurns turns, Pag
     Piece in[N][2];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const InT *p = from + min(h0 + i, heads - 1) * DH;
+      const InT *p = from + (size_t)min(h0 + i, heads - 1) * DH;
       const Piece *x = reinterpret_cast<const Piece *>(p + first), *y = reinterpret_cast<const Piece *>(p + second);
       in[i][0] = STREAM ? __builtin_nontemporal_load(x) : *x;
       in[i][1] = STREAM ? __builtin_nontemporal_load(y) : *y;
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedTurns turns, Pag
         }
       };
       if constexpr (KIND == 0) {
-        InT *o = static_cast<InT *>(a.q_out) + (size_t)rr * a.q_out_stride + (h0 + i) * DH;
+        InT *o = static_cast<InT *>(a.q_out) + (size_t)rr * a.q_out_stride + (size_t)(h0 + i) * DH;
         if (!fits) continue;
         if constexpr (sizeof(InT) == 4) put(o, u32x4{raw(0), raw(1), raw(2), raw(3)}, u32x4{raw(4), raw(5), raw(6), raw(7)});
         else put(o, u32x2{bf(0), bf(2)}, u32x2{bf(4), bf(6)});

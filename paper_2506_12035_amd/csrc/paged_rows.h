@@ -77,7 +77,7 @@ __device__ __forceinline__ float half_sum(float v) {
 }
 
 template <int FMT, int DH, int QB, int MODE>
-__global__ __launch_bounds__(QB * 64, 2) void paged_rows_kernel(PagedAttnArgs a, const int32_t *__restrict__ table) {
+__global__ __launch_bounds__(QB * 64, DH == 64 && FMT != BF ? 3 : 2) void paged_rows_kernel(PagedAttnArgs a, const int32_t *__restrict__ table) {
   using L = RowsLay<DH>;
   constexpr bool WIN = MODE == PAGED_WINDOW;
   constexpr int T = QB * 64;
