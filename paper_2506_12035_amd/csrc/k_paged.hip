@@ -621,12 +621,11 @@ __global__ __launch_bounds__(PAGED_JOIN_THREADS) void paged_join_kernel(PagedAtt
   static_cast<RowT *>(a.o)[row * DH + d] = (RowT)(seen ? total / l : 0.f);
 }
 
-// The same for many rows, whose sequences of one range have been written already: a lane
-// group per (row, head), four channels a lane, ROWS_JOIN of them in turn; the
-// group's lanes hold the parts' maxima and sums.
-constexpr int ROWS_JOIN = 4;
+// The same for many rows: a lane group per (row, head), four channels a lane, `times`
+// of them in turn; the group's lanes hold the parts' maxima and sums.  (paged_rows.h has
+// written the sequences of one range already.)
 template <int DH, typename RowT>
-__global__ __launch_bounds__(256) void paged_rows_join_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256) void paged_rows_join_kernel(PagedAttnArgs a, int times) {
   constexpr int LANES = DH == 64 ? 16 : 32, PER = 256 / LANES, K = 64 / LANES;
   const int tid = threadIdx.x, lane = tid & 63, c = tid % LANES;
   const int heads = a.n_heads * a.group;
@@ -634,21 +633,27 @@ __global__ __launch_bounds__(256) void paged_rows_join_kernel(PagedAttnArgs a) {
   int chunk = 0;
   if (a.budget > 0) chunk = Shares(a, lane).chunk;
   const int first = a.q_off ? a.q_off[0] : 0, last = a.q_off ? a.q_off[a.n_seqs] : a.q_total;
+  int row = -1, b = 0, splits = a.splits;
 #pragma unroll 1
-  for (int i = 0; i < ROWS_JOIN; ++i) {
-    const int64_t x0 = ((int64_t)blockIdx.x * ROWS_JOIN + i) * PER + (tid & ~63) / LANES;  // of the wavefront
+  for (int i = 0; i < times; ++i) {
+    const int64_t x0 = ((int64_t)blockIdx.x * times + i) * PER + (tid & ~63) / LANES;  // of the wavefront
     if (x0 >= n) return;
     const int64_t x = min(x0 + lane / LANES, n - 1);
     const int r = (int)(x / heads);
-    int b = a.q_off ? wave_find_seq(a.q_off, a.n_seqs, __builtin_amdgcn_readfirstlane((int)(x0 / heads)), lane) : r / a.rows_each;
-    if (a.q_off)
-      while (b < a.n_seqs && a.q_off[b + 1] <= r) ++b;
-    int splits = a.splits;
-    if (a.budget > 0) {
-      const int len = min(paged_len(a.lens[min(b, a.n_seqs - 1)], a.max_pages, a.page_log2), a.len_max);
-      splits = (((len + 31) >> 5) + chunk - 1) / chunk;
+    if (a.q_off && i == 0) b = wave_find_seq(a.q_off, a.n_seqs, __builtin_amdgcn_readfirstlane((int)(x0 / heads)), lane);
+    if (r != row) {
+      row = r;
+      if (a.q_off) {
+        while (b < a.n_seqs && a.q_off[b + 1] <= r) ++b;
+      } else {
+        b = r / a.rows_each;
+      }
+      if (a.budget > 0) {
+        const int len = min(paged_len(a.lens[min(b, a.n_seqs - 1)], a.max_pages, a.page_log2), a.len_max);
+        splits = (((len + 31) >> 5) + chunk - 1) / chunk;
+      }
     }
-    if (r < first || r >= last || splits == 1 || x0 + lane / LANES >= n) continue;  // (whole groups)
+    if (r < first || r >= last || (splits == 1 && a.row_waves > 0) || x0 + lane / LANES >= n) continue;  // (whole groups)
     float ms[K], ls[K], m = -INFINITY;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -923,10 +928,16 @@ hipError_t launch_paged_attention(DType dt, int32_t format, int32_t head_dim, co
 
 hipError_t launch_paged_join(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)a.q_total * a.n_heads * a.group);
-  if (a.row_waves > 0) {
-    const int64_t per = ROWS_JOIN * (head_dim == 64 ? 16 : 8);
+  // (304 rows of 16 heads of 64 in up to 23 parts: 13.5 us with a workgroup each, 6.3 so.
+  // Four in turn repeat less of what comes before the parts: 2048 rows of 32 heads of 128 in up to
+  // two parts 17.1 us, 21.2 one by one; the 304 rows 15.2.)
+  if (a.row_waves > 0 || ((a.look == PAGED_WINDOW || a.look == PAGED_TREE) && grid >= 4096)) {
+    const unsigned per = head_dim == 64 ? 16 : 8;
+    const int times = grid >= 4096 * per ? 4 : 1;
+    const unsigned groups = (grid + per * times - 1) / (per * times);
     return by_shape(BF, head_dim, [&](auto, auto dh) {
-      launch_kernel(paged_rows_join_kernel<dh.value, bf16>, (unsigned)((grid + per - 1) / per), 256, 0, s, a);
+      if (dt == DType::BF16) launch_kernel(paged_rows_join_kernel<dh.value, bf16>, groups, 256, 0, s, a, times);
+      else launch_kernel(paged_rows_join_kernel<dh.value, float>, groups, 256, 0, s, a, times);
     });
   }
   return by_shape(BF, head_dim, [&](auto, auto dh) {
