@@ -804,10 +804,13 @@ int64_t paged_grid(const PagedAttnArgs &a) {
   return (pairs + 7) / 8 * 8 * a.row_blocks * (a.budget > 0 ? 1 : a.splits);
 }
 
-// Sequences of a tree call cut into equal ranges on the device, of 2 `waves` tiles at
-// least, such that those of a whole chunk fill `slots` workgroups and the sequences'
-// last ones, which begin later, the gaps.  (16 int8 caches of 900 .. 32768 tokens, 16 heads of 64, 12 ..
-// 25 rows: 245 us with 512 workgroups for all ranges, in the sequences' order.)
+// Sequences of a tree call cut into equal ranges on the device, of 8 `waves` 32-key tiles
+// at least, such that those of a whole chunk fill `slots` workgroups and the sequences'
+// last ones, which begin later, the gaps: where the longest cache has more than three such
+// ranges.  16 int8 caches of 900 .. 32768 tokens, 16 heads of 64, 12 .. 25 rows: 245 us with 512
+// workgroups for all ranges in the sequences' order, 148 so (768 slots; 152 with 512, 203 with
+// 256).  Caches of 2000 tokens are as fast or faster in equal parts of each (8 rows over one: 18.3 us
+// shared out, 15.3 not; 32 of 500 .. 2000: 62.7 and 53.1).
 static void share_out(PagedAttnArgs &a, int64_t tiles, int waves, int64_t slots) {
   const int64_t per = (int64_t)a.n_heads * a.row_blocks, most = (tiles + 8 * waves - 1) / (8 * waves);
   if (a.n_seqs > PAGED_MAX_SHARED || tiles * a.n_seqs >= (1LL << 30) || most < 4) return;
@@ -817,7 +820,20 @@ static void share_out(PagedAttnArgs &a, int64_t tiles, int waves, int64_t slots)
   a.splits = (int32_t)std::min<int64_t>({64, a.budget, most});
 }
 
-// The plan of windows and trees with many rows (paged_rows.h).
+// Whether windows and trees go by blocks of many rows (paged_rows.h): bf16 rows, more
+// than half a block of them for a key head, and blocks for a good part of the chip, as a
+// block's wavefronts do not share its keys out.  Heads of 128 over e4m3 caches up to 8000
+// tokens: 32 sequences of 64 (packed) rows 148.3 us by blocks and 133.6 without, of 128 rows 170.1 and
+// 231.7; 16 blocks in all 43.9 and 33.6, 24 43.8 and 38.3, 32 44.5 and 47.7.  Windows of 1024, heads of
+// 64: 110 blocks 26.2 and 21.0, 128 25.1 and 22.8, 160 29.6 and 31.4, 256 33.4 and 36.5, 1024
+// 66.2 and 101.0.
+static bool by_rows(DType dt, int32_t head_dim, const PagedAttnArgs &a) {
+  const int64_t rows = (int64_t)a.q_max * a.group, block = 32 * PAGED_ROW_WAVES;
+  if (dt != DType::BF16 || (a.look != PAGED_WINDOW && a.look != PAGED_TREE) || rows <= block / 2) return false;
+  return (int64_t)a.n_seqs * a.n_heads * ((rows + block - 1) / block) >= (head_dim == 128 ? 32 : 128);
+}
+
+// Their plan.
 static void rows_plan(PagedAttnArgs &a) {
   const int rows = a.q_max * a.group;
   a.row_waves = PAGED_ROW_WAVES;
@@ -829,7 +845,8 @@ static void rows_plan(PagedAttnArgs &a) {
   if (a.look == PAGED_WINDOW)
     keys = std::min<int64_t>(keys, (int64_t)a.sinks + a.window + 32 * a.row_waves / a.group + 126);
   const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32);
-  // two workgroups for each compute unit, twelve 32-key tiles each at least
+  // two workgroups for each compute unit, twelve 32-key tiles each at least (a prompt of 512 rows, 128
+  // blocks: 31.4 us in two ranges of eight tiles, 20.9 in one)
   const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({64, (512 + units - 1) / units, tiles / 12}));
   a.chunk = (int32_t)((tiles + splits - 1) / splits);
   a.chunk += a.chunk & 1;
@@ -842,7 +859,7 @@ void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a) {
   a.row_waves = a.budget = 0;
   a.d_heads = FastDiv::of(a.n_heads);
   a.d_group = FastDiv::of(a.group);
-  if (dt == DType::BF16 && rows > PAGED_FEW_ROWS && (a.look == PAGED_WINDOW || a.look == PAGED_TREE)) {
+  if (by_rows(dt, head_dim, a)) {
     rows_plan(a);
     a.d_splits = FastDiv::of(a.budget > 0 ? 1 : a.splits);
     a.d_blocks = FastDiv::of(a.row_blocks);

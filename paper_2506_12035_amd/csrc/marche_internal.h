@@ -339,8 +339,7 @@ hipError_t launch_paged_select(DType dt, int32_t head_dim, const PagedSelectArgs
 // of a window up to its own token, and the sequence's first ones; a context and the
 // drafted tokens that its mask names.
 enum PagedLook : int32_t { PAGED_ALL = 0, PAGED_LISTED = 1, PAGED_WINDOW = 2, PAGED_TREE = 3 };
-constexpr int PAGED_FEW_ROWS = 64;  // packed rows up to which windows and trees go the way of the others
-constexpr int PAGED_ROW_WAVES = 4;  // wavefronts of 32 rows of a workgroup otherwise
+constexpr int PAGED_ROW_WAVES = 4;  // wavefronts of 32 rows of a workgroup of paged_rows.h
 constexpr int PAGED_MAX_MASK_WORDS = 64;  // of 32 drafted tokens each
 constexpr int PAGED_JOIN_THREADS = 256;  // of the join's workgroup, one per (row, query head)
 constexpr int PAGED_MAX_SHARED = 256;  // sequences of a call whose ranges are shared out on the device

@@ -27,12 +27,18 @@ MANY_ROWS = [
     ([333, 4097], [128, 129], 1, 2, 256),
     ([2049, 700, 4200], [300, 500, 257], 1, 1, 128),
     ([900], [25], 16, 1, 64),
+    # enough blocks of 128 rows to go by them: caches cut in equal parts, shared out, ragged, blocks of
+    # more than 64 rows
+    ([1700], [70], 1, 128, 32),
+    ([3300, 100, 1000], [66, 70, 5], 1, 43, 64),
+    ([64, 65, 63, 128, 129, 16, 15, 1], [33, 32, 31, 64, 65, 16, 15, 1], 4, 6, 16),
+    ([1049, 700], [300, 257], 1, 22, 16),
 ]
 
 
 @pytest.mark.parametrize("dh", [64, 80, 128])
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("case", MANY_ROWS, ids=lambda c: f"n{max(c[0])}r{sum(c[1])}g{c[2]}b{len(c[0])}")
+@pytest.mark.parametrize("case", MANY_ROWS, ids=lambda c: f"n{max(c[0])}r{sum(c[1])}g{c[2]}h{c[3]}b{len(c[0])}")
 def test_many_rows(case, fmt, dh):
     say(f"paged masks, many rows {case[0][:4]} {case[1][:4]} {fmt} {dh}")
     lens, rows, group, H, page = case
@@ -76,18 +82,18 @@ def test_equal_rows_need_no_offsets(rows):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("rows", [2, 100])
-def test_queries_that_are_not_finite_stay_among_themselves(fmt, rows):
-    say(f"paged masks, NaN queries {fmt} {rows}")
+@pytest.mark.parametrize("rows,H", [(2, 1), (100, 1), (100, 64)])
+def test_queries_that_are_not_finite_stay_among_themselves(fmt, rows, H):
+    say(f"paged masks, NaN queries {fmt} {rows} {H}")
     rng = np.random.default_rng(1)
-    pool = Pool(fmt, [300], 1, 64, 16, seed=1)
-    q = rnd(rng.standard_normal((rows, 128)), "bf16")
+    pool = Pool(fmt, [300], H, 64, 16, seed=1)
+    q = rnd(rng.standard_normal((rows, H * 128)), "bf16")
     q[1, 3], q[0, 70] = np.nan, np.inf
     t = np.full(rows, 250)
     for got in (window(pool, dev(q, torch.bfloat16), [rows], 2, "bf16", t, 100, 3),
                 tree(pool, dev(q, torch.bfloat16), [rows], 2, "bf16", [200], np.full((rows, 1), 5, np.uint32))):
-        g = got.double().cpu().numpy().reshape(rows, 2, 64)
-        bad = np.zeros((rows, 2), bool)
+        g = got.double().cpu().numpy().reshape(rows, 2 * H, 64)
+        bad = np.zeros((rows, 2 * H), bool)
         bad[1, 0] = bad[0, 1] = True
         assert np.isnan(g[bad]).all() and np.isfinite(g[~bad]).all()
 
@@ -96,9 +102,9 @@ def test_lengths_are_cut():
     """len_max below a length, and lengths past the page table, for few and many rows."""
     say("paged masks, cut lengths")
     rng = np.random.default_rng(4)
-    for rows in (4, 90):
-        pool = Pool("bf16", [200, 90], 1, 64, 16, seed=1, width_extra=0)
-        q = rnd(rng.standard_normal((2 * rows, 64)), "bf16")
+    for rows, H in ((4, 1), (90, 1), (90, 64)):
+        pool = Pool("bf16", [200, 90], H, 64, 16, seed=1, width_extra=0)
+        q = rnd(rng.standard_normal((2 * rows, H * 64)), "bf16")
         d = dev(q, torch.bfloat16)
         t = np.arange(2 * rows) % rows + 50
         mask = rng.integers(0, 2 ** 32, (2 * rows, 7), dtype=np.uint32)
@@ -114,15 +120,15 @@ def test_lengths_are_cut():
                 assert attention_errors(pool, g.double().cpu().numpy(), q, [rows] * 2, 1, "bf16", look) <= 1
 
 
-@pytest.mark.parametrize("fmt,dh,rows", [("e4m3", 128, 80), ("bf16", 80, 80), ("int8", 64, 3)])
-def test_captured_calls_replay(fmt, dh, rows):
+@pytest.mark.parametrize("fmt,dh,rows,H", [("e4m3", 128, 80, 8), ("bf16", 80, 80, 32), ("int8", 64, 3, 1), ("bf16", 128, 70, 1)])
+def test_captured_calls_replay(fmt, dh, rows, H):
     """Both attentions captured, with split caches and their joins, replayed on new queries and
     lengths with eager calls between."""
-    say(f"paged masks captured {fmt} {dh} {rows}")
+    say(f"paged masks captured {fmt} {dh} {rows} {H}")
     lens = [9000, 40]
-    pool = Pool(fmt, lens, 1, dh, 64, seed=1)
+    pool = Pool(fmt, lens, H, dh, 64, seed=1)
     group, total, len_max = 2, 2 * rows, 9000
-    heads = group
+    heads = group * H
     D = heads * dh
     n1 = binding.paged_attention_window_workspace_bytes(pool.cache, 2, total, rows, heads, len_max, 6000, 4)
     n2 = binding.paged_attention_tree_workspace_bytes(pool.cache, 2, total, rows, heads, len_max)
@@ -166,13 +172,103 @@ def test_captured_calls_replay(fmt, dh, rows):
         assert torch.equal(e1, o1) and torch.equal(e2, o2) and e1.isfinite().all() and e2.isfinite().all()
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dh,H", [(64, 64), (80, 64), (128, 16)])
+def test_masked_places_count_nothing_in_many_rows(dh, H, fmt):
+    """Infinities and NaN in masked keys and values, in tiles that rows see a part of, by blocks
+    of many rows; an infinite value that some rows see reaches its channel there alone."""
+    say(f"paged masked infinities, many rows {fmt} {dh}")
+    rng = np.random.default_rng(3)
+    n, rows = 400, 150
+    pool = Pool(fmt, [n], H, dh, 16, seed=4)
+    bad = [3, 150, 151, 249, n - 1]
+    for j, x in zip(bad, (np.nan, np.inf, -np.inf, np.nan, np.inf)):
+        page, slot = pool.table[0][j // 16], j % 16
+        for d, e in ((pool.dk, pool.dke), (pool.dv, pool.dve)):
+            if fmt == "bf16":
+                d[0, page, 1, slot, 5:9] = x
+            else:
+                d[0, page, 1, slot] = 0x7F if fmt == "e4m3" else 0
+                e[0, page, 1, slot] = 255
+    group = 2 if dh == 128 else 1
+    q = rnd(rng.standard_normal((rows, H * group * dh)), "bf16")
+    t = np.array([250 + 20 + 119 * i // rows for i in range(rows)])
+    t = np.where(t == n - 1, n - 2, t)
+    got = window(pool, dev(q, torch.bfloat16), [rows], group, "bf16", t, 20, 3).double().cpu().numpy()
+    assert np.isfinite(got).all()
+    assert attention_errors(pool, got, q, [rows], group, "bf16", _window_look(pool, [rows], t, 20, 3)) <= 1
+    mask = rng.integers(0, 2 ** 32, (rows, 13), dtype=np.uint32)
+    for j in bad:
+        mask[:, (j - 3) // 32] &= ~np.uint32(1 << ((j - 3) % 32))
+    got = tree(pool, dev(q, torch.bfloat16), [rows], group, "bf16", [3], mask).double().cpu().numpy()
+    assert np.isfinite(got).all()
+    assert attention_errors(pool, got, q, [rows], group, "bf16", _tree_look(pool, [rows], [3], mask)) <= 1
+    if fmt != "bf16":
+        return
+    pool = Pool(fmt, [n], H, dh, 16, seed=4)
+    page, slot = pool.table[0][100 // 16], 100 % 16
+    pool.dv[0, page, 0, slot, 9] = float("inf")
+    t = np.array([100 + (i % 2) * 60 for i in range(rows)])
+    o = window(pool, dev(q, torch.bfloat16), [rows], group, "bf16", t, 30, 0).double().cpu().numpy().reshape(rows, H, group, dh)
+    want = np.zeros(o.shape, bool)
+    want[::2, 0, :, 9] = True
+    assert np.array_equal(np.isinf(o), want) and not np.isnan(o).any()
+
+
+@pytest.mark.parametrize("dh,H", [(64, 64), (128, 16)])
+def test_layout_of_many_rows(dh, H):
+    """Rows of no sequence are left alone, pages that no row sees may be gone, by blocks of many rows."""
+    say(f"paged masks, layout of many rows {dh}")
+    rng = np.random.default_rng(2)
+    lens, rows, before, extra = [300, 20, 600], [70, 1, 140], 2, 3
+    total = sum(rows)
+    pool = Pool("bf16", lens, H, dh, 32, seed=7)
+    q = rnd(rng.standard_normal((total, H * dh)), "bf16")
+    buf = torch.full((before + total + extra, H * dh + 24), float("nan"), dtype=torch.bfloat16, device="cuda")
+    buf[before:before + total, 8:8 + H * dh] = dev(q, torch.bfloat16)
+    off = i32(offsets(rows) + before)
+    t = np.concatenate([[BIG] * before] + [n - 1 - np.arange(r) for n, r in zip(lens, rows)] + [[5] * extra])
+    mask = rng.integers(0, 2 ** 32, (before + total + extra, 2), dtype=np.uint32)
+    ctx = [max(0, n - r) for n, r in zip(lens, rows)]
+    for kind in ("tree", "window"):
+        o = torch.full((before + total + extra, H * dh), 7.0, dtype=torch.bfloat16, device="cuda")
+        if kind == "window":
+            seen, pool.table = pool.table, pool.table.copy()
+            pool.table[2, 1:(600 - 140 - 77) // 32] = -1
+            pool.dtable = i32(pool.table)
+            window(pool, buf[:, 8:], rows, 1, "bf16", t, 77, 5, o=o, off=off, q_stride=H * dh + 24)
+            pool.table = seen
+            look = _window_look(pool, rows, t[before:before + total], 77, 5)
+        else:
+            tree(pool, buf[:, 8:], rows, 1, "bf16", ctx, mask, o=o, off=off, q_stride=H * dh + 24)
+            look = _tree_look(pool, rows, ctx, mask[before:before + total])
+        assert (o[:before] == 7).all() and (o[before + total:] == 7).all()
+        got = o[before:before + total].double().cpu().numpy()
+        assert attention_errors(pool, got, q, rows, 1, "bf16", look) <= 1
+
+
+def test_rows_that_see_nothing_among_many():
+    """Empty masks and windows in blocks of many rows, on cut caches and on others."""
+    say("paged masks that leave nothing, many rows")
+    pool = Pool("e4m3", [5000, 40, 0], 16, 128, 16, seed=2)
+    rows = [130, 70, 66]
+    q = dev(np.ones((266, 16 * 128)), torch.bfloat16)
+    t = np.full(266, -1)
+    mask = np.zeros((266, 3), np.uint32)
+    assert (window(pool, q, rows, 1, "bf16", t, 900, 9) == 0).all() and (tree(pool, q, rows, 1, "bf16", [0, 0, 0], mask) == 0).all()
+    t[5], mask[129, 2] = 7000, 1
+    one = window(pool, q, rows, 1, "bf16", t, 900, 3).cpu(), tree(pool, q, rows, 1, "bf16", [0, 0, 0], mask).cpu()
+    for o, i in zip(one, (5, 129)):
+        assert (o[i] != 0).any() and (o[[j for j in range(266) if j != i]] == 0).all()
+
+
 def test_repeated_calls_are_equal():
     """Sums do not depend on the order in which workgroups run."""
     say("paged masks repeated")
     rng = np.random.default_rng(1)
-    pool = Pool("e4m3", [9000, 3000, 77], 2, 128, 64, seed=1)
-    for rows in ([2, 2, 2], [90, 70, 50]):
-        q = dev(rnd(rng.standard_normal((sum(rows), 2 * 2 * 128)), "bf16"), torch.bfloat16)
+    for rows, H in (([2, 2, 2], 2), ([90, 70, 50], 2), ([90, 70, 50], 8)):
+        pool = Pool("e4m3", [9000, 3000, 77], H, 128, 64, seed=1)
+        q = dev(rnd(rng.standard_normal((sum(rows), H * 2 * 128)), "bf16"), torch.bfloat16)
         mask = rng.integers(0, 2 ** 32, (sum(rows), 2), dtype=np.uint32)
         t = rng.integers(0, 9000, sum(rows))
         one = tree(pool, q, rows, 2, "bf16", [8950, 2990, 0], mask), window(pool, q, rows, 2, "bf16", t, 4000, 4)
