@@ -7,6 +7,10 @@
 // to either side, as float32 has no bits left for far positions (2^20 times any
 // frequency is off by 0.06 radians); sine and cosine of what is left are float32
 // polynomials.  Keys go from float32 to the cache's format by one rounding.
+//
+// Bound by bytes: 40960 rows of 12 heads of 64, three axes, bf16 to int8, 316 MB: 76.4 us,
+// 4.1 TB/s (93.6 with queries, keys and values of a row side by side in a wavefront, which
+// then ran each other's instructions).  One row of 48 heads: 3.2 us, latency.
 #include <algorithm>
 
 #include "paged_device.h"
@@ -163,7 +167,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedTurns turns, Pag
 
 hipError_t launch_paged_append(DType dt, int32_t format, int32_t head_dim, bool halves, const PagedTurns &turns,
                                PagedAppendArgs a, hipStream_t s) {
-  // Four heads a lane group share the angles where there are enough of them to fill the chip.
+  // Four heads a lane group share the angles where that leaves 2048 wavefronts or more of 64
+  // channels; below, a head each is the shorter way.
   const int64_t pairs = (int64_t)a.a_total * (a.q_heads + 2 * a.n_heads);
   const int n = pairs >= 32768 && a.n_heads >= 4 ? 4 : 1;
   const int per = paged_write_pairs(head_dim);
