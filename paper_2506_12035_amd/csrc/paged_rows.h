@@ -459,6 +459,7 @@ __global__ __launch_bounds__(QB * 64, DH == 64 && FMT != BF ? 3 : 2) void paged_
           sa[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(k_slot(0), k_base, kb, st), qf[st], sa[kb], 0, 0, 0);
       }
     }
+    __syncthreads();  // (the first tile's K is read: the third one's takes its place)
     // one tile of parity `par` (behind the last tile the logits are of what lies in LDS, and
     // not used)
     auto step = [&](int t, auto par, f32x16 (&s)[2], f32x16 (&s_next)[2]) {
