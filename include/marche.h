@@ -582,7 +582,7 @@ marche_status_t marche_rotary_init(marche_rotary_t *rotary, int32_t head_dim, in
  * turned likewise, go to row r of q_out (rows q_out_stride apart).  Angles are formed in 64
  * bits, the rotation in float32; keys are rounded once, to the cache's format, queries to
  * `dtype`.  Keys whose turned values pass float32's range are stored as a row that is
- * not finite.  q, k_new and v_new: rows of [n_q_heads][head_dim] and [n_heads][head_dim]
+ * not finite (bf16 caches: with infinities).  q, k_new and v_new: rows of [n_q_heads][head_dim] and [n_heads][head_dim]
  * elements of `dtype` at distance row_stride.  q_out may be q where q_out_stride is
  * row_stride; no other output may overlap an input.  Queries are turned whatever becomes of
  * their row's token (one that is negative, at or past max_pages * page_size or of a
@@ -605,7 +605,7 @@ marche_status_t marche_paged_append(const marche_paged_cache_t *cache, int32_t l
  * gets zeros.  Rows may stand in any order, and run fastest where those of a sequence follow
  * each other.  Pages whose tokens no row sees are not looked at: their table entries may be -1
  * (MARCHE_VALIDATE checks no page here).  Masked keys and values count nothing, whatever
- * they are.  Everything else as in marche_paged_attention, the limits too; the workspace
+ * they are; rows near a value that is not finite are computed again one by one, slowly.  Everything else as in marche_paged_attention, the limits too; the workspace
  * query likewise (for these sizes; 0 for sizes that the call refuses). */
 size_t marche_paged_attention_window_workspace_bytes(const marche_paged_cache_t *cache,
                                                      int32_t n_seqs, int32_t q_total,

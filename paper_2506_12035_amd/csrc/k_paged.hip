@@ -838,7 +838,6 @@ static void rows_plan(PagedAttnArgs &a) {
   const int rows = a.q_max * a.group;
   a.row_waves = PAGED_ROW_WAVES;
   a.waves = a.row_waves;
-  a.row_tiles = 2 * a.row_waves;
   a.row_blocks = (rows - 1) / (32 * a.row_waves) + 1;
   const int64_t units = (int64_t)a.n_seqs * a.n_heads * a.row_blocks;
   int64_t keys = a.len_max;

@@ -4,7 +4,8 @@
 //   o_i = sum_j softmax_j(q_i . K_j / sqrt(dh)) V_j
 //
 // over a sequence's cached tokens j, or over those of the pages listed for row
-// i.  The rows of one sequence that share a key head (its query heads times
+// i, of a window up to the row's own token, or of a context and the drafted tokens that
+// the row's mask names (PagedLook).  The rows of one sequence that share a key head (its query heads times
 // the sequence's rows, "packed rows") form tiles of 16; a workgroup takes up
 // to RT tiles and a range of the keys, its wavefronts alternating 32-key
 // tiles.  Per 32 keys a wavefront forms S^T = K Q^T (16 keys x 16 rows per
