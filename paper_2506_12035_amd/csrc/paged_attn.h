@@ -49,6 +49,7 @@
 #include <type_traits>
 
 #include "paged_device.h"
+#include "paged_walk.h"
 
 namespace marche {
 
@@ -559,19 +560,14 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256, MODE == PAGED_TREE ? 2 : 1) vo
     for (int x = tid; x < n; x += blockDim.x) s_bits[x] = a.mask[(size_t)(row0 + i0) * words + x];
     __syncthreads();
   }
-  // windows: what any row of the block sees is the sinks' tiles and, from tile `jump`
-  // positions further on, those from the first row's window to the last row's token
+  // windows: what any row of the block sees (paged_walk.h)
   Span sp;
-  int sink_tiles = 0, jump = 0;
+  WindowWalk<32> walk{};
   if constexpr (WIN) {
     sp = span_of(a, len, row0 + i0, i1 - i0 + 1, lane);
-    const int end = (sp.hi_max + 31) >> 5;
-    sink_tiles = (min(a.sinks, sp.hi_max) + 31) >> 5;
-    const int from = max(sp.lo_min >> 5, sink_tiles);
-    jump = from - sink_tiles;
-    const int tiles = sink_tiles + max(end - from, 0);
-    n_keys = 32 * tiles;
-    chunk = ((int)a.d_splits.div(tiles + a.splits - 1) + waves - 1) / waves * waves;
+    walk = WindowWalk<32>::of(sp.lo_min, sp.hi_max, a.sinks);
+    n_keys = 32 * walk.tiles;
+    chunk = ((int)a.d_splits.div(walk.tiles + a.splits - 1) + waves - 1) / waves * waves;
     first = split_i * chunk + wave;
   }
   const int t1 = min((split_i + 1) * chunk, (n_keys + 31) >> 5);  // the range's last tile
@@ -622,7 +618,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256, MODE == PAGED_TREE ? 2 : 1) vo
     Tile x;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int pos = 32 * (WIN && t >= sink_tiles ? t + jump : t) + 16 * u;
+      const int pos = (WIN ? walk.key(t) : 32 * t) + 16 * u;
       x.key[u] = pos;
       if (u == 1 && a.page_log2 > 4) {  // the same page
         x.lp[1] = x.lp[0];
@@ -958,7 +954,7 @@ __global__ __launch_bounds__(RT == 1 ? 512 : 256, MODE == PAGED_TREE ? 2 : 1) vo
           a, tab,
           [&](int pos) {
             if constexpr (SEL) return ((int)s_list[pos >> a.page_log2] << a.page_log2) + (pos & (page - 1));
-            else return WIN && pos >= 32 * sink_tiles ? pos + 32 * jump : pos;
+            else return WIN && pos >= 32 * walk.sink_tiles ? pos + 32 * walk.jump : pos;
           },
           [&](int i, int key) {
             if constexpr (SEL) {

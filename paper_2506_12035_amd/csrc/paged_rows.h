@@ -144,8 +144,9 @@ __global__ __launch_bounds__(QB * 64, DH == 64 && FMT != BF ? 3 : 2) void paged_
   // The range's keys, in tiles; all uniform.
   const int ctx = WIN ? 0 : max(a.ctx[b], 0);
   const uint32_t *mask = WIN ? nullptr : a.mask + (size_t)(row0 + i) * a.mask_words;
-  int w_lo = 0, w_hi = 0, sink_tiles = 0, jump = 0, base = 0, end = len, t0, t1;
+  int w_lo = 0, w_hi = 0, base = 0, end = len, t0, t1;
   Span sp{};
+  WindowWalk<ROWS_TK> walk{};
   if constexpr (WIN) {
     window_of(a, len, a.q_idx[row0 + i], w_lo, w_hi);
     // of the block's rows, 64 at a time
@@ -155,25 +156,21 @@ __global__ __launch_bounds__(QB * 64, DH == 64 && FMT != BF ? 3 : 2) void paged_
       sp = Span{min(sp.lo_min, s2.lo_min), max(sp.lo_max, s2.lo_max), min(sp.hi_min, s2.hi_min), max(sp.hi_max, s2.hi_max)};
     }
     end = sp.hi_max;
-    const int last = (end + ROWS_TK - 1) / ROWS_TK;
-    sink_tiles = (min(a.sinks, end) + ROWS_TK - 1) / ROWS_TK;
-    const int from = max(sp.lo_min / ROWS_TK, sink_tiles);
-    jump = from - sink_tiles;
-    const int tiles = sink_tiles + max(last - from, 0);
-    chunk = (int)((uint32_t)(tiles + a.splits - 1) / (uint32_t)a.splits);
+    walk = WindowWalk<ROWS_TK>::of(sp.lo_min, end, a.sinks);
+    chunk = (int)((uint32_t)(walk.tiles + a.splits - 1) / (uint32_t)a.splits);
     t0 = split_i * chunk;
-    t1 = min(t0 + chunk, tiles);
+    t1 = min(t0 + chunk, walk.tiles);
   } else {
     base = 32 * chunk * split_i;
     end = min(len, base + 32 * chunk);
     t0 = 0;
     t1 = (max(end - base, 0) + ROWS_TK - 1) / ROWS_TK;
   }
-  auto key_of = [&](int t) { return WIN ? ROWS_TK * (t >= sink_tiles ? t + jump : t) : base + ROWS_TK * t; };
+  auto key_of = [&](int t) { return WIN ? walk.key(t) : base + ROWS_TK * t; };
 
   // Page ids of a tile's four 16-key parts, -1 where there are no tokens.  Uniform, from a
-  // register that holds those of 16 tiles, asked for in order (scalar loads in the loop
-  // would make the waits for LDS reads waits for them).
+  // register that holds those of 16 tiles, the last of which may lie behind the range, asked
+  // for in order (scalar loads in the loop would make the waits for LDS reads waits for them).
   struct Pages {
     int id[4];
   };
@@ -181,8 +178,8 @@ __global__ __launch_bounds__(QB * 64, DH == 64 && FMT != BF ? 3 : 2) void paged_
   auto pages_of = [&](int t) {
     if (t - ids_at >= 16) {
       ids_at = t;
-      const int key = key_of(t + (lane >> 2)) + 16 * (lane & 3);
-      const int x = key < end ? tab[key >> a.page_log2] : -1;
+      const int key = token_of(key_of, t + (lane >> 2), t1, lane & 3, end);
+      const int x = key >= 0 ? tab[key >> a.page_log2] : -1;
       ids = (unsigned)x < (unsigned)a.n_pages ? x : -1;
     }
     Pages p;
@@ -524,7 +521,7 @@ __global__ __launch_bounds__(QB * 64, DH == 64 && FMT != BF ? 3 : 2) void paged_
     PagedAttnArgs one = a;
     if (direct) one.splits = 1;
     one_by_one<FMT, DH, bf16>(
-        one, tab, [&](int pos) { return WIN && pos >= ROWS_TK * sink_tiles ? pos + ROWS_TK * jump : pos; },
+        one, tab, [&](int pos) { return WIN && pos >= ROWS_TK * walk.sink_tiles ? pos + ROWS_TK * walk.jump : pos; },
         [&](int x, int key) {
           if constexpr (WIN) {
             int lo, hi;
