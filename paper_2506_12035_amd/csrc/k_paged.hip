@@ -946,15 +946,19 @@ hipError_t launch_paged_attention(DType dt, int32_t format, int32_t head_dim, co
   return hipErrorInvalidValue;
 }
 
+// (304 rows of 16 heads of 64 in up to 23 parts: 13.5 us with a workgroup each, 6.3 in lane groups.
+// Four in turn repeat less of what comes before the parts: 2048 rows of 32 heads of 128 in up to
+// two parts 17.1 us, 21.2 one by one; the 304 rows 15.2.)
+int paged_join_turns(int32_t head_dim, const PagedAttnArgs &a) {
+  const int64_t n = (int64_t)a.q_total * a.n_heads * a.group;
+  if (a.row_waves == 0 && ((a.look != PAGED_WINDOW && a.look != PAGED_TREE) || n < 4096)) return 0;
+  return n >= 4096 * paged_join_groups(head_dim) ? 4 : 1;
+}
+
 hipError_t launch_paged_join(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)a.q_total * a.n_heads * a.group);
-  // (304 rows of 16 heads of 64 in up to 23 parts: 13.5 us with a workgroup each, 6.3 so.
-  // Four in turn repeat less of what comes before the parts: 2048 rows of 32 heads of 128 in up to
-  // two parts 17.1 us, 21.2 one by one; the 304 rows 15.2.)
-  if (a.row_waves > 0 || ((a.look == PAGED_WINDOW || a.look == PAGED_TREE) && grid >= 4096)) {
-    const unsigned per = head_dim == 64 ? 16 : 8;
-    const int times = grid >= 4096 * per ? 4 : 1;
-    const unsigned groups = (grid + per * times - 1) / (per * times);
+  if (const int times = paged_join_turns(head_dim, a)) {
+    const unsigned per = paged_join_groups(head_dim) * times, groups = (grid + per - 1) / per;
     return by_shape(BF, head_dim, [&](auto, auto dh) {
       if (dt == DType::BF16) launch_kernel(paged_rows_join_kernel<dh.value, bf16>, groups, 256, 0, s, a, times);
       else launch_kernel(paged_rows_join_kernel<dh.value, float>, groups, 256, 0, s, a, times);

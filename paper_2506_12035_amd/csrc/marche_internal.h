@@ -342,6 +342,7 @@ enum PagedLook : int32_t { PAGED_ALL = 0, PAGED_LISTED = 1, PAGED_WINDOW = 2, PA
 constexpr int PAGED_ROW_WAVES = 4;  // wavefronts of 32 rows of a workgroup of paged_rows.h
 constexpr int PAGED_MAX_MASK_WORDS = 64;  // of 32 drafted tokens each
 constexpr int PAGED_JOIN_THREADS = 256;  // of the join's workgroup, one per (row, query head)
+constexpr int paged_join_groups(int32_t head_dim) { return head_dim == 64 ? 16 : 8; }  // lane groups of the rows' join
 constexpr int PAGED_MAX_SHARED = 256;  // sequences of a call whose ranges are shared out on the device
 struct PagedAttnArgs {
   const void *k, *v;
@@ -376,6 +377,8 @@ int64_t paged_grid(const PagedAttnArgs &a);
 void paged_plan(DType dt, int32_t head_dim, PagedAttnArgs &a);
 hipError_t launch_paged_attention(DType dt, int32_t format, int32_t head_dim, const PagedAttnArgs &a,
                                   hipStream_t s);
+// How many (row, query head) pairs a lane group of the join takes in turn, or 0: a workgroup each.
+int paged_join_turns(int32_t head_dim, const PagedAttnArgs &a);
 hipError_t launch_paged_join(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
 hipError_t launch_paged_attention_bf16(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);
 hipError_t launch_paged_attention_e4m3(DType dt, int32_t head_dim, const PagedAttnArgs &a, hipStream_t s);

@@ -8,6 +8,7 @@ import pytest
 
 from paper_2506_12035_amd import build
 
+import test_gpu_paged_joins as joins
 import test_gpu_paged_many_rows as many
 from test_abi_paged import built_library  # noqa: F401
 
@@ -34,7 +35,7 @@ int main() {
     a.window = window;
     a.sinks = sinks;
     paged_plan(f32 ? DType::F32 : DType::BF16, dh, a);
-    std::printf("%d %d %d\n", a.row_waves, a.splits, a.budget);
+    std::printf("%d %d %d %d\n", a.row_waves, a.splits, a.budget, paged_join_turns(dh, a));
   }
 }
 """
@@ -58,13 +59,19 @@ def program(tmp_path_factory, built_library):  # noqa: F811
 @pytest.fixture(scope="module")
 def plan(program):
     """(dtype, dh, seqs, rows in all, rows of a sequence, heads, group, len_max, look, window, sinks) ->
-    dict of row_waves, splits, budget"""
+    dict of row_waves, splits, budget, turns (of the join)"""
     def ask(dtype, dh, seqs, total, most, heads, group, len_max, look, window=1, sinks=0):
         sizes = [int(dtype == "f32"), dh, seqs, total, most, heads, group, len_max, LOOK[look], window, sinks]
-        return dict(zip(("row_waves", "splits", "budget"), program(sizes)))
+        return dict(zip(("row_waves", "splits", "budget", "turns"), program(sizes)))
     return ask
 
 
 @pytest.mark.parametrize("case", many.by_blocks(), ids=lambda c: f"{c['look']}-{c['dh']}-{c['heads']}h-{c['most']}r-{c['len_max']}")
 def test_many_rows_go_by_blocks(plan, case):
     assert plan(**case)["row_waves"] > 0
+
+
+@pytest.mark.parametrize("case,many_rows,turns", joins.plans(), ids=[joins._name(c) for c in joins.CASES])
+def test_joins_are_reached(plan, case, many_rows, turns):
+    p = plan(**case)
+    assert (p["row_waves"] > 0, p["splits"] > 1, p["turns"]) == (many_rows, True, turns)
