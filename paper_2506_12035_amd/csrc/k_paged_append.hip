@@ -4,8 +4,8 @@
 // Pair i of a head's channels (x, y) at position p (on the pair's axis) becomes
 //   (x cos t - y sin t, y cos t + x sin t),   t = p * freq_i.
 // The angle is formed in turns and in 64 bits and reduced there to an eighth of a turn
-// to either side, as float32 has no bits left for far positions (2^20 times any
-// frequency is off by 0.06 radians); sine and cosine of what is left are float32
+// to either side, as float32 has no bits left for far positions (at 2^20 a frequency
+// near 1 gives angles off by up to 0.06 radians); sine and cosine of what is left are float32
 // polynomials.  Keys go from float32 to the cache's format by one rounding.
 //
 // Bound by bytes: 40960 rows of 12 heads of 64, three axes, bf16 to int8, 316 MB: 76.4 us,
@@ -165,12 +165,18 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedTurns turns, Pag
   else run(std::integral_constant<int, 2>(), id - a.q_blocks - a.kv_blocks);
 }
 
+// Four heads a lane group share the angles where that leaves 1024 wavefronts or more of 64
+// channels (2048 of 80 and 128); below, a head each is the shorter way.
+PagedAppendPlan paged_append_plan(DType dt, int32_t head_dim, int32_t a_total, int32_t q_heads, int32_t n_heads) {
+  const int64_t pairs = (int64_t)a_total * (q_heads + 2 * n_heads);
+  return PagedAppendPlan{pairs >= 32768 && n_heads >= 4 ? 4 : 1, (double)pairs * head_dim * (dt == DType::BF16 ? 2 : 4) >= 64e6};
+}
+
 hipError_t launch_paged_append(DType dt, int32_t format, int32_t head_dim, bool halves, const PagedTurns &turns,
                                PagedAppendArgs a, hipStream_t s) {
-  // Four heads a lane group share the angles where that leaves 2048 wavefronts or more of 64
-  // channels; below, a head each is the shorter way.
-  const int64_t pairs = (int64_t)a.a_total * (a.q_heads + 2 * a.n_heads);
-  const int n = pairs >= 32768 && a.n_heads >= 4 ? 4 : 1;
+  const PagedAppendPlan plan = paged_append_plan(dt, head_dim, a.a_total, a.q_heads, a.n_heads);
+  const int n = plan.heads;
+  const bool stream = plan.stream;
   const int per = paged_write_pairs(head_dim);
   a.q_slots = std::max(1, (a.q_heads + n - 1) / n);
   a.kv_slots = (a.n_heads + n - 1) / n;
@@ -180,7 +186,6 @@ hipError_t launch_paged_append(DType dt, int32_t format, int32_t head_dim, bool 
   a.q_blocks = a.q_heads ? (uint32_t)(((int64_t)a.a_total * a.q_slots + per - 1) / per) : 0;
   a.kv_blocks = (uint32_t)(((int64_t)a.a_total * a.kv_slots + per - 1) / per);
   const unsigned grid = a.q_blocks + 2 * a.kv_blocks;
-  const bool stream = (double)pairs * head_dim * (dt == DType::BF16 ? 2 : 4) >= 64e6;
   return by_shape(format, head_dim, [&](auto fmt, auto dh) {
     auto go = [&](auto half, auto several, auto st) {
       constexpr bool H = half.value, S = st.value;

@@ -295,6 +295,12 @@ struct PagedAppendArgs {
   uint32_t q_blocks, kv_blocks;
   FastDiv d_q_slots, d_kv_slots, d_rows;
 };
+// Heads of a row that a lane group takes, and whether rows go past the caches.
+struct PagedAppendPlan {
+  int heads;
+  bool stream;
+};
+PagedAppendPlan paged_append_plan(DType dt, int32_t head_dim, int32_t a_total, int32_t q_heads, int32_t n_heads);
 hipError_t launch_paged_append(DType dt, int32_t format, int32_t head_dim, bool halves, const PagedTurns &turns,
                                PagedAppendArgs a, hipStream_t s);
 constexpr int PAGED_READ_TOKENS = 128;  // tokens per workgroup of the read kernel

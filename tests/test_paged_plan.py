@@ -8,6 +8,7 @@ import pytest
 
 from paper_2506_12035_amd import build
 
+import test_gpu_paged_append_many as appends
 import test_gpu_paged_joins as joins
 import test_gpu_paged_many_rows as many
 from test_abi_paged import built_library  # noqa: F401
@@ -17,7 +18,15 @@ PROGRAM = r"""
 #include <cstdio>
 #include "marche_internal.h"
 using namespace marche;
-int main() {
+int main(int argc, char **) {
+  if (argc > 1) {  // appends
+    int f32, dh, rows, q_heads, heads;
+    while (std::scanf("%d %d %d %d %d", &f32, &dh, &rows, &q_heads, &heads) == 5) {
+      const PagedAppendPlan p = paged_append_plan(f32 ? DType::F32 : DType::BF16, dh, rows, q_heads, heads);
+      std::printf("%d %d\n", p.heads, (int)p.stream);
+    }
+    return 0;
+  }
   int f32, dh, seqs, total, most, heads, group, len, look, window, sinks;
   while (std::scanf("%d %d %d %d %d %d %d %d %d %d %d", &f32, &dh, &seqs, &total, &most, &heads, &group, &len, &look, &window,
                     &sinks) == 11) {
@@ -50,8 +59,8 @@ def program(tmp_path_factory, built_library):  # noqa: F811
                         f"-Wl,-rpath,{build.PKG}", "-o", str(d / "plan")], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
 
-    def run(sizes):
-        r = subprocess.run([str(d / "plan")], input=" ".join(map(str, sizes)), capture_output=True, text=True, check=True)
+    def run(sizes, *args):
+        r = subprocess.run([str(d / "plan"), *args], input=" ".join(map(str, sizes)), capture_output=True, text=True, check=True)
         return list(map(int, r.stdout.split()))
     return run
 
@@ -75,3 +84,8 @@ def test_many_rows_go_by_blocks(plan, case):
 def test_joins_are_reached(plan, case, many_rows, turns):
     p = plan(**case)
     assert (p["row_waves"] > 0, p["splits"] > 1, p["turns"]) == (many_rows, True, turns)
+
+
+@pytest.mark.parametrize("sizes,heads,stream", appends.plans(), ids=lambda x: "-".join(map(str, x)) if isinstance(x, tuple) else str(x))
+def test_appends_take_four_heads(program, sizes, heads, stream):
+    assert program([int(sizes[0] == "f32"), *sizes[1:]], "append") == [heads, stream]
