@@ -820,17 +820,34 @@ static void share_out(PagedAttnArgs &a, int64_t tiles, int waves, int64_t slots)
   a.splits = (int32_t)std::min<int64_t>({64, a.budget, most});
 }
 
+// Tokens that a block of `rows` neighbouring rows walks through at most.
+static int64_t block_keys(const PagedAttnArgs &a, int64_t rows) {
+  return a.look == PAGED_WINDOW ? std::min<int64_t>(a.len_max, (int64_t)a.sinks + a.window + rows + 126) : a.len_max;
+}
+
 // Whether windows and trees go by blocks of many rows (paged_rows.h): bf16 rows, more
-// than half a block of them for a key head, and blocks for a good part of the chip, as a
-// block's wavefronts do not share its keys out.  Heads of 128 over e4m3 caches up to 8000
-// tokens: 32 sequences of 64 (packed) rows 148.3 us by blocks and 133.6 without, of 128 rows 170.1 and
-// 231.7; 16 blocks in all 43.9 and 33.6, 24 43.8 and 38.3, 32 44.5 and 47.7.  Windows of 1024, heads of
-// 64: 110 blocks 26.2 and 21.0, 128 25.1 and 22.8, 160 29.6 and 31.4, 256 33.4 and 36.5, 1024
-// 66.2 and 101.0.
+// than half a block of them for a key head, and blocks for the whole chip or, as a block's
+// wavefronts do not share its keys out, long enough walks for a part of it.  By blocks and by
+// the few-row kernel, us (one box):
+//   heads of 64, bf16, windows   of 256: 128 blocks 15.6 and 13.3, 512 20.5 and 22.8; of 1024: 128 28.6 and 20.6,
+//     384 49.2 and 39.0, 512 35.8 and 51.8; of 4096: 128 39.3 and 48.1; of 8192: 32 30.9 and 38.7, 64 41.2 and 57.1
+//   heads of 80, bf16, windows of 1024: 256 blocks 43.9 and 37.3, 512 48.1 and 61.4
+//   heads of 64, bf16, trees   over 600 tokens: 128 blocks 18.6 and 15.2, 256 21.5 and 22.9; over 4000: 128 47.8 and 61.2
+//   heads of 128, bf16, windows   of 256: 32 blocks 17.6 and 12.8, 96 18.2 and 24.5; of 1024: 32 23.9 and 30.0
+//   heads of 128, e4m3, windows   of 1024: 128 blocks 40.7 and 28.4, 384 71.4 and 79.3; of 4096: 128 64.9 and 70.1
+//   heads of 128, e4m3, trees   over 300 tokens: 64 blocks 17.4 and 12.6; over 2000: 64 33.1 and 32.3; up to 8000:
+//     16 43.3 and 32.7, 32 44.5 and 51.6
+// Over 716 such pairs of times the choice is 1.7% behind the better one in the mean (6.5% with a number of
+// blocks alone), at worst 1.5 times (windows of 256, heads of 128, 64 blocks).
 static bool by_rows(DType dt, int32_t head_dim, const PagedAttnArgs &a) {
   const int64_t rows = (int64_t)a.q_max * a.group, block = 32 * PAGED_ROW_WAVES;
-  if (dt != DType::BF16 || (a.look != PAGED_WINDOW && a.look != PAGED_TREE) || rows <= block / 2) return false;
-  return (int64_t)a.n_seqs * a.n_heads * ((rows + block - 1) / block) >= (head_dim == 128 ? 32 : 128);
+  const bool tree = a.look == PAGED_TREE;
+  if (dt != DType::BF16 || (a.look != PAGED_WINDOW && !tree) || rows <= block / 2) return false;
+  const int64_t blocks = std::min<int64_t>((int64_t)a.n_seqs * a.n_heads * ((rows + block - 1) / block), 1 << 20);
+  const int64_t walk = blocks * block_keys(a, block / a.group);
+  if (blocks < 32) return false;
+  if (head_dim == 128 && (tree || !a.bits8)) return walk >= 32 << 10;
+  return blocks >= (tree ? 256 : head_dim == 128 ? 384 : 512) || walk >= 448 << 10;
 }
 
 // Their plan.
@@ -840,10 +857,7 @@ static void rows_plan(PagedAttnArgs &a) {
   a.waves = a.row_waves;
   a.row_blocks = (rows - 1) / (32 * a.row_waves) + 1;
   const int64_t units = (int64_t)a.n_seqs * a.n_heads * a.row_blocks;
-  int64_t keys = a.len_max;
-  if (a.look == PAGED_WINDOW)
-    keys = std::min<int64_t>(keys, (int64_t)a.sinks + a.window + 32 * a.row_waves / a.group + 126);
-  const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32);
+  const int64_t tiles = std::max<int64_t>(1, (block_keys(a, 32 * a.row_waves / a.group) + 31) / 32);
   // two workgroups for each compute unit, twelve 32-key tiles each at least (a prompt of 512 rows, 128
   // blocks: 31.4 us in two ranges of eight tiles, 20.9 in one)
   const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({64, (512 + units - 1) / units, tiles / 12}));

@@ -1220,6 +1220,7 @@ void paged_attn_sizes(PagedAttnArgs &p, const marche_paged_cache_t *c, int32_t n
   p.group = n_q_heads / c->n_heads;
   p.len_max = len_max;
   p.n_select = n_select;
+  p.bits8 = raw_enum(c->format) != MARCHE_CACHE_BF16;
   paged_plan(dt, c->head_dim, p);
 }
 

@@ -365,6 +365,7 @@ struct PagedAttnArgs {
   int32_t n_pages, n_heads, page_log2, max_pages, n_seqs, q_total, q_max, rows_each, group, len_max,
       n_select;
   int32_t look, window, sinks, mask_words;  // PagedLook
+  int32_t bits8;  // whether the cache holds 8 bits
   float sl2;  // log2(e) / sqrt(head_dim)
   // the plan (paged_plan): 16-row tiles and wavefronts per workgroup, row
   // blocks per sequence, key ranges, 32-key tiles per range, rows of a block

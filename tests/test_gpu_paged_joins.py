@@ -43,9 +43,9 @@ def _name(c):
 
 def plans():
     """(sizes, what their plan has to be) of the calls below."""
-    return [(dict(dtype=dtype, dh=dh, seqs=len(rows), total=before + sum(rows) + extra, most=max(rows), heads=H, group=group,
+    return [(dict(dtype=dtype, fmt=fmt, dh=dh, seqs=len(rows), total=before + sum(rows) + extra, most=max(rows), heads=H, group=group,
                   len_max=max(lens), look=look, window=max(1, size), sinks=sinks), many, turns)
-            for look, dtype, dh, H, group, _, lens, rows, before, extra, size, sinks, many, turns in CASES]
+            for look, dtype, dh, H, group, fmt, lens, rows, before, extra, size, sinks, many, turns in CASES]
 
 
 @pytest.mark.parametrize("case", CASES, ids=_name)

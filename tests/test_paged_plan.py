@@ -11,6 +11,7 @@ from paper_2506_12035_amd import build
 import test_gpu_paged_append_many as appends
 import test_gpu_paged_joins as joins
 import test_gpu_paged_many_rows as many
+import test_gpu_paged_window_limits as limits
 from test_abi_paged import built_library  # noqa: F401
 
 LOOK = {"all": 0, "window": 2, "tree": 3}
@@ -27,9 +28,9 @@ int main(int argc, char **) {
     }
     return 0;
   }
-  int f32, dh, seqs, total, most, heads, group, len, look, window, sinks;
-  while (std::scanf("%d %d %d %d %d %d %d %d %d %d %d", &f32, &dh, &seqs, &total, &most, &heads, &group, &len, &look, &window,
-                    &sinks) == 11) {
+  int f32, bits8, dh, seqs, total, most, heads, group, len, look, window, sinks;
+  while (std::scanf("%d %d %d %d %d %d %d %d %d %d %d %d", &f32, &bits8, &dh, &seqs, &total, &most, &heads, &group, &len, &look, &window,
+                    &sinks) == 12) {
     PagedAttnArgs a{};
     a.n_pages = 1 << 20;
     a.n_heads = heads;
@@ -41,6 +42,7 @@ int main(int argc, char **) {
     a.group = group;
     a.len_max = len;
     a.look = look;
+    a.bits8 = bits8;
     a.window = window;
     a.sinks = sinks;
     paged_plan(f32 ? DType::F32 : DType::BF16, dh, a);
@@ -67,15 +69,16 @@ def program(tmp_path_factory, built_library):  # noqa: F811
 
 @pytest.fixture(scope="module")
 def plan(program):
-    """(dtype, dh, seqs, rows in all, rows of a sequence, heads, group, len_max, look, window, sinks) ->
+    """(dtype, format, dh, seqs, rows in all, rows of a sequence, heads, group, len_max, look, window, sinks) ->
     dict of row_waves, splits, budget, turns (of the join)"""
-    def ask(dtype, dh, seqs, total, most, heads, group, len_max, look, window=1, sinks=0):
-        sizes = [int(dtype == "f32"), dh, seqs, total, most, heads, group, len_max, LOOK[look], window, sinks]
+    def ask(dtype, fmt, dh, seqs, total, most, heads, group, len_max, look, window=1, sinks=0):
+        sizes = [int(dtype == "f32"), int(fmt != "bf16"), dh, seqs, total, most, heads, group, len_max, LOOK[look], window, sinks]
         return dict(zip(("row_waves", "splits", "budget", "turns"), program(sizes)))
     return ask
 
 
-@pytest.mark.parametrize("case", many.by_blocks(), ids=lambda c: f"{c['look']}-{c['dh']}-{c['heads']}h-{c['most']}r-{c['len_max']}")
+@pytest.mark.parametrize("case", many.by_blocks() + limits.by_blocks(), ids=lambda c: "-".join(str(c[k]) for k in (
+    "look", "fmt", "dh", "heads", "most", "group", "len_max", "window")))
 def test_many_rows_go_by_blocks(plan, case):
     assert plan(**case)["row_waves"] > 0
 
