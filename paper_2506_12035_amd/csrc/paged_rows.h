@@ -83,6 +83,9 @@ __device__ __forceinline__ float half_sum(float v) {
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
+// (Three workgroups a compute unit for 8-bit heads of 64, which spill 6 or 7 registers for it: 8192 rows
+// of 12 heads over windows of 1024 in e4m3 59.8 us, 75.4 with two and no spill; 32 trees of 64 x 4 x 8 over 1100 ..
+// 8000 tokens 154 and 168; windows of 8192 206 and 196.)
 template <int FMT, int DH, int QB, int MODE>
 __global__ __launch_bounds__(QB * 64, DH == 64 && FMT != BF ? 3 : 2) void paged_rows_kernel(PagedAttnArgs a, const int32_t *__restrict__ table) {
   using L = RowsLay<DH>;
