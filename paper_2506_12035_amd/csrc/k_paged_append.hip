@@ -5,8 +5,10 @@
 //   (x cos t - y sin t, y cos t + x sin t),   t = p * freq_i.
 // The angle is formed in turns and in 64 bits and reduced there to an eighth of a turn
 // to either side, as float32 has no bits left for far positions (at 2^20 a frequency
-// near 1 gives angles off by up to 0.06 radians); sine and cosine of what is left are float32
-// polynomials.  Keys go from float32 to the cache's format by one rounding.
+// near 1 gives angles off by up to 0.06 radians); sine and cosine of what is left are
+// polynomials in 64 bits, rounded once (12.0 us for 1826 fp32 rows of 48 heads of 80, 11.7 with sums in
+// float32, which were off by up to 1.8 times what the products may be).  Keys go from float32 to
+// the cache's format by one rounding.
 //
 // Bound by bytes: 40960 rows of 12 heads of 64, three axes, bf16 to int8, 316 MB: 76.4 us,
 // 4.1 TB/s (93.6 with queries, keys and values of a row side by side in a wavefront, which
@@ -17,25 +19,26 @@
 
 namespace marche {
 
-// Sine and cosine of 2 pi pos turn: Taylor's sums on [-pi/4, pi/4], whose next terms are
-// below 2e-9 (sine, x^11 / 11!) and 2e-10 (cosine, x^12 / 12!).
+// Sine and cosine of 2 pi pos turn, the nearest float32 numbers: Taylor's sums on [-pi/4, pi/4] in
+// 64 bits, whose next terms are below 1e-11 (sine, x^13 / 13!) and 2e-10 (cosine, x^12 / 12!).
 __device__ __forceinline__ void turn(int pos, double per, float &sn, float &cs) {
   double t = (double)pos * per;
   t -= rint(t);
   const double quarter = rint(4.0 * t);  // -2 .. 2
-  const float x = (float)fma(-0.25, quarter, t) * 6.28318530717958648f;
-  const float z = x * x;
-  float s = fmaf(z, 2.75573192e-6f, -1.98412698e-4f);
-  s = fmaf(z, s, 8.33333333e-3f);
-  s = fmaf(z, s, -1.66666667e-1f);
-  s = fmaf(x * z, s, x);
-  float c = fmaf(z, -2.75573192e-7f, 2.48015873e-5f);
-  c = fmaf(z, c, -1.38888889e-3f);
-  c = fmaf(z, c, 4.16666667e-2f);
-  c = fmaf(z, c, -0.5f);
-  c = fmaf(z, c, 1.f);
+  const double x = fma(-0.25, quarter, t) * 6.283185307179586477;
+  const double z = x * x;
+  double s = fma(z, -1.0 / 39916800, 1.0 / 362880);
+  s = fma(z, s, -1.0 / 5040);
+  s = fma(z, s, 1.0 / 120);
+  s = fma(z, s, -1.0 / 6);
+  s = fma(x * z, s, x);
+  double c = fma(z, -1.0 / 3628800, 1.0 / 40320);
+  c = fma(z, c, -1.0 / 720);
+  c = fma(z, c, 1.0 / 24);
+  c = fma(z, c, -0.5);
+  c = fma(z, c, 1.0);
   const int q = (int)quarter & 3;
-  const float a = q & 1 ? c : s, b = q & 1 ? s : c;
+  const float a = (float)(q & 1 ? c : s), b = (float)(q & 1 ? s : c);
   sn = q & 2 ? -a : a;
   cs = (q + 1) & 2 ? -b : b;
 }
