@@ -577,17 +577,19 @@ marche_status_t marche_rotary_init(marche_rotary_t *rotary, int32_t head_dim, in
                                    double base);
 
 /* marche_paged_write with the rotation on the way: row r's keys, turned by its
- * positions pos[axis][r] (pos [rotary->n_axes][a_total] int32, device, any sign; NULL: a_idx[r] on
- * every axis), and its values become token a_idx[r] of its sequence, and its queries,
- * turned likewise, go to row r of q_out (rows q_out_stride apart).  Angles are formed in 64
- * bits, the rotation in float32; keys are rounded once, to the cache's format, queries to
- * `dtype`.  Keys whose turned values pass float32's range are stored as a row that is
- * not finite (bf16 caches: with infinities).  q, k_new and v_new: rows of [n_q_heads][head_dim] and [n_heads][head_dim]
- * elements of `dtype` at distance row_stride.  q_out may be q where q_out_stride is
+ * positions pos[axis][r] (pos [rotary->n_axes][a_total] int32, device, any sign; NULL: a_idx[r]
+ * on every axis), and its values become token a_idx[r] of its sequence, and its queries,
+ * turned likewise, go to row r of q_out (rows q_out_stride apart).  Angles and their sines
+ * and cosines are formed in 64 bits and these rounded to float32, as the rotation is; then
+ * keys are rounded once, to the cache's format, queries to `dtype`.  Keys whose turned values
+ * pass float32's range are stored as a row that is not finite (bf16 caches: with infinities).
+ * q, k_new and v_new: rows of [n_q_heads][head_dim] and [n_heads][head_dim] elements of
+ * `dtype` at distance row_stride.  q_out may be q where q_out_stride is
  * row_stride; no other output may overlap an input.  Queries are turned whatever becomes of
  * their row's token (one that is negative, at or past max_pages * page_size or of a
  * page outside the pool is not written).  q and q_out NULL, n_q_heads 0: keys and
- * values alone.  a_total * (n_q_heads + 2 n_heads) <= 2^28 - 64.  Bounds of the pages (marche_paged_bounds) are of the turned keys. */
+ * values alone.  a_total * (n_q_heads + 2 n_heads) <= 2^28 - 64.  Bounds of the pages
+ * (marche_paged_bounds) are of the turned keys. */
 marche_status_t marche_paged_append(const marche_paged_cache_t *cache, int32_t layer,
                                     const int32_t *page_table, int32_t max_pages, int32_t n_seqs,
                                     const int32_t *a_idx, const int32_t *a_off, int32_t a_total,
@@ -600,13 +602,15 @@ marche_status_t marche_paged_append(const marche_paged_cache_t *cache, int32_t l
  * sequence ([q_total] int32, device), sees the cached tokens j with
  *   j < lens[b],  j <= t,  and  j > t - window or j < sinks,
  * so the last `window` tokens up to its own and the sequence's first `sinks` ones (window
- * INT32_MAX: every token up to its own, for t < INT32_MAX).  window >= 1, sinks >= 0.  t may lie past lens[b]
- * (its keys not yet written) or be negative (the row sees nothing); a row that sees nothing
- * gets zeros.  Rows may stand in any order, and run fastest where those of a sequence follow
- * each other.  Pages whose tokens no row sees are not looked at: their table entries may be -1
- * (MARCHE_VALIDATE checks no page here).  Masked keys and values count nothing, whatever
- * they are; rows near a value that is not finite are computed again one by one, slowly.  Everything else as in marche_paged_attention, the limits too; the workspace
- * query likewise (for these sizes; 0 for sizes that the call refuses). */
+ * INT32_MAX: every token up to its own, for t < INT32_MAX).  window >= 1, sinks >= 0.  t may
+ * lie past lens[b] (its keys not yet written) or be negative (the row sees nothing); a row
+ * that sees nothing gets zeros.  Rows may stand in any order, and run fastest where those of
+ * a sequence follow each other.  The launch is laid out for q_max rows of every sequence: one
+ * prompt and many single rows are faster in two calls.  Pages whose tokens no row sees are
+ * not looked at: their table entries may be -1 (MARCHE_VALIDATE checks no page here).  Masked
+ * keys and values count nothing, whatever they are; rows near a value that is not finite are
+ * computed again one by one, slowly.  Everything else as in marche_paged_attention, the limits
+ * too; the workspace query likewise (for these sizes; 0 for sizes that the call refuses). */
 size_t marche_paged_attention_window_workspace_bytes(const marche_paged_cache_t *cache,
                                                      int32_t n_seqs, int32_t q_total,
                                                      int32_t q_max, int32_t n_q_heads,

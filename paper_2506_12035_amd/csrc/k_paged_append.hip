@@ -10,9 +10,9 @@
 // float32, which were off by up to 1.8 times what the products may be).  Keys go from float32 to
 // the cache's format by one rounding.
 //
-// Bound by bytes: 40960 rows of 12 heads of 64, three axes, bf16 to int8, 316 MB: 76.4 us,
+// Bound by bytes: 40960 rows of 12 heads of 64, three axes, bf16 to int8, 316 MB: 76.9 us,
 // 4.1 TB/s (93.6 with queries, keys and values of a row side by side in a wavefront, which
-// then ran each other's instructions).  One row of 48 heads: 3.2 us, latency.
+// then ran each other's instructions).  One row of 48 heads: 3.0 us, latency.
 #include <algorithm>
 
 #include "paged_device.h"

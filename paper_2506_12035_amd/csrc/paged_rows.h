@@ -13,10 +13,10 @@
 //
 // Bound: LDS, which every wavefront reads 32 KB a tile from (heads of 128) for 32 products'
 // 1024 cycles, beside 1100 cycles of vector instructions: 8192 rows of 32 heads over
-// windows of 8192 take 561 .. 599 us (0.92 .. 0.98 PFLOP/s), without its reads 479, without loads to it
-// 503, without either 368.  Over windows of 1024 (173 .. 197 us by the box, 0.65 .. 0.75 PFLOP/s) the
-// start and the end of each workgroup count too: windows of one token take 58 us.  8-bit formats
-// convert a tile once for the workgroup: 218 us in e4m3.
+// windows of 8192 take 537 .. 599 us by the box (0.92 .. 1.02 PFLOP/s); where they took 599, 479 without its
+// reads, 503 without loads to it, 368 without either.  Over windows of 1024 (172 .. 190 us by the box, 0.68 .. 0.75
+// PFLOP/s) the start and the end of each workgroup count too: windows of one token take 57 us.  8-bit formats
+// convert a tile once for the workgroup: 213 .. 218 us in e4m3, 231 in int8.
 #pragma once
 
 #include "paged_attn.h"
