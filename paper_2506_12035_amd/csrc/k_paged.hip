@@ -837,17 +837,17 @@ static int64_t block_keys(const PagedAttnArgs &a, int64_t rows) {
 //   heads of 128, e4m3, windows   of 1024: 128 blocks 40.7 and 28.4, 384 71.4 and 79.3; of 4096: 128 64.9 and 70.1
 //   heads of 128, e4m3, trees   over 300 tokens: 64 blocks 17.4 and 12.6; over 2000: 64 33.1 and 32.3; up to 8000:
 //     16 43.3 and 32.7, 32 44.5 and 51.6
-// Over 716 such pairs of times the choice is 1.7% behind the better one in the mean (6.5% with a number of
+// Over 806 such pairs of times the choice is 1.4% behind the better one in the mean (7.3% with a number of
 // blocks alone), at worst 1.5 times (windows of 256, heads of 128, 64 blocks).
 static bool by_rows(DType dt, int32_t head_dim, const PagedAttnArgs &a) {
   const int64_t rows = (int64_t)a.q_max * a.group, block = 32 * PAGED_ROW_WAVES;
   const bool tree = a.look == PAGED_TREE;
   if (dt != DType::BF16 || (a.look != PAGED_WINDOW && !tree) || rows <= block / 2) return false;
   const int64_t blocks = std::min<int64_t>((int64_t)a.n_seqs * a.n_heads * ((rows + block - 1) / block), 1 << 20);
-  const int64_t walk = blocks * block_keys(a, block / a.group);
+  const int64_t keys = block_keys(a, block / a.group);
   if (blocks < 32) return false;
-  if (head_dim == 128 && (tree || !a.bits8)) return walk >= 32 << 10;
-  return blocks >= (tree ? 256 : head_dim == 128 ? 384 : 512) || walk >= 448 << 10;
+  if (head_dim == 128 && (tree || !a.bits8)) return blocks * keys >= 32 << 10;
+  return blocks >= (tree ? 256 : head_dim == 128 ? 384 : 512) || blocks * keys >= 448 << 10 || keys >= 6 << 10;
 }
 
 // Their plan.
